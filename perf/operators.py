@@ -170,8 +170,10 @@ def _order(d, device):
 def _quantised(x):
     """(codes [..., D] of 0 to 15, scale and minimum [..., D/64][2] in bfloat16) of rows in 32 bits."""
     g = x.unflatten(-1, (-1, GROUP))
-    m = g.amin(-1).bfloat16()
-    s = ((g.amax(-1) - m.float()) / 15).clamp(0, 65280).bfloat16()
+    u = g.amin(-1).view(torch.int32)  # the largest bfloat16 that is not above the minimum
+    m = torch.where((u < 0) & (u & 0xFFFF != 0), u + 0x10000, u).bitwise_and(-0x10000).view(torch.float32).bfloat16()
+    u = ((g.amax(-1) - m.float()) / 15).clamp(0, 65280).view(torch.int32)  # and the smallest that is not below the step
+    s = (u + 0xFFFF).bitwise_and(-0x10000).view(torch.float32).bfloat16()
     c = torch.where(s[..., None] > 0, torch.round((g - m.float()[..., None]) / s.float()[..., None]), torch.zeros_like(g))
     return c.clamp(0, 15).to(torch.uint8).flatten(-2), torch.stack((s, m), -1)
 
@@ -554,8 +556,12 @@ def _exact_held(x):
     parts = []
     for j in range(0, x.shape[-1], GROUP):
         y = x[..., j:j + GROUP]
-        low = y.min(-1, keepdim=True).values.bfloat16().double()
-        step = ((y.max(-1, keepdim=True).values - low) / 15).clamp(0, 65280).bfloat16().double()
+        least = y.min(-1, keepdim=True).values
+        low = least.bfloat16()
+        low = torch.where(low.double() > least, torch.nextafter(low, torch.full_like(low, -math.inf)), low).double()
+        most = ((y.max(-1, keepdim=True).values - low) / 15).clamp(0, 65280)
+        step = most.bfloat16()
+        step = torch.where(step.double() < most, torch.nextafter(step, torch.full_like(step, math.inf)), step).double()
         code = ((y - low) / step.clamp(min=1e-300)).round().clamp(0, 15)
         parts.append(code * step + low)
     return torch.cat(parts, -1)
