@@ -320,6 +320,138 @@ remp_status remp_weights_reshard(const remp_topo* topo, int32_t num_layers, cons
                                  int32_t num_params, void* const* dst_shards, int64_t* h2d_bytes, int32_t max_ctas,
                                  void* stream);
 
+/* ---- serving from a cache held in 4 bits, between two topology switches ----
+ *
+ * A rank's pool as remp_shard describes it, whose elements are 4-bit codes. A row of one head (head_dim values of K or
+ * of V for one token) is cut into groups of 64 dims; a group keeps its minimum m and its step s in bfloat16 and stands
+ * for s*c + m with codes c of 0 to 15:
+ *     m = largest bfloat16 <= min x,  s = smallest bfloat16 >= min((max x - m) * (1/15), 65280),  c = clamp(rint((x - m) / s), 0, 15)
+ * (all in 32 bits, 1/15 too; rint to nearest even; s = 0: every code is 0), so the codes span every value and none is
+ * off by more than s/2. A group that holds a NaN or an infinity is kept as
+ * m = NaN, s = 0: it stands for NaN in every dim. Rows take remp_kvq_token_bytes(head_dim) = head_dim/2 + head_dim/16
+ * bytes for each of K and V, 3.6 times fewer than in 16 bits.
+ * A head slice (one block, one head, K or V) is block_size/16 tiles of 16 tokens, each [16][head_dim/2] bytes of codes
+ * followed by [16][head_dim/64] pairs (s, m) of bfloat16. Inside a token's codes the dims stand in the order in which a
+ * warp's matrix instructions take them. Place n (nibble n%2 of byte n/2) holds, with D = head_dim,
+ *     K: dim 32*((n % (D/4)) / 8) + 8*(n % 4) + 2*(n / (D/4)) + (n % 8) / 4
+ *     V: dim 8*(n % (D/8)) + n / (D/8)
+ * For remp_migrate_kv and remp_pages_copy a slice is opaque bytes: describe the cache with head_dim = token bytes and
+ * elem_bytes = 1 and move whole blocks (dense head slices; not REMP_OPT_VALID_TOKENS_ONLY, not token-major blocks).
+ * head_dim is 64, 128 or 256; block_size a multiple of 16. */
+int64_t remp_kvq_token_bytes(int32_t head_dim); /* or REMP_ERR_SHAPE */
+
+typedef enum { REMP_DTYPE_BFLOAT = 1, REMP_DTYPE_HALF = 2 } remp_dtype; /* bfloat16, IEEE half: 16 bits each */
+
+/* One layer of a rank's 4-bit pool. shard: strides as in remp_shard, 0 = dense (stride_token must be dense). */
+typedef struct {
+    remp_shard shard;
+    int32_t layer; /* index of the layer inside the shard */
+    int32_t kv_heads, head_dim, block_size;
+} remp_kvq_pool;
+
+/* The tokens a call is about: the LAST query_start[s+1] - query_start[s] positions of every sequence s. All pointers
+ * are DEVICE pointers, read when the enqueued work runs. tables.seq_lens counts the cached tokens, the new ones among
+ * them. Token t of sequence s (query_start[s] <= t < query_start[s+1]) is row t of the tensors of the call and stands at
+ * position seq_lens[s] - query_start[s+1] + t. */
+typedef struct {
+    remp_block_tables tables;
+    const int32_t* query_start; /* device, [num_seqs + 1], ascending from 0                                    */
+    int32_t num_tokens;         /* rows of the call's tensors = query_start[num_seqs]                          */
+    int32_t max_queries;        /* no sequence has more rows than this (chooses the kernel; more are not read) */
+    uint32_t* error;            /* device word or NULL: bits of what the device found are OR-ed into it, with the
+                                   meaning of remp_remap_tables_noalloc's status word: bit 1 bad length (negative
+                                   position, position beyond the table row or the rotation table), bit 3 block id outside the pool */
+} remp_kvq_batch;
+
+/* Rows [num_tokens][heads][head_dim] of 16-bit values on the device; strides in elements, multiples of 8, base 16-byte
+ * aligned, dims dense: the slices of a fused projection need no copy. */
+typedef struct {
+    void* data;
+    int64_t stride_token, stride_head;
+} remp_kvq_rows;
+
+/* What happens to queries and keys before they are used: per-head root-mean-square norm (x / sqrt(mean x^2 + eps) * w),
+ * then rotation of pairs of the first rotary_dim dims, (a, b) -> (a cos - b sin, b cos + a sin). */
+typedef struct {
+    const float* q_norm;  /* DEVICE [head_dim] or NULL: no norm                                                    */
+    const float* k_norm;
+    const float* rope;    /* DEVICE [rope_rows][rotary_dim]: rotary_dim/2 cosines, then as many sines; NULL: no rotation */
+    const int32_t* positions; /* DEVICE [num_tokens]: rows of `rope`, or NULL: the token's position in its sequence */
+    float eps;
+    int32_t rope_rows, rotary_dim; /* a multiple of 16, at most head_dim                                           */
+    int32_t interleaved;           /* 0: pair (i, i + rotary_dim/2), 1: pair (2i, 2i + 1)                          */
+} remp_kvq_transform;
+
+/* Write new tokens: norm and rotation of q and k, quantisation of k and v into their pages, one pass and one launch.
+ *   q, q_out  rows of q_heads heads; q_out may alias q; both NULL (q_heads 0): keys and values only
+ *   transform NULL: neither norm nor rotation
+ * A token whose position or block is invalid is not written (its bit is set in batch->error); a bad block id loses K and
+ * V only. Two tokens of a call must not share a slot (sequences that share their last block: fork it first). */
+remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
+                            const remp_kvq_rows* k, const remp_kvq_rows* v, const remp_kvq_rows* q_out, int32_t q_heads,
+                            int32_t dtype, const remp_kvq_transform* transform, void* stream);
+
+/* Read the batch's tokens back as values s*c + m in `dtype`, finite ones beyond its largest value as that (either output
+ * may be NULL). Invalid tokens are not written. */
+remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* k_out,
+                          const remp_kvq_rows* v_out, int32_t dtype, void* stream);
+
+/* Attention over the cache: out = softmax(scale * q.K^T).V for every row of the batch, over the positions up to the
+ * row's own (causal) and, with window > 0, over the last `window` of these only. q_heads is a multiple of
+ * pool->kv_heads; query head h reads KV head h / (q_heads / kv_heads). A row that sees nothing (a negative position)
+ * gives 0, and -infinity as its lse. Slots behind a sequence's length may hold anything. Positions in a block whose id
+ * is outside the pool count as not there (error bit 3); lengths beyond the table row are cut to it (bit 1).
+ *   scale      positive
+ *   lse        DEVICE float [num_tokens][q_heads] or NULL: natural logarithm of the sum of exp(scale * q.k)
+ *   workspace  DEVICE, remp_kvq_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call
+ *              leaves it ready for the next. Calls that may overlap need workspaces of their own.
+ * The result does not depend on the order in which thread blocks run. */
+int64_t remp_kvq_workspace_bytes(void);
+remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
+                            const remp_kvq_rows* out, int32_t q_heads, int32_t dtype, float scale, int32_t window,
+                            float* lse, void* workspace, void* stream);
+
+/* ---- pages between two switches: fork, free, compact, copy ----
+ *
+ * refs: DEVICE int32 [num_blocks], how many live table entries (entries below ceil(seq_lens/block_size)) name a block; 0 =
+ * free. Tables and reference counts are the same on every rank; remp_pages_copy then moves the pages of each rank. All
+ * arrays are DEVICE arrays; where an output may alias an input, that is said. result: DEVICE 2 x int32, written: a
+ * count, and a status word with the bits of remp_remap_tables_noalloc (bit 0 no free block, bit 1 bad length or
+ * sequence index, bit 3 block id outside the pool or reference count below zero). The calls only enqueue. pairs: rows (source block, destination
+ * block), `result[0]` of them, -1 behind them.
+ *
+ * remp_pages_fork: sequence children[i] becomes a copy of parents[i]: its row names the parent's blocks, except that a
+ * last block that is not full is replaced by a free block (it will be written by both), listed in `pairs`; children are
+ * served in order, the lowest free id first, so the ids are deterministic. refs_out (may alias refs) counts the new
+ * entries. Rows and lengths of the children are written in place and their old contents ignored; no child may be a
+ * parent or be named twice. With too few free blocks (bit 0) or a bad sequence index or length (bit 1) nothing but
+ * result, pairs (-1) and the copy of refs is written; block ids outside the pool are passed on, not counted (bit 3).
+ *   num_forks  children; pairs has that many rows
+ * remp_pages_free: sequences with finished[s] != 0 give their blocks back: refs_out, seq_lens_out (0) and block_tables_out (-1
+ * in their whole row) - each may alias its input, everything else is copied. result[0] = blocks that became free.
+ * remp_pages_compact: the N blocks in use move to ids below N: blocks above, in ascending order, to the free ids below,
+ * in ascending order. block_tables_out and refs_out may alias their inputs; result[0] = pages to copy; pairs has
+ * max_pairs >= num_blocks/2 rows. */
+remp_status remp_pages_fork(int32_t* seq_lens, int32_t* block_tables, int32_t num_seqs, int32_t max_blocks_per_seq,
+                            int32_t block_size, const int32_t* parents, const int32_t* children, int32_t num_forks,
+                            const int32_t* refs, int32_t* refs_out, int32_t num_blocks, int32_t* pairs,
+                            int32_t* result, void* stream);
+remp_status remp_pages_free(const int32_t* seq_lens, const int32_t* block_tables, int32_t num_seqs,
+                            int32_t max_blocks_per_seq, int32_t block_size, const int32_t* finished,
+                            const int32_t* refs, int32_t num_blocks, int32_t* seq_lens_out, int32_t* block_tables_out,
+                            int32_t* refs_out, int32_t* result, void* stream);
+remp_status remp_pages_compact(const int32_t* seq_lens, const int32_t* block_tables, int32_t num_seqs,
+                               int32_t max_blocks_per_seq, int32_t block_size, const int32_t* refs, int32_t num_blocks,
+                               int32_t* block_tables_out, int32_t* refs_out, int32_t* pairs, int32_t max_pairs,
+                               int32_t* result, void* stream);
+
+/* Copy pages inside every rank's pool: block pairs[i][0] to block pairs[i][1] for i < count[0] (a DEVICE word, such as
+ * result[0] above; at most max_pairs), all layers, K and V, all heads, one launch for all ranks. No destination may be a
+ * source or appear twice (fork and compact give such lists); pairs with an id outside a rank's pool are skipped in it.
+ *   shards  HOST [topo.tp*topo.pp], rank order */
+remp_status remp_pages_copy(const remp_topo* topo, const remp_model_shape* shape, const remp_shard* shards,
+                            const int32_t* pairs, const int32_t* count, int32_t max_pairs, void* stream);
+
 /* ---- introspection (tests, benchmarks) ---- */
 
 /* Number of Algorithm-1 items, and the items themselves as rows of 5 int32:

@@ -12,7 +12,8 @@ EXPORTS = (
     "remp_shard_bytes", "remp_plan_create", "remp_alloc_dst_blocks", "remp_migrate_kv", "remp_plan_status",
     "remp_plan_destroy", "remp_last_error", "remp_plan_num_items", "remp_plan_get_items", "remp_plan_traffic",
     "remp_plan_set_option", "remp_kernel_launch_count", "remp_remap_tables_noalloc", "remp_reshard_host", "remp_migrate_kv_layers", "remp_alloc_dst_blocks_preempt", "remp_alloc_dst_blocks_shared", "remp_plan_traffic_tokens", "remp_release_cached_memory", "remp_rank_ownership", "remp_plan_partition", "remp_migrate_kv_exchange", "remp_weight_shard_bytes", "remp_weight_slice",
-    "remp_weights_reshard",
+    "remp_weights_reshard", "remp_kvq_token_bytes", "remp_kvq_append", "remp_kvq_read", "remp_kvq_attend",
+    "remp_kvq_workspace_bytes", "remp_pages_fork", "remp_pages_free", "remp_pages_compact", "remp_pages_copy",
 )
 
 
@@ -43,6 +44,25 @@ class RempWeightParam(C.Structure):
 
 class RempHostShard(C.Structure):
     _fields_ = [("base", C.c_void_p), ("num_blocks", C.c_int64)]
+
+
+class RempKvqPool(C.Structure):
+    _fields_ = [("shard", RempShard), ("layer", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("block_size", C.c_int32)]
+
+
+class RempKvqBatch(C.Structure):
+    _fields_ = [("tables", RempBlockTables), ("query_start", C.c_void_p), ("num_tokens", C.c_int32),
+                ("max_queries", C.c_int32), ("error", C.c_void_p)]
+
+
+class RempKvqRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_token", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class RempKvqTransform(C.Structure):
+    _fields_ = [("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("rope", C.c_void_p), ("positions", C.c_void_p),
+                ("eps", C.c_float), ("rope_rows", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
 _lib = None
@@ -117,5 +137,26 @@ def load():
                                     C.c_void_p, P(RempHostShard), P(RempHostShard), C.c_int32, C.c_int32, C.c_void_p,
                                     P(C.c_int64), P(C.c_int64), P(C.c_int64)]
     L.remp_reshard_host.restype = C.c_int
+    V = C.c_void_p
+    L.remp_kvq_token_bytes.argtypes = [C.c_int32]
+    L.remp_kvq_token_bytes.restype = C.c_int64
+    L.remp_kvq_append.argtypes = [P(RempKvqPool), P(RempKvqBatch)] + [P(RempKvqRows)] * 4 + [
+        C.c_int32, C.c_int32, P(RempKvqTransform), V]
+    L.remp_kvq_append.restype = C.c_int
+    L.remp_kvq_read.argtypes = [P(RempKvqPool), P(RempKvqBatch), P(RempKvqRows), P(RempKvqRows), C.c_int32, V]
+    L.remp_kvq_read.restype = C.c_int
+    L.remp_kvq_attend.argtypes = [P(RempKvqPool), P(RempKvqBatch), P(RempKvqRows), P(RempKvqRows), C.c_int32, C.c_int32,
+                                  C.c_float, C.c_int32, V, V, V]
+    L.remp_kvq_attend.restype = C.c_int
+    L.remp_kvq_workspace_bytes.argtypes = []
+    L.remp_kvq_workspace_bytes.restype = C.c_int64
+    L.remp_pages_fork.argtypes = [V, V, C.c_int32, C.c_int32, C.c_int32, V, V, C.c_int32, V, V, C.c_int32, V, V, V]
+    L.remp_pages_fork.restype = C.c_int
+    L.remp_pages_free.argtypes = [V, V, C.c_int32, C.c_int32, C.c_int32, V, V, C.c_int32, V, V, V, V, V]
+    L.remp_pages_free.restype = C.c_int
+    L.remp_pages_compact.argtypes = [V, V, C.c_int32, C.c_int32, C.c_int32, V, C.c_int32, V, V, V, C.c_int32, V, V]
+    L.remp_pages_compact.restype = C.c_int
+    L.remp_pages_copy.argtypes = [P(RempTopo), P(RempModelShape), P(RempShard), V, V, C.c_int32, V]
+    L.remp_pages_copy.restype = C.c_int
     _lib = L
     return L

@@ -12,7 +12,8 @@ from typing import List, Optional, Sequence
 import numpy as np
 
 from . import _lib
-from ._lib import RempBlockTables, RempHostShard, RempModelShape, RempShard, RempTopo, RempWeightParam
+from ._lib import (RempBlockTables, RempHostShard, RempKvqBatch, RempKvqPool, RempKvqRows, RempKvqTransform,
+                   RempModelShape, RempShard, RempTopo, RempWeightParam)
 
 REMP_OK = 0
 REMP_ERR_INVALID_ARG = -1
@@ -330,6 +331,211 @@ def remp_weights_reshard(topo, num_layers: int, params, dst_shards, stream=None,
     _check(_lib.load().remp_weights_reshard(C.byref(t), num_layers, params, len(params), ptrs, C.byref(moved),
                                             max_ctas, _stream_ptr(stream)))
     return int(moved.value)
+
+
+# ---- serving from a cache held in 4 bits ----
+
+REMP_DTYPE_BFLOAT, REMP_DTYPE_HALF = 1, 2
+
+
+def remp_kvq_token_bytes(head_dim: int) -> int:
+    n = _lib.load().remp_kvq_token_bytes(head_dim)
+    if n < 0:
+        raise RempError(int(n), remp_last_error())
+    return int(n)
+
+
+def make_kvq_pool(buffer, num_blocks: int, kv_heads: int, head_dim: int, block_size: int, layer: int = 0,
+                  strides: Optional[dict] = None) -> RempKvqPool:
+    """remp_kvq_pool of one layer of a rank's pool (a CUDA tensor; strides in bytes as for make_shards)."""
+    pool = RempKvqPool(make_shards([buffer], [num_blocks], [strides] if strides else None)[0], layer, kv_heads, head_dim,
+                       block_size)
+    pool.keep = buffer
+    return pool
+
+
+def _int32_cuda(t, name: str) -> int:
+    import torch
+    if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+        raise RempError(REMP_ERR_INVALID_ARG, f"{name} must be a contiguous int32 CUDA tensor")
+    return t.data_ptr()
+
+
+def make_kvq_batch(seq_lens, block_tables, query_start, num_tokens: int, max_queries: int, error=None) -> RempKvqBatch:
+    """remp_kvq_batch of CUDA int32 tensors: seq_lens [n], block_tables [n][max_blocks], query_start [n + 1]; error: one
+    word or None. The tensors are read when the enqueued work runs; the batch keeps them alive."""
+    n = int(seq_lens.shape[0])
+    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n or int(query_start.shape[0]) != n + 1:
+        raise RempError(REMP_ERR_INVALID_ARG, "block_tables must be [n][max_blocks] and query_start [n + 1]")
+    tables = RempBlockTables(n, int(block_tables.shape[1]), _int32_cuda(seq_lens, "seq_lens"),
+                             _int32_cuda(block_tables, "block_tables"))
+    batch = RempKvqBatch(tables, _int32_cuda(query_start, "query_start"), num_tokens, max_queries,
+                         _int32_cuda(error, "error") if error is not None else None)
+    batch.keep = (seq_lens, block_tables, query_start, error)
+    return batch
+
+
+def make_kvq_workspace(device=None):
+    """The zeroed workspace that remp_kvq_attend wants (a CUDA uint8 tensor); one for each stream."""
+    import torch
+    return torch.zeros(int(_lib.load().remp_kvq_workspace_bytes()), dtype=torch.uint8, device=device or "cuda")
+
+
+@functools.lru_cache(maxsize=None)
+def _dtypes():
+    import torch
+    return {torch.bfloat16: REMP_DTYPE_BFLOAT, torch.float16: REMP_DTYPE_HALF}
+
+
+def _rows(t, name: str, num_tokens: int, heads: int, head_dim: int, dtype):
+    """remp_kvq_rows of a CUDA tensor [num_tokens][heads][head_dim]."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (num_tokens, heads, head_dim):
+        raise RempError(REMP_ERR_SHAPE, f"{name} must be a CUDA tensor [{num_tokens}][{heads}][{head_dim}] of {dtype}")
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise RempError(REMP_ERR_SHAPE, f"{name}: the dims of a head must be dense")
+    return RempKvqRows(t.data_ptr(), st, sh)
+
+
+def _f32_cuda(t, name: str, *shape) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or (shape and tuple(t.shape) != shape):
+        raise RempError(REMP_ERR_SHAPE, f"{name} must be a contiguous float32 CUDA tensor{list(shape) if shape else ''}")
+    return t.data_ptr()
+
+
+def remp_kvq_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6,
+                    rope=None, interleaved: bool = False, positions=None, stream=None) -> None:
+    """Norm and rotation of q and k, 4-bit quantisation of k and v into their pages. q, k, v, q_out: [num_tokens][heads]
+    [head_dim] CUDA tensors of one 16-bit type, any token and head strides (q and q_out may be None, or the same
+    tensor); q_norm, k_norm: float32 [head_dim]; rope: float32 [rows][rotary_dim], cosines then sines; positions: int32
+    [num_tokens] rows of rope (default: the token's position). Only enqueues."""
+    n, d = batch.num_tokens, pool.head_dim
+    dtype = k.dtype
+    if dtype not in _dtypes():
+        raise RempError(REMP_ERR_INVALID_ARG, "k must be bfloat16 or float16")
+    heads = int(q.shape[1]) if q is not None else 0
+    tr = None
+    if q_norm is not None or k_norm is not None or rope is not None:
+        rows, dim = (int(rope.shape[0]), int(rope.shape[1])) if rope is not None else (0, 0)
+        if positions is not None and int(positions.shape[0]) != n:
+            raise RempError(REMP_ERR_SHAPE, "positions must be [num_tokens]")
+        tr = RempKvqTransform(_f32_cuda(q_norm, "q_norm", d), _f32_cuda(k_norm, "k_norm", d), _f32_cuda(rope, "rope"),
+                              _int32_cuda(positions, "positions") if positions is not None else None, eps, rows, dim,
+                              int(interleaved))
+    _check(_lib.load().remp_kvq_append(
+        pool, batch, _rows(q, "q", n, heads, d, dtype) if q is not None else None, _rows(k, "k", n, pool.kv_heads, d, dtype),
+        _rows(v, "v", n, pool.kv_heads, d, dtype),
+        _rows(q_out, "q_out", n, heads, d, dtype) if q_out is not None else None, heads, _dtypes()[dtype], tr,
+        _stream_ptr(stream)))
+
+
+def remp_kvq_read(pool: RempKvqPool, batch: RempKvqBatch, k_out, v_out, stream=None) -> None:
+    """The values that the batch's tokens have in the cache: [num_tokens][kv_heads][head_dim] CUDA tensors (either may
+    be None). Only enqueues."""
+    n, d, h = batch.num_tokens, pool.head_dim, pool.kv_heads
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        return
+    if some.dtype not in _dtypes():
+        raise RempError(REMP_ERR_INVALID_ARG, "outputs must be bfloat16 or float16")
+    _check(_lib.load().remp_kvq_read(pool, batch, _rows(k_out, "k_out", n, h, d, some.dtype) if k_out is not None else None,
+                                     _rows(v_out, "v_out", n, h, d, some.dtype) if v_out is not None else None,
+                                     _dtypes()[some.dtype], _stream_ptr(stream)))
+
+
+def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float, workspace, window: int = 0, lse=None,
+                    stream=None) -> None:
+    """Causal attention of q [num_tokens][heads][head_dim] over the cached positions of each sequence, into out (same
+    shape); window > 0: over the last `window` positions only. lse: float32 [num_tokens][heads] or None. workspace:
+    make_kvq_workspace(). Only enqueues."""
+    n, d = batch.num_tokens, pool.head_dim
+    if q.dtype not in _dtypes():
+        raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
+    heads = int(q.shape[1])
+    if not workspace.is_cuda or workspace.numel() * workspace.element_size() < _workspace_bytes():
+        raise RempError(REMP_ERR_INVALID_ARG, "the workspace is too small")
+    _check(_lib.load().remp_kvq_attend(pool, batch, _rows(q, "q", n, heads, d, q.dtype), _rows(out, "out", n, heads, d, q.dtype),
+                                       heads, _dtypes()[q.dtype], scale, window, _f32_cuda(lse, "lse", n, heads),
+                                       workspace.data_ptr(), _stream_ptr(stream)))
+
+
+@functools.lru_cache(maxsize=None)
+def _workspace_bytes() -> int:
+    return int(_lib.load().remp_kvq_workspace_bytes())
+
+
+# ---- pages between two switches ----
+
+def _tables_of(seq_lens, block_tables):
+    n = int(seq_lens.shape[0])
+    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n:
+        raise RempError(REMP_ERR_INVALID_ARG, "block_tables must be [n][max_blocks]")
+    return _int32_cuda(seq_lens, "seq_lens"), _int32_cuda(block_tables, "block_tables"), n, int(block_tables.shape[1])
+
+
+def _same(t, like, name: str) -> int:
+    if t.shape != like.shape:
+        raise RempError(REMP_ERR_INVALID_ARG, f"{name} must have shape {list(like.shape)}")
+    return _int32_cuda(t, name)
+
+
+def _pairs_of(pairs, result, least: int):
+    if pairs.dim() != 2 or int(pairs.shape[1]) != 2 or int(pairs.shape[0]) < least or result.numel() != 2:
+        raise RempError(REMP_ERR_INVALID_ARG, f"pairs must be [{least} or more][2] and result [2]")
+    return _int32_cuda(pairs, "pairs"), _int32_cuda(result, "result")
+
+
+def remp_pages_fork(seq_lens, block_tables, block_size: int, parents, children, refs, refs_out, pairs, result,
+                    stream=None) -> None:
+    """Rows and lengths of `children` (int32 [m], rows of the tables) become copies of `parents`, sharing all blocks but
+    a last one that is not full; pairs [m][2] lists the blocks to copy, result [2] their number and the status bits. All CUDA
+    int32 tensors. Only enqueues."""
+    lens, tabs, n, width = _tables_of(seq_lens, block_tables)
+    m = int(children.shape[0])
+    pp, rp = _pairs_of(pairs, result, m)
+    if int(pairs.shape[0]) != m:
+        raise RempError(REMP_ERR_INVALID_ARG, "pairs must have one row for each child")
+    _check(_lib.load().remp_pages_fork(lens, tabs, n, width, block_size, _same(parents, children, "parents"),
+                                       _int32_cuda(children, "children"), m, _int32_cuda(refs, "refs"),
+                                       _same(refs_out, refs, "refs_out"), int(refs.numel()), pp, rp, _stream_ptr(stream)))
+
+
+def remp_pages_free(seq_lens, block_tables, block_size: int, finished, refs, seq_lens_out, block_tables_out, refs_out,
+                    result, stream=None) -> None:
+    """Sequences with finished[s] != 0 give their blocks back. Outputs may be their inputs. result [2]: blocks that
+    became free, status bits. Only enqueues."""
+    lens, tabs, n, width = _tables_of(seq_lens, block_tables)
+    if result.numel() != 2:
+        raise RempError(REMP_ERR_INVALID_ARG, "result must be [2]")
+    _check(_lib.load().remp_pages_free(lens, tabs, n, width, block_size, _same(finished, seq_lens, "finished"),
+                                       _int32_cuda(refs, "refs"), int(refs.numel()), _same(seq_lens_out, seq_lens, "seq_lens_out"),
+                                       _same(block_tables_out, block_tables, "block_tables_out"), _same(refs_out, refs, "refs_out"),
+                                       _int32_cuda(result, "result"), _stream_ptr(stream)))
+
+
+def remp_pages_compact(seq_lens, block_tables, block_size: int, refs, block_tables_out, refs_out, pairs, result,
+                       stream=None) -> None:
+    """The N blocks in use move to ids below N. pairs [num_blocks // 2 or more][2]: pages to copy (remp_pages_copy);
+    result [2]: their number, status bits. Outputs may be their inputs. Only enqueues."""
+    lens, tabs, n, width = _tables_of(seq_lens, block_tables)
+    blocks = int(refs.numel())
+    pp, rp = _pairs_of(pairs, result, blocks // 2)
+    _check(_lib.load().remp_pages_compact(lens, tabs, n, width, block_size, _int32_cuda(refs, "refs"), blocks,
+                                          _same(block_tables_out, block_tables, "block_tables_out"), _same(refs_out, refs, "refs_out"), pp,
+                                          int(pairs.shape[0]), rp, _stream_ptr(stream)))
+
+
+def remp_pages_copy(topo, shape, shards, pairs, count, stream=None) -> None:
+    """Copy blocks pairs[i][0] -> pairs[i][1], i < count[0], in the pools of all ranks (make_shards). count: a CUDA
+    int32 tensor, such as the result of remp_pages_fork or remp_pages_compact. Only enqueues."""
+    t, _keep = _topo(topo)
+    if pairs.dim() != 2 or int(pairs.shape[1]) != 2 or count.numel() < 1 or len(shards) != topo.tp * topo.pp:
+        raise RempError(REMP_ERR_INVALID_ARG, "pairs must be [m][2], count [1 or more], shards one for each rank")
+    _check(_lib.load().remp_pages_copy(C.byref(t), C.byref(_shape(shape)), shards, _int32_cuda(pairs, "pairs"),
+                                       _int32_cuda(count, "count"), int(pairs.shape[0]), _stream_ptr(stream)))
 
 
 def _host_ptr(buf) -> int:

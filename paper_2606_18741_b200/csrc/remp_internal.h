@@ -188,6 +188,8 @@ struct ShardView {  // a shard with its strides resolved
 remp_status ensure_scratch(remp_plan_s* P, int64_t need_pairs, cudaStream_t stream);
 void release_scratch(remp_plan_s* P);
 remp_status status_from_word(uint32_t w);
+// A shard's strides resolved and checked; nl: layers that the caller's buffer holds.
+remp_status resolve_shard(const remp_shard& sh, const TopoMap& T, int64_t nl, const remp_model_shape& m, ShardView* v);
 // Build the addressing tables of the layers [layer_lo, layer_hi) and launch the migration kernel.
 // dst_here (optional, one flag per destination rank): only the flagged ranks are written (the others live on
 // other GPUs); planes none of whose replicas is flagged are left out of the launch altogether.

@@ -1,0 +1,430 @@
+// Writing a 4-bit cache and reading it back (format and rules: include/remp.h).
+//
+// Mathematics, per row x of one head of one token: xn = x / sqrt(mean(x^2) + eps) * w, then pairs (a, b) of dims turn to
+// (a cos - b sin, b cos + a sin); queries leave in 16 bits, keys and values as codes c = rint((x - m)/s) with a minimum
+// m and a step s for each 64 dims. All sums, norms and turns are in 32 bits; products and sums are rounded one by one
+// and the squares are added neighbours first, so that any program that follows the formula in that order gets the same
+// codes (a contracted multiply-add would move values on the edge between two codes).
+//
+// Bound: HBM (each row is read and written once). A row is held by head_dim/8 lanes, 8 dims (16 bytes) each: the norm is
+// a butterfly over these lanes, a turn's partner dim is in the same lane (interleaved) or one shuffle away, and a group
+// of 64 dims is 8 lanes. A warp takes kRowSets sets of rows of ONE token and issues all their loads before it looks up
+// where the token belongs (two or three dependent loads), so the look-up hides behind them.
+
+#include "remp_kvq.h"
+
+namespace remp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+struct Transform {
+    const float* q_norm;
+    const float* k_norm;
+    const float* rope;
+    const int32_t* positions;
+    float eps;
+    int32_t rope_rows, rotary_dim, interleaved;
+};
+
+struct Slot {  // where a token's codes are
+    int64_t off;   // bytes from the pool's base to its tile (of head 0, K)
+    int32_t pos;   // position in its sequence
+    bool known;    // the token has a position
+    bool stored;   // and a block
+};
+
+// The slot of row `token`; a whole warp asks for the same token.
+__device__ __forceinline__ Slot find_slot(const KvqView& v, int token, int tile_bytes) {
+    Slot r{0, -1, false, false};
+    const int s = kvq_sequence_of(v, token);
+    if (s < 0) return r;
+    const int end = v.query_start[s + 1];
+    if (token >= end) return r;
+    const int64_t pos = (int64_t)v.seq_lens[s] - end + token;
+    const int64_t tile = pos >> 4;
+    if (pos < 0 || tile >= (int64_t)v.max_blocks * v.block_tiles) return r;
+    r.pos = (int)pos, r.known = true;
+    const int in_row = (int)(tile / v.block_tiles);
+    const int block = v.tables[(int64_t)s * v.max_blocks + in_row];
+    r.stored = block >= 0 && block < v.nb;
+    r.off = (int64_t)block * v.s_block + (int64_t)((int)tile - in_row * v.block_tiles) * tile_bytes;
+    return r;
+}
+
+__device__ __forceinline__ void unpack8(const uint4& raw, bool bf, float (&x)[8]) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (bf) {
+            x[2 * i] = bf_low(w[i]), x[2 * i + 1] = bf_high(w[i]);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+    }
+}
+
+__device__ __forceinline__ uint4 pack8(const float (&x)[8], bool bf) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (bf) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// One step of a transpose between lanes and nibbles: lane bit `s` changes places with nibble-index bit `s`.
+__device__ __forceinline__ uint32_t nibble_step(uint32_t w, int s, uint32_t low, int lane) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, w, s);
+    return (lane & s) ? (w & ~low) | ((other & ~low) >> (4 * s)) : (w & low) | ((other & low) << (4 * s));
+}
+
+// Codes of 8 neighbouring dims, nibble t + 4e = dim 2t + e (K) or nibble j = dim j (V), to the word that this lane
+// stores, and back: both are their own inverse. K: among the four lanes of 32 dims; V: a third step, among the eight of 64.
+__device__ __forceinline__ uint32_t k_transpose(uint32_t w, int lane) {
+    return nibble_step(nibble_step(w, 1, 0x0f0f0f0fu, lane), 2, 0x00ff00ffu, lane);
+}
+__device__ __forceinline__ int k_place(int j) { return (j >> 1) + 4 * (j & 1); }
+
+// Byte of lane l's word inside a token's codes.
+template <int D>
+__device__ __forceinline__ int word_at(int l, bool is_v) {
+    return is_v ? (l & 7) * (D / 16) + (l >> 3) * 4 : (l & 3) * (D / 8) + (l >> 2) * 4;
+}
+
+template <int D, int kRowSets>
+__global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, const KvqRows q, const KvqRows k,
+                                                              const KvqRows val, const KvqRows q_out,
+                                                              const Transform tr, const int q_heads, const int bf_,
+                                                              const int sets_per_token) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
+    constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
+    const bool bf = bf_ != 0;
+    const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
+    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int token = (int)(item / sets_per_token);
+    if (token >= v.num_tokens) return;
+    const int row0 = (int)(item - (int64_t)token * sets_per_token) * (kRows * kRowSets) + sub;
+    const int rows = q_heads + 2 * v.kv_heads;
+
+    uint4 raw[kRowSets];
+#pragma unroll
+    for (int u = 0; u < kRowSets; ++u) {
+        const int row = row0 + u * kRows;
+        raw[u] = make_uint4(0, 0, 0, 0);
+        if (row < rows) {
+            const uint16_t* p = row < q_heads ? q.data + token * q.s_token + row * q.s_head
+                                : row < q_heads + v.kv_heads
+                                    ? k.data + token * k.s_token + (row - q_heads) * k.s_head
+                                    : val.data + token * val.s_token + (row - q_heads - v.kv_heads) * val.s_head;
+            raw[u] = *reinterpret_cast<const uint4*>(p + 8 * l);
+        }
+    }
+
+    const Slot slot = find_slot(v, token, kTileBytes);
+    bool known = slot.known;
+    int turn_row = slot.pos;
+    if (tr.rope && known) {
+        if (tr.positions) turn_row = tr.positions[token];
+        known = turn_row >= 0 && turn_row < tr.rope_rows;
+    }
+    if (!known || !slot.stored) {
+        if (lane == 0) kvq_error(v, known ? kErrBadBlock : kErrBadLength);
+        if (!known) return;
+    }
+
+    // cosines and sines of this lane's dims, the same for every head of the token
+    const int half = tr.rotary_dim / 2;
+    const bool turns = tr.rope && 8 * l < tr.rotary_dim;
+    float cs[8], sn[8];
+    int partner = lane;
+    float sign = 1.f;
+    if (turns) {
+        const float* row = tr.rope + (int64_t)turn_row * tr.rotary_dim;
+        if (tr.interleaved) {
+            const float4 c = *reinterpret_cast<const float4*>(row + 4 * l);
+            const float4 s = *reinterpret_cast<const float4*>(row + half + 4 * l);
+            cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
+        } else {
+            const bool upper = 8 * l >= half;
+            const float* c = row + 8 * l - (upper ? half : 0);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const float4 a = *reinterpret_cast<const float4*>(c + i), b = *reinterpret_cast<const float4*>(c + half + i);
+                cs[i] = a.x, cs[i + 1] = a.y, cs[i + 2] = a.z, cs[i + 3] = a.w;
+                sn[i] = b.x, sn[i + 1] = b.y, sn[i + 2] = b.z, sn[i + 3] = b.w;
+            }
+            partner = lane + (upper ? -half / 8 : half / 8);
+            sign = upper ? 1.f : -1.f;
+        }
+    }
+
+#pragma unroll
+    for (int u = 0; u < kRowSets; ++u) {
+        const int row = row0 + u * kRows;
+        const bool is_q = row < q_heads, is_v = row >= q_heads + v.kv_heads, real = row < rows;
+        float x[8];
+        unpack8(raw[u], bf, x);
+
+        const float* weight = is_q ? tr.q_norm : is_v ? nullptr : tr.k_norm;
+        if (__any_sync(0xffffffffu, weight != nullptr)) {
+            float q2[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q2[i] = __fmul_rn(x[i], x[i]);
+            float sum = __fadd_rn(__fadd_rn(__fadd_rn(q2[0], q2[1]), __fadd_rn(q2[2], q2[3])),
+                                  __fadd_rn(__fadd_rn(q2[4], q2[5]), __fadd_rn(q2[6], q2[7])));
+#pragma unroll
+            for (int s = 1; s < kLanes; s <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, s));
+            if (weight) {
+                const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.f / D), tr.eps)));
+                const float4 a = *reinterpret_cast<const float4*>(weight + 8 * l);
+                const float4 b = *reinterpret_cast<const float4*>(weight + 8 * l + 4);
+                const float wt[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], r), wt[i]);
+            }
+        }
+
+        if (tr.rope) {
+            if (tr.interleaved) {
+                if (turns && !is_v) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float a = x[2 * i], b = x[2 * i + 1];
+                        x[2 * i] = __fsub_rn(__fmul_rn(a, cs[i]), __fmul_rn(b, sn[i]));
+                        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cs[i]), __fmul_rn(a, sn[i]));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float other = __shfl_sync(0xffffffffu, x[i], partner);
+                    if (turns && !is_v) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i]), __fmul_rn(sign, __fmul_rn(other, sn[i])));
+                }
+            }
+        }
+
+        if (is_q)
+            *reinterpret_cast<uint4*>(q_out.data + token * q_out.s_token + row * q_out.s_head + 8 * l) = pack8(x, bf);
+        if (!__any_sync(0xffffffffu, real && !is_q)) continue;
+
+        float lo = x[0], hi = x[0];
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
+            odd |= !(fabsf(x[i]) <= 3.402823466e38f);  // NaN or infinity
+        }
+#pragma unroll
+        for (int s = 1; s < 8; s <<= 1) {
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+        }
+        odd = __ballot_sync(0xffffffffu, odd) & (0xffu << (lane & 24));
+        uint32_t m_bits = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
+        const float m = bf_low(m_bits);
+        const float span = fmaxf(__fmul_rn(__fsub_rn(hi, m), 1.f / 15.f), 0.f);
+        uint32_t s_bits = __bfloat16_as_ushort(__float2bfloat16_ru(fminf(span, 65280.f)));
+        if (odd) m_bits = 0x7fc0u, s_bits = 0;
+        const float step = bf_low(s_bits);
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = step > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], m), step)), 0.f), 15.f) : 0.f;
+            word |= (uint32_t)c << (4 * (is_v ? i : k_place(i)));
+        }
+        const uint32_t of_k = k_transpose(word, lane), of_v = nibble_step(of_k, 4, 0x0000ffffu, lane);
+        if (!is_q && real && slot.stored) {
+            const int head = is_v ? row - q_heads - v.kv_heads : row - q_heads;
+            uint8_t* tile = v.base + slot.off + head * v.s_head + (is_v ? v.s_kv : 0);
+            const int in_tile = slot.pos & 15;
+            *reinterpret_cast<uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, is_v)) = is_v ? of_v : of_k;
+            if ((l & 7) == 0)
+                *reinterpret_cast<uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4) = s_bits | m_bits << 16;
+        }
+    }
+}
+
+template <int D, int kRowSets>
+__global__ void __launch_bounds__(kThreads) kvq_read_kernel(const KvqView v, const KvqRows k, const KvqRows val,
+                                                            const int bf, const int sets_per_token) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+    constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
+    const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
+    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int token = (int)(item / sets_per_token);
+    if (token >= v.num_tokens) return;
+    const int row0 = (int)(item - (int64_t)token * sets_per_token) * (kRows * kRowSets) + sub;
+    const Slot slot = find_slot(v, token, kTileBytes);
+    if (!slot.stored) {
+        if (lane == 0) kvq_error(v, slot.known ? kErrBadBlock : kErrBadLength);
+        return;
+    }
+    const int in_tile = slot.pos & 15;
+    uint32_t word[kRowSets], par[kRowSets];
+#pragma unroll
+    for (int u = 0; u < kRowSets; ++u) {
+        const int row = row0 + u * kRows;
+        word[u] = par[u] = 0;
+        if (row < 2 * v.kv_heads) {
+            const bool is_v = row >= v.kv_heads;
+            const uint8_t* tile = v.base + slot.off + (is_v ? row - v.kv_heads : row) * v.s_head + (is_v ? v.s_kv : 0);
+            word[u] = *reinterpret_cast<const uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, is_v));
+            par[u] = *reinterpret_cast<const uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kRowSets; ++u) {
+        const int row = row0 + u * kRows;
+        const bool is_v = row >= v.kv_heads;
+        const uint32_t of_k = k_transpose(word[u], lane), of_v = nibble_step(of_k, 4, 0x0000ffffu, lane);
+        const uint32_t w = is_v ? of_v : of_k;
+        const float s = bf_low(par[u]), m = bf_high(par[u]);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = __fadd_rn(__fmul_rn((float)((w >> (4 * (is_v ? i : k_place(i)))) & 15), s), m);
+            if (!bf && fabsf(x[i]) > 65504.f) x[i] = copysignf(65504.f, x[i]);  // the span's ends were rounded outwards
+        }
+        const KvqRows& out = is_v ? val : k;
+        if (row < 2 * v.kv_heads && out.data)
+            *reinterpret_cast<uint4*>(out.data + token * out.s_token + (is_v ? row - v.kv_heads : row) * out.s_head + 8 * l) =
+                pack8(x, bf);
+    }
+}
+
+constexpr int kAppendSets = 4, kReadSets = 4;
+
+}  // namespace
+
+remp_status kvq_view(const remp_kvq_pool* pool, const remp_kvq_batch* batch, KvqView* v) {
+    if (!pool || !batch) return fail(REMP_ERR_INVALID_ARG, "null pool or batch");
+    const int64_t tb = remp_kvq_token_bytes(pool->head_dim);
+    if (tb < 0) return (remp_status)tb;
+    if (pool->block_size < kKvqTile || pool->block_size % kKvqTile)
+        return fail(REMP_ERR_SHAPE, "block_size must be a multiple of 16");
+    if (pool->kv_heads < 1) return fail(REMP_ERR_SHAPE, "kv_heads must be positive");
+    if (pool->layer < 0) return fail(REMP_ERR_INVALID_ARG, "negative layer");
+    if (pool->shard.stride_token && pool->shard.stride_token != tb)
+        return fail(REMP_ERR_SHAPE, "token rows of a 4-bit cache are dense");
+    const remp_model_shape m = {1, pool->kv_heads, (int32_t)tb, pool->block_size, 1};
+    TopoMap T;
+    T.heads_per_rank = pool->kv_heads;
+    ShardView s;
+    if (remp_status st = resolve_shard(pool->shard, T, 1, m, &s)) return st;
+    if (s.s_head < pool->block_size * tb) return fail(REMP_ERR_SHAPE, "stride_head must hold a head slice");
+    if (s.nb > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "block ids are 32-bit");
+    const remp_block_tables& bt = batch->tables;
+    if (bt.num_seqs < 0 || bt.max_blocks_per_seq < 0 || batch->num_tokens < 0 || batch->max_queries < 0)
+        return fail(REMP_ERR_INVALID_ARG, "negative batch dimensions");
+    if (batch->num_tokens > 0 && (!bt.seq_lens || !batch->query_start || (bt.max_blocks_per_seq > 0 && !bt.block_tables)))
+        return fail(REMP_ERR_INVALID_ARG, "null seq_lens, block_tables or query_start");
+    v->base = reinterpret_cast<uint8_t*>(s.base + (uint64_t)((int64_t)pool->layer * s.s_layer));
+    v->s_kv = s.s_kv, v->s_block = s.s_block, v->s_head = s.s_head;
+    v->nb = (int32_t)s.nb, v->kv_heads = pool->kv_heads, v->block_tiles = pool->block_size / kKvqTile;
+    v->max_blocks = bt.max_blocks_per_seq, v->num_seqs = bt.num_seqs, v->num_tokens = bt.num_seqs ? batch->num_tokens : 0;
+    v->seq_lens = bt.seq_lens, v->tables = bt.block_tables, v->query_start = batch->query_start;
+    v->error = batch->error;
+    return REMP_OK;
+}
+
+remp_status kvq_rows(const remp_kvq_rows* r, int32_t heads, int32_t head_dim, const char* name, KvqRows* out) {
+    if (!r || !r->data) return fail(REMP_ERR_INVALID_ARG, std::string("null ") + name);
+    if ((reinterpret_cast<uint64_t>(r->data) & 15) || (r->stride_token & 7) || (r->stride_head & 7))
+        return fail(REMP_ERR_SHAPE, std::string(name) + ": base must be 16-byte aligned and strides multiples of 8 elements");
+    if (heads > 1 && r->stride_head < head_dim && r->stride_head > -head_dim)
+        return fail(REMP_ERR_SHAPE, std::string(name) + ": heads overlap");
+    out->data = static_cast<uint16_t*>(r->data);
+    out->s_token = r->stride_token, out->s_head = r->stride_head;
+    return REMP_OK;
+}
+
+static remp_status check_dtype(int32_t dtype) {
+    return dtype == REMP_DTYPE_BFLOAT || dtype == REMP_DTYPE_HALF ? REMP_OK : fail(REMP_ERR_INVALID_ARG, "unknown dtype");
+}
+
+}  // namespace remp
+
+using namespace remp;
+
+extern "C" int64_t remp_kvq_token_bytes(int32_t head_dim) {
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256)
+        return fail(REMP_ERR_SHAPE, "head_dim of a 4-bit cache must be 64, 128 or 256");
+    return kvq_token_bytes(head_dim);
+}
+
+extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
+                                       const remp_kvq_rows* k, const remp_kvq_rows* v, const remp_kvq_rows* q_out,
+                                       int32_t q_heads, int32_t dtype, const remp_kvq_transform* transform,
+                                       void* stream_) {
+    KvqView view;
+    KvqRows rq{nullptr, 0, 0}, rk, rv, ro{nullptr, 0, 0};
+    if (remp_status st = kvq_view(pool, batch, &view)) return st;
+    if (remp_status st = check_dtype(dtype)) return st;
+    const int32_t d = pool->head_dim;
+    if (q_heads < 0 || (q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr))
+        return fail(REMP_ERR_INVALID_ARG, "q, q_out and q_heads go together");
+    Transform tr{nullptr, nullptr, nullptr, nullptr, 0.f, 0, 0, 0};
+    if (transform) {
+        tr = Transform{transform->q_norm, transform->k_norm, transform->rope, transform->positions, transform->eps,
+                       transform->rope_rows, transform->rotary_dim, transform->interleaved};
+        if ((reinterpret_cast<uint64_t>(tr.q_norm) | reinterpret_cast<uint64_t>(tr.k_norm) | reinterpret_cast<uint64_t>(tr.rope)) & 15)
+            return fail(REMP_ERR_SHAPE, "norm weights and the rotation table must be 16-byte aligned");
+        if (!(tr.eps >= 0.f)) return fail(REMP_ERR_INVALID_ARG, "eps must not be negative");
+        if (tr.rope && (tr.rotary_dim < 16 || tr.rotary_dim % 16 || tr.rotary_dim > d || tr.rope_rows < 0))
+            return fail(REMP_ERR_SHAPE, "rotary_dim must be a multiple of 16 and at most head_dim");
+        if (!tr.rope) tr.rotary_dim = 0;
+    }
+    if (view.num_tokens == 0) return REMP_OK;
+    if (q_heads) {
+        if (remp_status st = kvq_rows(q, q_heads, d, "q", &rq)) return st;
+        if (remp_status st = kvq_rows(q_out, q_heads, d, "q_out", &ro)) return st;
+    }
+    if (remp_status st = kvq_rows(k, pool->kv_heads, d, "k", &rk)) return st;
+    if (remp_status st = kvq_rows(v, pool->kv_heads, d, "v", &rv)) return st;
+    const int64_t rows = (int64_t)q_heads + 2 * (int64_t)pool->kv_heads;
+    const int per_item = 32 / (d / 8) * kAppendSets;
+    const int64_t sets = (rows + per_item - 1) / per_item, grid = (view.num_tokens * sets + kWarps - 1) / kWarps;
+    if (grid > 0x7fffffffLL || rows > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
+    const auto kernel = d == 64 ? kvq_append_kernel<64, kAppendSets>
+                        : d == 128 ? kvq_append_kernel<128, kAppendSets> : kvq_append_kernel<256, kAppendSets>;
+    kernel<<<(unsigned)grid, kThreads, 0, static_cast<cudaStream_t>(stream_)>>>(
+        view, rq, rk, rv, ro, tr, q_heads, dtype == REMP_DTYPE_BFLOAT, (int)sets);
+    count_launch();
+    REMP_CUDA(cudaGetLastError());
+    return REMP_OK;
+}
+
+extern "C" remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* k_out,
+                                     const remp_kvq_rows* v_out, int32_t dtype, void* stream_) {
+    KvqView view;
+    KvqRows rk{nullptr, 0, 0}, rv{nullptr, 0, 0};
+    if (remp_status st = kvq_view(pool, batch, &view)) return st;
+    if (remp_status st = check_dtype(dtype)) return st;
+    const int32_t d = pool->head_dim;
+    if (view.num_tokens == 0 || (!k_out && !v_out)) return REMP_OK;
+    if (k_out)
+        if (remp_status st = kvq_rows(k_out, pool->kv_heads, d, "k_out", &rk)) return st;
+    if (v_out)
+        if (remp_status st = kvq_rows(v_out, pool->kv_heads, d, "v_out", &rv)) return st;
+    const int per_item = 32 / (d / 8) * kReadSets;
+    const int64_t sets = (2 * (int64_t)pool->kv_heads + per_item - 1) / per_item;
+    const int64_t grid = (view.num_tokens * sets + kWarps - 1) / kWarps;
+    if (grid > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
+    const auto kernel = d == 64 ? kvq_read_kernel<64, kReadSets>
+                        : d == 128 ? kvq_read_kernel<128, kReadSets> : kvq_read_kernel<256, kReadSets>;
+    kernel<<<(unsigned)grid, kThreads, 0, static_cast<cudaStream_t>(stream_)>>>(view, rk, rv, dtype == REMP_DTYPE_BFLOAT,
+                                                                             (int)sets);
+    count_launch();
+    REMP_CUDA(cudaGetLastError());
+    return REMP_OK;
+}

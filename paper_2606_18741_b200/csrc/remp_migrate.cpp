@@ -225,7 +225,7 @@ extern "C" remp_status remp_plan_status(remp_plan* plan, void* stream_) {
     return status_from_word((uint32_t)plan->h_result[1]);
 }
 
-namespace {
+namespace remp {
 
 // nl: layers of this rank that the caller's buffer holds (its whole stage, or the part inside a layer window).
 remp_status resolve_shard(const remp_shard& sh, const TopoMap& T, int64_t nl, const remp_model_shape& m, ShardView* v) {
@@ -253,6 +253,10 @@ remp_status resolve_shard(const remp_shard& sh, const TopoMap& T, int64_t nl, co
     if (nl <= 0) v->extent = 0;
     return REMP_OK;
 }
+
+}  // namespace remp
+
+namespace {
 
 bool overlaps(const ShardView& a, const ShardView& b) {
     return a.extent && b.extent && a.base < b.base + b.extent && b.base < a.base + a.extent;
