@@ -1,22 +1,22 @@
 // Attention over the 4-bit cache for few queries per sequence (decode, drafts, short continuations).
 //
 // Mathematics. With a key's codes c, step s and minimum m for each group of 64 dims, q.k = sum over groups of
-// s*(q.c) + m*sum(q); with a value's, sum p*v = sum (p*s)*c + sum p*m. So the matrix instructions work on bare codes: a
-// code in the low bits of a half is the subnormal c*2^-24, exact, and taking codes out of a word is an AND (and a shift for
-// half of them); codes left at bits 4..7 count 16-fold, which the query's other half of the dims (K) or the output
-// row (V) undoes. The factor 2^-24 leaves with the scale. Softmax with a running reference: the sums are kept
-// relative to a reference that is raised by kSlack beyond a new maximum only when some score passes it (one vote per
-// tile), so p <= 1 always and accumulators are seldom rescaled.
-// Rounding: q is exact in half after a power of two per row; p*s is rounded to half (2^-11, before a sum of many); scores,
-// references, sums of p, sums of p*m and outputs are in 32 bits.
+// s*(q.c) + m*sum(q); with a value's, sum p*v = sum (p*s)*(c - 8) + sum p*(m + 8s). So the matrix instructions work on
+// bare codes: a key's code in the low bits of a half is the subnormal c*2^-24, exact, and taking codes out of a word is an
+// AND (and a shift for half of them); codes left at bits 4..7 count 16-fold, which the query's other half of the dims (K) or
+// the output row (V) undoes. The factor 2^-24 leaves with the scale. A value's codes take one subtraction more.
+// Softmax with a running reference: p = 2^(x - ref), and p times the largest step seen stays at or below 2^15. A
+// reference moves only when a score (or a step) passes that bound, by kSlack further than needed, which one vote for each
+// 32 tokens finds out; accumulators are seldom rescaled, and p*s keeps 11 bits over 29 powers of two.
+// Rounding: q is exact in half after a power of two per row; p*s is rounded to half (kvq_values); scores, references, sums of p, sums of p*m and outputs are in 32 bits.
 //
 // Roles: a tile is 16 tokens of one head. S^T[16 tokens][8 rows] = K.Q^T and O^T[D][8 rows] += V^T.P^T, so the eight query
 // heads of a KV head fill the 8 columns of m16n8k16; P^T goes from accumulator to operand layout with one
 // matrix transpose for each 8 tokens. NT = 2 takes 16 rows and is used when 8 do not hold a sequence's rows.
 //
-// Bound: HBM. Work is the list of all (sequence, row block, KV head, tile), cut evenly over the thread blocks and within
-// one evenly over its warps, so ragged batches and single long sequences fill the GPU alike. A warp streams its
-// tiles through a ring of kStages in shared memory with 16-byte asynchronous copies and needs no block-wide
+// Bound: HBM. Work is the list of all (sequence, row block, KV head, step of two tiles), cut evenly over the thread blocks
+// and within one evenly over its warps, so ragged batches and single long sequences fill the GPU alike. A warp streams
+// its steps through two buffers in shared memory with 16-byte asynchronous copies and needs no block-wide
 // barrier until its share is done. Parts of a sequence are merged in the block, and across blocks by the block that
 // arrives last (a counter; nobody waits), always in the order of the list: the result does not depend on timing.
 
@@ -28,7 +28,9 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
-constexpr float kSlack = 4.f;     // log2: a new reference is 16 times the maximum
+constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
+constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
+constexpr int kStepTiles = 2, kStepTokens = kStepTiles * kKvqTile;
 
 struct AttendArgs {
     KvqView v;
@@ -38,12 +40,12 @@ struct AttendArgs {
     float scale_log2;  // softmax scale * log2(e)
     int32_t group, q_heads, window, bf;
     int32_t spt;       // sequences of one thread of the block-wide scan
-    int32_t min_tiles; // tiles that a thread block takes at least
 };
 
 struct Seq {  // one sequence's share of the list
     int len, q0, rows;      // cached tokens, first row of the batch, query rows (queries * group)
-    int tile0, tiles;       // tiles that its rows see; at least one, so that rows which see nothing are written too
+    int tile0, tiles;       // tiles that its rows see
+    int steps;              // of kStepTiles; at least one, so that rows which see nothing are written too
     int first_pos;          // position of its first query
     int blocks;             // row blocks
 };
@@ -60,26 +62,29 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     r.first_pos = len - n;
     const int from = a.window > 0 ? max(0, r.first_pos - a.window + 1) : 0;
     r.tile0 = min(from, r.len) / kKvqTile;
-    r.tiles = max(1, (r.len + kKvqTile - 1) / kKvqTile - r.tile0);
+    r.tiles = (r.len + kKvqTile - 1) / kKvqTile - r.tile0;
+    r.steps = max(1, (r.tiles + kStepTiles - 1) / kStepTiles);
     return r;
 }
 
 template <int RB>
-__device__ __forceinline__ long long tiles_of(const AttendArgs& a, int s) {
+__device__ __forceinline__ long long steps_of(const AttendArgs& a, int s) {
     const Seq q = seq_of<RB>(a, s);
-    return (long long)q.blocks * a.v.kv_heads * q.tiles;
+    return (long long)q.blocks * a.v.kv_heads * q.steps;
 }
 
 struct Cursor {  // a place in the list
     Seq q;
-    int s, unit, tile;  // sequence, (KV head, row block) in it, tile in that
+    int s, head, block, step;  // sequence, KV head, row block, step
 };
 
 template <int RB>
 __device__ __forceinline__ void next_unit(const AttendArgs& a, Cursor& c) {
-    c.tile = 0;
-    if (++c.unit < c.q.blocks * a.v.kv_heads) return;
-    c.unit = 0;
+    c.step = 0;
+    if (++c.block < c.q.blocks) return;
+    c.block = 0;
+    if (++c.head < a.v.kv_heads) return;
+    c.head = 0;
     do {
         if (++c.s >= a.v.num_seqs) return;
         c.q = seq_of<RB>(a, c.s);
@@ -87,7 +92,7 @@ __device__ __forceinline__ void next_unit(const AttendArgs& a, Cursor& c) {
 }
 
 struct Part {  // what a warp leaves of a unit that it did not see whole
-    long long from, to;  // the unit's tiles in the list
+    long long from, to;  // the unit's steps in the list
     int q0, row0, rows, head;
     int live;
 };
@@ -96,11 +101,11 @@ template <int D, int NT>
 struct Sizes {
     static constexpr int kRows = 8 * NT;
     static constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
-    static constexpr int kStage = 2 * kTileBytes;
+    static constexpr int kStage = 2 * kTileBytes;                    // K and V of a tile
+    static constexpr int kBuffer = kStepTiles * kStage;
     static constexpr int kPitch = D + 4;                             // floats of a part's row: spreads the banks
     static constexpr int kPart = kRows * (kPitch + 2) * 4;           // rows, references, sums
-    static constexpr int kStages = D == 256 ? 3 : 4;
-    static constexpr int kRing = kStages * kStage > kPart ? kStages * kStage : kPart;  // the tail part reuses the ring
+    static constexpr int kRing = 2 * kBuffer > kPart ? 2 * kBuffer : kPart;  // the tail part reuses the buffers
     static constexpr int kWarpBytes = (kRing + kPart + 127) / 128 * 128;
     static constexpr int kBytes = kWarps * kWarpBytes;
     static constexpr int kSlotFloats = kRows * (D + 2);  // a part in the workspace
@@ -158,7 +163,7 @@ __device__ __forceinline__ void merge(const AttendArgs& a, const Part& p, int n,
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_attend_kernel(const AttendArgs a) {
     using Z = Sizes<D, NT>;
-    constexpr int RB = Z::kRows, G = D / kKvqGroup, kStages = Z::kStages;
+    constexpr int RB = Z::kRows, G = D / kKvqGroup;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long scan[kThreads + 1];
     __shared__ long long warp_sum[kWarps];
@@ -168,12 +173,12 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
     const KvqView& v = a.v;
 
-    // ---- the list: tiles before each thread's sequences ----
+    // ---- the list: steps before each thread's sequences ----
     {
         long long mine = 0;
         const int s0 = min(v.num_seqs, tid * a.spt), s1 = min(v.num_seqs, s0 + a.spt);
         for (int s = s0; s < s1; ++s) {
-            mine += tiles_of<RB>(a, s);
+            mine += steps_of<RB>(a, s);
             if (blockIdx.x == 0) {
                 const int len = v.seq_lens[s];
                 if (len < 0 || len > (int64_t)v.max_blocks * v.block_tiles * kKvqTile) kvq_error(v, kErrBadLength);
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
         __syncthreads();
     }
     const long long total = scan[kThreads];
-    const long long per = max((long long)a.min_tiles, (total + gridDim.x - 1) / gridDim.x);
+    const long long per = max((long long)kWarps, (total + gridDim.x - 1) / gridDim.x);
     const long long cta0 = blockIdx.x * per, cta1 = min(total, cta0 + per);
     if (cta0 >= total) return;
     const long long wper = (cta1 - cta0 + kWarps - 1) / kWarps;
@@ -208,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
     if (w0 < w1) {
         // ---- the warp's first place ----
         Cursor c;  // of the loads, ahead of the work
-        long long unit0;  // list index of tile 0 of the unit at work
+        long long unit0;  // list index of step 0 of the unit at work
         {
             int lo = 0, hi = kThreads - 1;  // last thread whose sequences begin at or before w0
             while (lo < hi) {
@@ -219,63 +224,67 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
             c.s = lo * a.spt;
             for (;; ++c.s) {
                 c.q = seq_of<RB>(a, c.s);
-                const long long n = (long long)c.q.blocks * v.kv_heads * c.q.tiles;
+                const long long n = (long long)c.q.blocks * v.kv_heads * c.q.steps;
                 if (at + n > w0) break;
                 at += n;
             }
             const long long in = w0 - at;
-            c.unit = (int)(in / c.q.tiles), c.tile = (int)(in % c.q.tiles);
-            unit0 = w0 - c.tile;
+            const int unit = (int)(in / c.q.steps);
+            c.step = (int)(in % c.q.steps), c.head = unit / c.q.blocks, c.block = unit - c.head * c.q.blocks;
+            unit0 = w0 - c.step;
         }
         Cursor w = c;
 
-        // ---- loads: a ring of tiles, ids of 32 blocks at a time in the lanes ----
+        // ---- loads: ids of 32 blocks at a time in the lanes, blocks walked without a division ----
         int ids = -1, ids_seq = -1, ids_first = 0;
-        uint32_t absent = 0;  // stages whose tile is not there
-        auto issue = [&](int stage) {
-            const int tile = c.q.tile0 + c.tile;
-            const int in_row = tile / v.block_tiles;
-            bool there = tile * kKvqTile < c.q.len;
-            if (there) {
-                if (c.s != ids_seq || in_row < ids_first || in_row >= ids_first + 32) {
-                    ids_seq = c.s, ids_first = in_row;
-                    ids = in_row + lane < v.max_blocks ? v.tables[(int64_t)c.s * v.max_blocks + in_row + lane] : -1;
-                }
-                const int id = __shfl_sync(0xffffffffu, ids, in_row - ids_first);
-                there = id >= 0 && id < v.nb;
-                if (there) {
-                    const int head = c.unit / c.q.blocks;
-                    const uint8_t* src = v.base + (int64_t)id * v.s_block + (int64_t)head * v.s_head +
-                                         (tile - in_row * v.block_tiles) * Z::kTileBytes;
-                    kvq_fetch_tile<D>(src, v.s_kv, ring_at + stage * Z::kStage, lane);
-                } else if (lane == 0) {
-                    kvq_error(v, kErrBadBlock);
-                }
-            }
-            absent = there ? absent & ~(1u << stage) : absent | (1u << stage);
-            if (++c.tile == c.q.tiles) next_unit<RB>(a, c);
+        int in_row = 0, in_block = 0;  // place of the next tile in its row of the table
+        uint32_t absent = 0;           // tiles of either buffer that are not there
+        const auto enter = [&]() {
+            const int tile = c.q.tile0 + c.step * kStepTiles;
+            in_row = tile / v.block_tiles, in_block = tile - in_row * v.block_tiles;
         };
-        long long ahead = w0;
-        int load_stage = 0;
+        enter();
+        const auto issue = [&](int buffer) {
+            const uint8_t* base = v.base + (int64_t)c.head * v.s_head;
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
-            if (ahead < w1) issue(load_stage), ++ahead;
-            load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
-            cp_async_commit();
-        }
+            for (int j = 0; j < kStepTiles; ++j) {
+                bool there = c.step * kStepTiles + j < c.q.tiles;
+                if (there) {
+                    if (c.s != ids_seq || in_row < ids_first || in_row >= ids_first + 32) {
+                        ids_seq = c.s, ids_first = in_row;
+                        ids = in_row + lane < v.max_blocks ? v.tables[(int64_t)c.s * v.max_blocks + in_row + lane] : -1;
+                    }
+                    const int id = __shfl_sync(0xffffffffu, ids, in_row - ids_first);
+                    there = (uint32_t)id < (uint32_t)v.nb;
+                    if (there)
+                        kvq_fetch_tile<D>(base + (int64_t)id * v.s_block + in_block * Z::kTileBytes, v.s_kv,
+                                          ring_at + buffer * Z::kBuffer + j * Z::kStage, lane);
+                    else if (lane == 0)
+                        kvq_error(v, kErrBadBlock);
+                    if (++in_block == v.block_tiles) in_block = 0, ++in_row;
+                }
+                const uint32_t bit = 1u << (buffer * kStepTiles + j);
+                absent = there ? absent & ~bit : absent | bit;
+            }
+            if (++c.step == c.q.steps) {
+                next_unit<RB>(a, c);
+                enter();
+            }
+        };
+        long long ahead = w0 + 1;
+        issue(0);
+        cp_async_commit();
 
         // ---- work ----
-        int stage = 0;
+        int buffer = 0;
         for (long long x = w0; x < w1;) {
-            const int head = w.unit / w.q.blocks, row0 = (w.unit - head * w.q.blocks) * RB;
+            const int head = w.head, row0 = w.block * RB;
             const int rows = min(RB, w.q.rows - row0);
-            const long long unit1 = unit0 + w.q.tiles, stop = min(unit1, w1);
+            const long long unit1 = unit0 + w.q.steps, stop = min(unit1, w1);
 
             // queries of this lane's column g (+8): halves of the operand, their sums, and the exponent that was taken out
             uint32_t qf[NT][D / 16][2];
             float qsum[NT][G][2], back[NT][2];
-            int limit[NT][2];
-            int low_limit = 0x7fffffff, high_limit = -1;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int r = row0 + min(8 * n + g, rows - 1);
@@ -283,16 +292,9 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
                 const uint16_t* src = a.q.data + (int64_t)(w.q.q0 + r / a.group) * a.q.s_token +
                                       (int64_t)(head * a.group + r % a.group) * a.q.s_head + 2 * t;
                 kvq_load_queries<D>(src, a.bf != 0, real, t, qf[n], qsum[n], back[n], a.scale_log2);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int col = 8 * n + 2 * t + e;
-                    limit[n][e] = col < rows ? w.q.first_pos + (row0 + col) / a.group : -1;
-                }
-                if (8 * n < rows) {
-                    low_limit = min(low_limit, w.q.first_pos + (row0 + 8 * n) / a.group);
-                    high_limit = max(high_limit, w.q.first_pos + (row0 + min(8 * n + 7, rows - 1)) / a.group);
-                }
             }
+            // the positions of the first and the last row
+            const int low_limit = w.q.first_pos + row0 / a.group, high_limit = w.q.first_pos + (row0 + rows - 1) / a.group;
             float o[NT][D / 16][4], ref[NT][2], sum[NT][2], low[NT][G][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -302,63 +304,100 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
 #pragma unroll
                 for (int i = 0; i < G; ++i) low[n][i][0] = low[n][i][1] = 0.f;
             }
+            float top_step = kTopStep, room = 25.f;  // p * top_step <= 2^15: p <= 2^room
 
             for (; x < stop; ++x) {
-                cp_async_wait<kStages - 2>();
+                cp_async_wait<0>();
                 __syncwarp();
-                const uint8_t* buf = ring + stage * Z::kStage;
-                const bool here = !(absent >> stage & 1);
-                if (ahead < w1) issue(load_stage), ++ahead;
-                load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+                const uint8_t* buf = ring + buffer * Z::kBuffer;
+                const uint32_t missing = absent >> (buffer * kStepTiles) & ((1u << kStepTiles) - 1);
+                buffer ^= 1;
+                if (ahead < w1) issue(buffer), ++ahead;
                 cp_async_commit();
-                stage = stage + 1 == kStages ? 0 : stage + 1;
-                const int key0 = (w.q.tile0 + w.tile) * kKvqTile;
-                ++w.tile;
-                if (!here) continue;
+                const int key0 = (w.q.tile0 + w.step * kStepTiles) * kKvqTile;
+                ++w.step;
 
-                float s[NT][4];
-                kvq_scores<D, NT>(buf, g, t, qf, qsum, s);
-                const bool whole = key0 + kKvqTile - 1 <= low_limit && (a.window <= 0 || key0 > high_limit - a.window);
-                if (!whole || key0 + kKvqTile > w.q.len) {
+                float s[kStepTiles][NT][4];
+                uint32_t par[kStepTiles][2][G];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int j = 0; j < kStepTiles; ++j) {
+                    kvq_scores<D, NT>(buf + j * Z::kStage, g, t, qf, qsum, s[j]);
+                    kvq_params<D>(buf + j * Z::kStage + Z::kTileBytes, g, par[j]);
+                }
+                if (missing || key0 + kStepTokens - 1 > low_limit || key0 + kStepTokens > w.q.len ||
+                    (a.window > 0 && key0 <= high_limit - a.window)) {
+                    // what a row does not see gets -infinity; the steps and minima of tokens that are not there, 0
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + g + (e >> 1) * 8, lim = limit[n][e & 1];
-                            if (key > lim || key >= w.q.len || (a.window > 0 && key <= lim - a.window)) s[n][e] = -INFINITY;
+                    for (int j = 0; j < kStepTiles; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int key = key0 + j * kKvqTile + g + 8 * h;
+                            const bool there = key < w.q.len && !(missing >> j & 1);
+#pragma unroll
+                            for (int i = 0; i < G; ++i)
+                                if (!there) par[j][h][i] = 0;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int col = min(8 * n + 2 * t + e, rows - 1);
+                                    const int limit = w.q.first_pos + (row0 + col) / a.group;
+                                    if (!there || key > limit || (a.window > 0 && key <= limit - a.window))
+                                        s[j][n][2 * h + e] = -INFINITY;
+                                }
                         }
                 }
-                bool raise = false;
+                float over = -INFINITY, step = 0.f;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int j = 0; j < kStepTiles; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) raise |= s[n][e] * back[n][e & 1] > ref[n][e & 1];
-                if (__any_sync(0xffffffffu, raise)) {
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < G; ++i) step = fmaxf(step, bf_low(par[j][h][i]));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) over = fmaxf(over, fmaf(s[j][n][2 * h + e], back[n][e], -ref[n][e]));
+                    }
+                if (__any_sync(0xffffffffu, over > room || step > top_step)) {
+                    float shift = 0.f;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, d));
+                    if (step > top_step) {  // a power of two, so that the accumulators change by one too
+                        const float now = __uint_as_float((__float_as_uint(step) & 0x7f800000u) + (5u << 23));
+                        shift = (float)((int)(__float_as_uint(now) >> 23) - (int)(__float_as_uint(top_step) >> 23));
+                        top_step = now, room -= shift;
+                    }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float top = fmaxf(s[n][e], s[n][e + 2]) * back[n][e];
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int j = 0; j < kStepTiles; ++j) top = fmaxf(top, fmaxf(s[j][n][e], s[j][n][e + 2]) * back[n][e]);
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                            if (top > ref[n][e]) {
-                                const float fall = exp2f(ref[n][e] - (top + kSlack));
-                                ref[n][e] = top + kSlack, sum[n][e] *= fall;
+                            float now = ref[n][e] + shift;
+                            if (top - now > room) now = top + kSlack - room;
+                            const float fall = exp2f(ref[n][e] - now);
+                            ref[n][e] = now, sum[n][e] *= fall;
 #pragma unroll
-                                for (int i = 0; i < G; ++i) low[n][i][e] *= fall;
+                            for (int i = 0; i < G; ++i) low[n][i][e] *= fall;
 #pragma unroll
-                                for (int i = 0; i < D / 16; ++i) o[n][i][e] *= fall, o[n][i][e + 2] *= fall;
-                            }
+                            for (int i = 0; i < D / 16; ++i) o[n][i][e] *= fall, o[n][i][e + 2] *= fall;
                         }
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int j = 0; j < kStepTiles; ++j) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[n][e] = exp2_approx(fmaf(s[n][e], back[n][e & 1], -ref[n][e & 1]));
-                        sum[n][e & 1] += s[n][e];
-                    }
-                kvq_values<D, NT>(buf + Z::kTileBytes, g, t, s, key0 + kKvqTile > w.q.len, w.q.len - key0, o, low);
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[j][n][e] = exp2_approx(fmaf(s[j][n][e], back[n][e & 1], -ref[n][e & 1]));
+                            sum[n][e & 1] += s[j][n][e];
+                        }
+                    kvq_values<D, NT>(buf + j * Z::kStage + Z::kTileBytes, g, t, s[j], par[j], o, low);
+                }
             }
 
             // ---- the unit is done, or this warp's share of it ----
@@ -374,14 +413,12 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) low[n][i][e] += __shfl_xor_sync(0xffffffffu, low[n][i][e], d);
                 }
-            // codes counted 2^-24 (2^-20 in the rows of the upper nibbles); add what the minima give
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[n][i][e] = fmaf(o[n][i][e], e < 2 ? 16777216.f : 1048576.f, low[n][i / 4][e & 1]);
+                    for (int e = 0; e < 4; ++e) o[n][i][e] = fmaf(o[n][i][e], e < 2 ? 1.f : 0.0625f, low[n][i / 4][e & 1]);
             Part p{unit0, unit1, w.q.q0, row0, rows, head, 1};
             if (begun && ended) {
 #pragma unroll
@@ -513,7 +550,6 @@ extern "C" remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq
     a.scale_log2 = scale * 1.4426950408889634f;
     a.group = q_heads / pool->kv_heads, a.q_heads = q_heads, a.window = window, a.bf = dtype == REMP_DTYPE_BFLOAT;
     a.spt = (a.v.num_seqs + kThreads - 1) / kThreads;
-    a.min_tiles = kWarps;
     if ((int64_t)batch->num_tokens * a.group > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const bool wide = (int64_t)batch->max_queries * a.group > 8;

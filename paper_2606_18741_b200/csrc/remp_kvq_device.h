@@ -52,21 +52,24 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, bool bf) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A tile of K and the tile of V behind it (stride kv) to shared memory at `dst`. The 16-byte pieces of V's codes change
-// places within 128 bytes (piece ^ (token & 6)), so that the lanes of a warp, which read four tokens' rows at once,
-// meet different banks.
+// A tile of K (at `src`) and its tile of V (`kv` bytes behind) to shared memory, 16 bytes at a time. The pieces of V's
+// codes change places within 128 bytes (piece ^ (token & 6)), so that the lanes of a warp, which read four tokens' rows
+// at once, meet different banks.
 template <int D>
 __device__ __forceinline__ void kvq_fetch_tile(const uint8_t* src, int64_t kv, uint32_t dst, int lane) {
     constexpr int kBytes = kKvqTile * kvq_token_bytes(D), kPieces = kBytes / 16, kCodes = kKvqTile * D / 32;
+    const uint8_t* k = src + lane * 16;
+    const uint8_t* v = k + kv - kBytes;  // piece p of both tiles is at v + 16 * (p - lane) once p >= kPieces
 #pragma unroll
     for (int i = 0; i < (2 * kPieces + 31) / 32; ++i) {
         const int p = lane + 32 * i;
         if (32 * i + 31 < kPieces) {
-            cp_async16(dst + p * 16, src + p * 16);
-        } else if (p < 2 * kPieces) {
+            cp_async16(dst + p * 16, k + 512 * i);
+        } else {
             const int pv = p - kPieces;
-            const int to = pv >= 0 && pv < kCodes ? pv ^ ((pv / (D / 32)) & 6) : pv;
-            cp_async16(dst + kBytes + to * 16, pv >= 0 ? src + kv + pv * 16 : src + p * 16);
+            const int to = (32 * i >= kPieces || pv >= 0) && pv < kCodes ? pv ^ ((pv / (D / 32)) & 6) : pv;
+            if (32 * i + 31 < 2 * kPieces || p < 2 * kPieces)
+                cp_async16(dst + kBytes + to * 16, (32 * i >= kPieces || pv >= 0 ? v : k) + 512 * i);
         }
     }
 }
@@ -126,36 +129,46 @@ __device__ __forceinline__ void kvq_load_queries(const uint16_t* src, bool bf, b
     for (int c = 0; c < 2; ++c) back[c] = __shfl_sync(0xffffffffu, down * 1048576.f, (2 * t + c) * 4);
 }
 
+// The steps and minima of tokens g (h = 0) and g+8 of a tile, one word for each group.
+template <int D>
+__device__ __forceinline__ void kvq_params(const uint8_t* tile, int g, uint32_t (&par)[2][D / kKvqGroup]) {
+    constexpr int G = D / kKvqGroup;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint8_t* p = tile + kKvqTile * D / 2 + (g + 8 * h) * (D / 16);
+        if constexpr (G == 1) {
+            par[h][0] = *reinterpret_cast<const uint32_t*>(p);
+        } else if constexpr (G == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            par[h][0] = x.x, par[h][1] = x.y;
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            par[h][0] = x.x, par[h][1] = x.y, par[h][2] = x.z, par[h][3] = x.w;
+        }
+    }
+}
+
 // s[n]: scores of tokens g (elements 0, 1) and g+8 (2, 3) with columns 8n + 2t, +1, before `back`.
 template <int D, int NT>
 __device__ __forceinline__ void kvq_scores(const uint8_t* tile, int g, int t, const uint32_t (&qf)[NT][D / 16][2],
                                            const float (&qsum)[NT][D / kKvqGroup][2], float (&s)[NT][4]) {
     constexpr int G = D / kKvqGroup, W = D / 32;  // groups, words of a lane's row
-    uint32_t w[2][W];
-    uint32_t par[2][G];
+    uint32_t w[2][W], par[2][G];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uint8_t* row = tile + (g + 8 * h) * (D / 2) + t * (D / 8);
-        const uint8_t* pp = tile + kKvqTile * D / 2 + (g + 8 * h) * (D / 16);
         if constexpr (W == 2) {
             const uint2 x = *reinterpret_cast<const uint2*>(row);
             w[h][0] = x.x, w[h][1] = x.y;
-            par[h][0] = *reinterpret_cast<const uint32_t*>(pp);
         } else {
 #pragma unroll
             for (int i = 0; i < W; i += 4) {
                 const uint4 x = *reinterpret_cast<const uint4*>(row + 4 * i);
                 w[h][i] = x.x, w[h][i + 1] = x.y, w[h][i + 2] = x.z, w[h][i + 3] = x.w;
             }
-#pragma unroll
-            for (int i = 0; i < G; i += 2) {
-                const uint2 x = *reinterpret_cast<const uint2*>(pp + 4 * i);
-                par[h][i] = x.x, par[h][i + 1] = x.y;
-            }
         }
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    kvq_params<D>(tile, g, par);
 #pragma unroll
     for (int grp = 0; grp < G; ++grp) {
         float acc[NT][4];
@@ -172,25 +185,38 @@ __device__ __forceinline__ void kvq_scores(const uint8_t* tile, int g, int t, co
                              qf[n][2 * i + h][0], qf[n][2 * i + h][1]);
             }
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 4; ++e) {
+            const float step = bf_low(par[e >> 1][grp]), low = bf_high(par[e >> 1][grp]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                s[n][e] += fmaf(bf_low(par[e >> 1][grp]), acc[n][e], bf_high(par[e >> 1][grp]) * qsum[n][grp][e & 1]);
+            for (int n = 0; n < NT; ++n) {
+                const float x = fmaf(low, qsum[n][grp][e & 1], grp ? s[n][e] : 0.f);
+                s[n][e] = fmaf(step, acc[n][e], x);
+            }
+        }
     }
 }
 
-// o += V^T . P^T in units of 2^-24 (rows g of each 16 dims) and 2^-20 (rows g+8); low += P . minima. p: the
-// probabilities of kvq_scores' layout, 0 where masked. cut: only the first `valid` tokens of the tile are there; the
-// parameters of the others may be anything.
+// c - 8 (codes at bits 0..3 of each half) or 16 (c - 8) (at bits 4..7), as halves: 1024 + c has the code in its last bits.
+__device__ __forceinline__ uint32_t centred(uint32_t x, bool upper) {
+    const uint32_t y = (x & (upper ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), __half2half2(__ushort_as_half(upper ? 0x6480 : 0x6408)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// o += (V's codes - 8)^T . R^T (16-fold in rows g+8 of each 16 dims), where R = p * step rounded to half; low += sums of
+// p * (minimum + 8 step); so sum p*v = o + low. Codes around 0 keep the sums of a long sequence small: the matrix
+// instructions' sums are cut, not rounded, and over 100 thousand tokens codes of one sign put the result off by 2^-18
+// of sum p*v's terms; what rounding R does is halved as well. p: the probabilities in kvq_scores' layout; par: kvq_params of the tile, 0
+// for tokens that are not there.
 template <int D, int NT>
-__device__ __forceinline__ void kvq_values(const uint8_t* tile, int g, int t, const float (&p)[NT][4], bool cut, int valid,
-                                           float (&o)[NT][D / 16][4], float (&low)[NT][D / kKvqGroup][2]) {
+__device__ __forceinline__ void kvq_values(const uint8_t* tile, int g, int t, const float (&p)[NT][4],
+                                           const uint32_t (&par)[2][D / kKvqGroup], float (&o)[NT][D / 16][4],
+                                           float (&low)[NT][D / kKvqGroup][2]) {
     constexpr int G = D / kKvqGroup;
     uint32_t w[4][G];  // tokens 2t, 2t+1, 2t+8, 2t+9: this lane's dims of each group
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int token = 2 * t + (j & 1) + (j >> 1) * 8;
-        const int at = (token * (D / 2) + g * (D / 16)) ^ ((token & 6) << 4);
+        const int at = ((2 * t + (j & 1) + (j >> 1) * 8) * (D / 2) + g * (D / 16)) ^ ((2 * t) << 4);
         if constexpr (G == 1) {
             w[j][0] = *reinterpret_cast<const uint32_t*>(tile + at);
         } else if constexpr (G == 2) {
@@ -201,36 +227,27 @@ __device__ __forceinline__ void kvq_values(const uint8_t* tile, int g, int t, co
             w[j][0] = x.x, w[j][1] = x.y, w[j][2] = x.z, w[j][3] = x.w;
         }
     }
-    uint32_t par[2][G];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint8_t* pp = tile + kKvqTile * D / 2 + (g + 8 * h) * (D / 16);
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-            par[h][i] = *reinterpret_cast<const uint32_t*>(pp + 4 * i);
-            if (cut && g + 8 * h >= valid) par[h][i] = 0;
-        }
-    }
 #pragma unroll
     for (int grp = 0; grp < G; ++grp) {
         uint32_t b[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int h = 0; h < 2; ++h) {
+            const float step = bf_low(par[h][grp]), middle = fmaf(8.f, step, bf_high(par[h][grp]));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float s = bf_low(par[h][grp]), m = bf_high(par[h][grp]);
-                b[n][h] = transpose8(pack2(p[n][2 * h] * s, p[n][2 * h + 1] * s, false));
-                low[n][grp][0] = fmaf(p[n][2 * h], m, low[n][grp][0]);
-                low[n][grp][1] = fmaf(p[n][2 * h + 1], m, low[n][grp][1]);
+            for (int n = 0; n < NT; ++n) {
+                b[n][h] = transpose8(pack2(p[n][2 * h] * step, p[n][2 * h + 1] * step, false));
+                low[n][grp][0] = fmaf(p[n][2 * h], middle, low[n][grp][0]);
+                low[n][grp][1] = fmaf(p[n][2 * h + 1], middle, low[n][grp][1]);
             }
+        }
         const uint32_t x[2] = {__byte_perm(w[0][grp], w[1][grp], 0x5410), __byte_perm(w[0][grp], w[1][grp], 0x7632)};
         const uint32_t y[2] = {__byte_perm(w[2][grp], w[3][grp], 0x5410), __byte_perm(w[2][grp], w[3][grp], 0x7632)};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // dims 64 grp + 16 i + g, + 8
             const uint32_t u = i & 1 ? x[i >> 1] >> 8 : x[i >> 1], z = i & 1 ? y[i >> 1] >> 8 : y[i >> 1];
+            const uint32_t a0 = centred(u, false), a1 = centred(u, true), a2 = centred(z, false), a3 = centred(z, true);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-                mma16816(o[n][4 * grp + i], u & 0x000f000fu, u & 0x00f000f0u, z & 0x000f000fu, z & 0x00f000f0u, b[n][0], b[n][1]);
+            for (int n = 0; n < NT; ++n) mma16816(o[n][4 * grp + i], a0, a1, a2, a3, b[n][0], b[n][1]);
         }
     }
 }
