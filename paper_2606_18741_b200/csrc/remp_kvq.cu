@@ -12,6 +12,7 @@
 // where the token belongs (two or three dependent loads), so the look-up hides behind them.
 
 #include "remp_kvq.h"
+#include "remp_launch.h"
 
 namespace remp {
 
@@ -109,6 +110,7 @@ __global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, c
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
     const bool bf = bf_ != 0;
+    grid_begin();
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
     const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     const int token = (int)(item / sets_per_token);
@@ -259,6 +261,7 @@ __global__ void __launch_bounds__(kThreads) kvq_read_kernel(const KvqView v, con
                                                             const int bf, const int sets_per_token) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
+    grid_begin();
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
     const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     const int token = (int)(item / sets_per_token);
@@ -397,10 +400,8 @@ extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq
     if (grid > 0x7fffffffLL || rows > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
     const auto kernel = d == 64 ? kvq_append_kernel<64, kAppendSets>
                         : d == 128 ? kvq_append_kernel<128, kAppendSets> : kvq_append_kernel<256, kAppendSets>;
-    kernel<<<(unsigned)grid, kThreads, 0, static_cast<cudaStream_t>(stream_)>>>(
-        view, rq, rk, rv, ro, tr, q_heads, dtype == REMP_DTYPE_BFLOAT, (int)sets);
-    count_launch();
-    REMP_CUDA(cudaGetLastError());
+    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads,
+                           (int)(dtype == REMP_DTYPE_BFLOAT), (int)sets));
     return REMP_OK;
 }
 
@@ -422,9 +423,7 @@ extern "C" remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_b
     if (grid > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
     const auto kernel = d == 64 ? kvq_read_kernel<64, kReadSets>
                         : d == 128 ? kvq_read_kernel<128, kReadSets> : kvq_read_kernel<256, kReadSets>;
-    kernel<<<(unsigned)grid, kThreads, 0, static_cast<cudaStream_t>(stream_)>>>(view, rk, rv, dtype == REMP_DTYPE_BFLOAT,
-                                                                             (int)sets);
-    count_launch();
-    REMP_CUDA(cudaGetLastError());
+    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rk, rv, (int)(dtype == REMP_DTYPE_BFLOAT),
+                           (int)sets));
     return REMP_OK;
 }

@@ -26,7 +26,6 @@ namespace remp {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
@@ -38,9 +37,12 @@ struct AttendArgs {
     float* lse;
     uint8_t* workspace;
     float scale_log2;  // softmax scale * log2(e)
-    int32_t group, q_heads, window, bf;
-    int32_t spt;       // sequences of one thread of the block-wide scan
+    int32_t group, q_heads, window;
+    uint32_t by_group; // row / group = high half of row * by_group (0: group is 1)
+    int32_t room;      // tokens that a row of the table holds
 };
+
+__device__ __forceinline__ int token_of(const AttendArgs& a, int row) { return a.by_group ? (int)__umulhi((uint32_t)row, a.by_group) : row; }
 
 struct Seq {  // one sequence's share of the list
     int len, q0, rows;      // cached tokens, first row of the batch, query rows (queries * group)
@@ -54,10 +56,8 @@ template <int RB>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     Seq r;
     const int qs = max(0, a.v.query_start[s]), qe = min(a.v.num_tokens, a.v.query_start[s + 1]);
-    const int n = max(0, qe - qs);
-    const int64_t room = (int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile;
-    const int len = a.v.seq_lens[s];
-    r.len = (int)min((int64_t)max(len, 0), room);
+    const int len = a.v.seq_lens[s], n = max(0, qe - qs);
+    r.len = min(max(len, 0), a.room);
     r.q0 = qs, r.rows = n * a.group, r.blocks = (r.rows + RB - 1) / RB;
     r.first_pos = len - n;
     const int from = a.window > 0 ? max(0, r.first_pos - a.window + 1) : 0;
@@ -67,341 +67,368 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     return r;
 }
 
-template <int RB>
-__device__ __forceinline__ long long steps_of(const AttendArgs& a, int s) {
-    const Seq q = seq_of<RB>(a, s);
-    return (long long)q.blocks * a.v.kv_heads * q.steps;
-}
-
-struct Cursor {  // a place in the list
-    Seq q;
-    int s, head, block, step;  // sequence, KV head, row block, step
-};
-
-template <int RB>
-__device__ __forceinline__ void next_unit(const AttendArgs& a, Cursor& c) {
-    c.step = 0;
-    if (++c.block < c.q.blocks) return;
-    c.block = 0;
-    if (++c.head < a.v.kv_heads) return;
-    c.head = 0;
-    do {
-        if (++c.s >= a.v.num_seqs) return;
-        c.q = seq_of<RB>(a, c.s);
-    } while (c.q.rows == 0);
-}
-
-struct Part {  // what a warp leaves of a unit that it did not see whole
-    long long from, to;  // the unit's steps in the list
+struct Unit {  // rows [row0, row0 + rows) of a sequence (first row of the batch q0) and a KV head; its steps in the list
+    int from, to;
     int q0, row0, rows, head;
     int live;
 };
 
-template <int D, int NT>
-struct Sizes {
-    static constexpr int kRows = 8 * NT;
-    static constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
-    static constexpr int kStage = 2 * kTileBytes;                    // K and V of a tile
-    static constexpr int kBuffer = kStepTiles * kStage;
-    static constexpr int kPitch = D + 4;                             // floats of a part's row: spreads the banks
-    static constexpr int kPart = kRows * (kPitch + 2) * 4;           // rows, references, sums
-    static constexpr int kRing = 2 * kBuffer > kPart ? 2 * kBuffer : kPart;  // the tail part reuses the buffers
-    static constexpr int kWarpBytes = (kRing + kPart + 127) / 128 * 128;
-    static constexpr int kBytes = kWarps * kWarpBytes;
-    static constexpr int kSlotFloats = kRows * (D + 2);  // a part in the workspace
+struct Chain {  // parts of one unit in the order of the list: the first, and from rest + stride on; merged into slot or the output
+    const float *first, *rest;
+    float* slot;
+    int64_t stride;
+    const Unit* unit;
+    int n;
 };
 
-// out[row][4 dims] = x
-__device__ __forceinline__ void store4(const AttendArgs& a, const Part& p, int r, int d, const float4& x) {
-    const int row = p.row0 + r, token = p.q0 + row / a.group, head = p.head * a.group + row % a.group;
-    uint2 w;
-    if (a.bf) {
-        const __nv_bfloat162 u = __floats2bfloat162_rn(x.x, x.y), v = __floats2bfloat162_rn(x.z, x.w);
-        w = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
-    } else {
-        const __half2 u = __floats2half2_rn(x.x, x.y), v = __floats2half2_rn(x.z, x.w);
-        w = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
-    }
-    *reinterpret_cast<uint2*>(a.out.data + token * a.out.s_token + head * a.out.s_head + d) = w;
-}
-
-__device__ __forceinline__ void store_lse(const AttendArgs& a, const Part& p, int r, float ref, float sum) {
-    const int row = p.row0 + r;
-    a.lse[(int64_t)(p.q0 + row / a.group) * a.q_heads + p.head * a.group + row % a.group] =
-        sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-}
-
-// Merge `n` parts (n >= 1; part i's rows at rows(i), references at refs(i), sums behind them) into the output or, with
-// `slot`, into a part of the workspace. The whole thread block works on it.
-template <int D, int NT, class Rows>
-__device__ __forceinline__ void merge(const AttendArgs& a, const Part& p, int n, int pitch, const Rows& part, float* slot) {
-    constexpr int R = 8 * NT;
-    for (int e = threadIdx.x; e < p.rows * (D / 4); e += kThreads) {
-        const int r = e / (D / 4), d = e % (D / 4) * 4;
-        float ref = kNoRef;
-        for (int i = 0; i < n; ++i) ref = fmaxf(ref, part(i)[R * pitch + r]);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-        for (int i = 0; i < n; ++i) {
-            const float* x = part(i);
-            const float w = exp2f(x[R * pitch + r] - ref);
-            const float4 o = *reinterpret_cast<const float4*>(x + r * pitch + d);
-            acc.x += w * o.x, acc.y += w * o.y, acc.z += w * o.z, acc.w += w * o.w;
-            sum += w * x[R * pitch + R + r];
-        }
-        if (slot) {
-            *reinterpret_cast<float4*>(slot + r * D + d) = acc;
-            if (d == 0) slot[R * D + r] = ref, slot[R * D + R + r] = sum;
-        } else {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            store4(a, p, r, d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-            if (d == 0 && a.lse) store_lse(a, p, r, ref, sum);
-        }
-    }
-}
-
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_attend_kernel(const AttendArgs a) {
+struct Sizes {
+    // One block to an SM: twelve warps of 168 registers hold everything where eight rows of up to 128 dims are at work (70B decode
+    // step 46 us, 131071 tokens 53 us; two blocks of eight warps, which spill: 52 and 65; three of four: 48 and 75), eight
+    // of 255 elsewhere.
+    static constexpr int kWarps = D == 256 || NT == 2 ? 8 : 12, kThreads = kWarps * 32;
+    static constexpr int kRows = 8 * NT, kQuads = NT * D / 16;
+    static constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
+    static constexpr int kBuffer = KvqStep<D>::kBytes;
+    // a part: accumulators as the lanes hold them (quad by quad), then references and sums of the rows
+    static constexpr int kPartFloats = kQuads * 128 + 2 * kRows, kPart = kPartFloats * 4;
+    static constexpr int kRing = 2 * kBuffer > kPart ? 2 * kBuffer : kPart;  // a tail part reuses the buffers
+    static constexpr int kWarpBytes = (kRing + kPart + 127) / 128 * 128;
+    static constexpr int kBytes = kWarps * kWarpBytes;
+};
+
+// One quad of results: dims 16i + g, 16i + 8 + g of columns 8n + 2t, +1 -> the output, 4 bytes to a lane.
+template <bool BF>
+__device__ __forceinline__ void put_quad(const float4& o, const float (&inv)[2], uint16_t* dst, bool real) {
+    const uint32_t x = transpose8(pack2(o.x * inv[0], o.y * inv[1], BF)), y = transpose8(pack2(o.z * inv[0], o.w * inv[1], BF));
+    if (real) *reinterpret_cast<uint32_t*>(dst) = x, *reinterpret_cast<uint32_t*>(dst + 8) = y;
+}
+
+// Where row 8n + g of a unit goes (dim 2t of it).
+__device__ __forceinline__ uint16_t* out_row(const AttendArgs& a, const Unit& u, int n, int g, int t) {
+    const int r = u.row0 + 8 * n + g, token = token_of(a, r);
+    return a.out.data + (int64_t)(u.q0 + token) * a.out.s_token + (int64_t)(u.head * a.group + r - token * a.group) * a.out.s_head + 2 * t;
+}
+
+__device__ __forceinline__ void put_lse(const AttendArgs& a, const Unit& u, int col, float ref, float sum) {
+    const int r = u.row0 + col, token = token_of(a, r);
+    if (col < u.rows)
+        a.lse[(int64_t)(u.q0 + token) * a.q_heads + u.head * a.group + r - token * a.group] =
+            sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+}
+
+// Parts are read in shared memory or, written by other blocks, in global memory: past the first-level cache.
+__device__ __forceinline__ float4 part4(const float* p) {
+    float4 x;
+    asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p));
+    return x;
+}
+__device__ __forceinline__ float2 part2(const float* p) {
+    float2 x;
+    asm volatile("ld.volatile.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "l"(p));
+    return x;
+}
+
+// Quad q of a chain.
+template <int D, int NT, bool BF>
+__device__ __forceinline__ void merge_quad(const AttendArgs& a, const Chain& c, int q, int lane) {
     using Z = Sizes<D, NT>;
-    constexpr int RB = Z::kRows, G = D / kKvqGroup;
+    const int g = lane >> 2, t = lane & 3, tile = q / (D / 16), col = 8 * tile + 2 * t;
+    float2 ref = make_float2(kNoRef, kNoRef), sum = make_float2(0.f, 0.f);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kAhead = 8;
+#pragma unroll 1
+    for (int i0 = 0; i0 < c.n; i0 += kAhead) {
+        float4 o[kAhead];
+        float2 r[kAhead], s[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const float* x = i0 + j ? c.rest + (i0 + j) * c.stride : c.first;
+            r[j] = make_float2(kNoRef, kNoRef), s[j] = make_float2(0.f, 0.f), o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i0 + j < c.n) o[j] = part4(x + q * 128 + lane * 4), r[j] = part2(x + Z::kQuads * 128 + col), s[j] = part2(x + Z::kQuads * 128 + Z::kRows + col);
+        }
+        float2 top = ref;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) top.x = fmaxf(top.x, r[j].x), top.y = fmaxf(top.y, r[j].y);
+        float fx = exp2_approx(ref.x - top.x), fy = exp2_approx(ref.y - top.y);
+        sum.x *= fx, sum.y *= fy, acc.x *= fx, acc.y *= fy, acc.z *= fx, acc.w *= fy;
+        ref = top;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (i0 + j >= c.n) break;
+            fx = exp2_approx(r[j].x - top.x), fy = exp2_approx(r[j].y - top.y);
+            sum.x = fmaf(fx, s[j].x, sum.x), sum.y = fmaf(fy, s[j].y, sum.y);
+            acc.x = fmaf(fx, o[j].x, acc.x), acc.y = fmaf(fy, o[j].y, acc.y);
+            acc.z = fmaf(fx, o[j].z, acc.z), acc.w = fmaf(fy, o[j].w, acc.w);
+        }
+    }
+    const bool keeper = q % (D / 16) == 0 && g == 0;  // of the rows' references and sums
+    if (c.slot) {
+        *reinterpret_cast<float4*>(c.slot + q * 128 + lane * 4) = acc;
+        if (keeper) {
+            *reinterpret_cast<float2*>(c.slot + Z::kQuads * 128 + col) = ref;
+            *reinterpret_cast<float2*>(c.slot + Z::kQuads * 128 + Z::kRows + col) = sum;
+        }
+    } else {
+        const Unit u = *c.unit;
+        const float inv[2] = {sum.x == 0.f ? 0.f : 1.f / sum.x, sum.y == 0.f ? 0.f : 1.f / sum.y};
+        put_quad<BF>(acc, inv, out_row(a, u, tile, g, t) + q % (D / 16) * 16, 8 * tile + g < u.rows);
+        if (keeper && a.lse) put_lse(a, u, col, ref.x, sum.x), put_lse(a, u, col + 1, ref.y, sum.y);
+    }
+}
+
+template <int D, int NT, bool BF>
+__global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(const __grid_constant__ AttendArgs a) {
+    using Z = Sizes<D, NT>;
+    using S = KvqStep<D>;
+    constexpr int RB = Z::kRows, G = D / kKvqGroup, kWarps = Z::kWarps, kThreads = Z::kThreads;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long scan[kThreads + 1];
     __shared__ long long warp_sum[kWarps];
-    __shared__ Part parts[kWarps][2];
-    __shared__ int last_of[2];
+    __shared__ int first_at[kWarps], first_seq[kWarps];  // where a warp's share begins: sequences from here, at this place in the list
+    __shared__ Unit parts[kWarps][2];  // of each warp: the unit that it found begun, the unit that it leaves unfinished
+    __shared__ Chain chains[kWarps + 1];
+    __shared__ int num_chains;
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
     const KvqView& v = a.v;
+    const int spt = (v.num_seqs + kThreads - 1) / kThreads;  // sequences of one thread in the scan
+    grid_begin();
 
-    // ---- the list: steps before each thread's sequences ----
-    {
-        long long mine = 0;
-        const int s0 = min(v.num_seqs, tid * a.spt), s1 = min(v.num_seqs, s0 + a.spt);
-        for (int s = s0; s < s1; ++s) {
-            mine += steps_of<RB>(a, s);
-            if (blockIdx.x == 0) {
-                const int len = v.seq_lens[s];
-                if (len < 0 || len > (int64_t)v.max_blocks * v.block_tiles * kKvqTile) kvq_error(v, kErrBadLength);
-            }
-        }
-        long long incl = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long up = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += up;
-        }
-        if (lane == 31) warp_sum[wid] = incl;
-        if (tid < kWarps * 2) parts[tid >> 1][tid & 1].live = 0;
-        __syncthreads();
-        long long before = 0;
-        for (int w = 0; w < wid; ++w) before += warp_sum[w];
-        scan[tid + 1] = before + incl;
-        if (tid == 0) scan[0] = 0;
-        __syncthreads();
+    // ---- the list: steps before each thread's sequences, and where this block's warps begin ----
+    const int s0 = min(v.num_seqs, tid * spt), s1 = min(v.num_seqs, s0 + spt);
+    long long mine = 0;
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+        const Seq q = seq_of<RB>(a, s);
+        mine += (long long)(q.blocks * v.kv_heads) * q.steps;
+        if (blockIdx.x == 0 && q.len != v.seq_lens[s]) kvq_error(v, kErrBadLength);  // it was cut
     }
-    const long long total = scan[kThreads];
-    const long long per = max((long long)kWarps, (total + gridDim.x - 1) / gridDim.x);
-    const long long cta0 = blockIdx.x * per, cta1 = min(total, cta0 + per);
+    long long before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, before, d);
+        if (lane >= d) before += up;
+    }
+    if (lane == 31) warp_sum[wid] = before;
+    if (tid < kWarps * 2) parts[tid >> 1][tid & 1].live = 0;
+    __syncthreads();
+    before -= mine;
+    long long total_ = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const long long x = warp_sum[w];
+        if (w < wid) before += x;
+        total_ += x;
+    }
+    if (total_ > 0x40000000) {  // 2^30 steps: more than 4 TB of cache
+        if (blockIdx.x == 0 && tid == 0) kvq_error(v, kErrOverflow);
+        return;
+    }
+    const int total = (int)total_, per = max(kWarps, (int)((uint32_t)(total + gridDim.x - 1) / gridDim.x));
+    const int cta0 = min((long long)blockIdx.x * per, 0x7fffffffLL), cta1 = min(total, cta0 + per);
     if (cta0 >= total) return;
-    const long long wper = (cta1 - cta0 + kWarps - 1) / kWarps;
-    const long long w0 = min(cta1, cta0 + wid * wper), w1 = min(cta1, w0 + wper);
+    const int wper = (cta1 - cta0 + kWarps - 1) / kWarps;
+    if (mine > 0 && before < cta1 && before + mine > cta0) {
+        // this thread's sequences hold the places [before, before + mine): the warps that begin there
+        const int from = max(0, ((int)before - cta0 + wper - 1) / wper), to = (int)before + (int)mine - cta0;
+#pragma unroll 1
+        for (int w = from; w < kWarps && w * wper < to; ++w) first_seq[w] = s0, first_at[w] = (int)before;
+    }
+    __syncthreads();
+    const int w0 = min(cta1, cta0 + wid * wper), todo = min(cta1, w0 + wper) - w0;
 
     uint8_t* ring = smem + wid * Z::kWarpBytes;
-    float* head_part = reinterpret_cast<float*>(ring + Z::kRing);
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
 
-    if (w0 < w1) {
-        // ---- the warp's first place ----
-        Cursor c;  // of the loads, ahead of the work
-        long long unit0;  // list index of step 0 of the unit at work
-        {
-            int lo = 0, hi = kThreads - 1;  // last thread whose sequences begin at or before w0
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (scan[mid] <= w0) lo = mid; else hi = mid - 1;
-            }
-            long long at = scan[lo];
-            c.s = lo * a.spt;
-            for (;; ++c.s) {
-                c.q = seq_of<RB>(a, c.s);
-                const long long n = (long long)c.q.blocks * v.kv_heads * c.q.steps;
-                if (at + n > w0) break;
-                at += n;
-            }
-            const long long in = w0 - at;
-            const int unit = (int)(in / c.q.steps);
-            c.step = (int)(in % c.q.steps), c.head = unit / c.q.blocks, c.block = unit - c.head * c.q.blocks;
-            unit0 = w0 - c.step;
-        }
-        Cursor w = c;
+    if (todo > 0) {
+        // the loads' place in the list, one step ahead of the work: sequence, KV head, row block, step of it
+        Seq q{};
+        int seq = first_seq[wid], seq_at = first_at[wid], head = 0, block = 0, step_at = 0;
+        int ids = -1, in_ids = 32;    // ids of 32 blocks of the row of the table, one to a lane; the next tile's place among them
+        int in_block = 0;             // its place in its block
+        const uint8_t* heads = v.base;  // the KV head's slice of block 0
+        const int32_t* row = nullptr;   // the rest of the row of the table
+        int row_left = 0;
+        uint32_t absent = 0;                        // tiles of the step that are not there
+        uint32_t qf[NT][D / 16][2];
+        float qsum[NT][G][2], back[NT][2];
+        int limit[NT][2];  // positions of columns 2t, 2t+1
+        float o[NT][D / 16][4], ref[NT][2], sum[NT][2], low[NT][G][2];
+        float top_step = kTopStep, bound = 0x1p25f;  // p * top_step <= 2^15: p <= bound
+        bool fresh = true;                       // the next step is the first of its unit here
 
-        // ---- loads: ids of 32 blocks at a time in the lanes, blocks walked without a division ----
-        int ids = -1, ids_seq = -1, ids_first = 0;
-        int in_row = 0, in_block = 0;  // place of the next tile in its row of the table
-        uint32_t absent = 0;           // tiles of either buffer that are not there
-        const auto enter = [&]() {
-            const int tile = c.q.tile0 + c.step * kStepTiles;
-            in_row = tile / v.block_tiles, in_block = tile - in_row * v.block_tiles;
-        };
-        enter();
-        const auto issue = [&](int buffer) {
-            const uint8_t* base = v.base + (int64_t)c.head * v.s_head;
+#pragma unroll 1
+        for (int i = 0; i <= todo; ++i) {
+            cp_async_wait<0>();
+            __syncwarp();
+            // the step at work is the one that was asked for in the last round
+            const uint32_t missing = absent;
+            const Seq wq = q;
+            const int w_head = head, w_block = block, w_step = step_at;
+            if (i < todo) {
+                // ---- loads of step i, into the buffer that the step before the last has left ----
+                bool enter = i == 0;
+                if (i > 0 && ++step_at == q.steps) {
+                    step_at = 0, enter = true;
+                    if (++block == q.blocks) block = 0, ++head;
+                    if (head == v.kv_heads) head = 0, ++seq;
+                }
+                if (enter) {
+                    if (i == 0 || (step_at | block | head) == 0) {
+                        // the next sequence with rows; at first, the one that holds place w0
+#pragma unroll 1
+                        for (;; ++seq) {
+                            q = seq_of<RB>(a, seq);
+                            const int n = q.blocks * v.kv_heads * q.steps;
+                            if (i == 0 ? seq_at + n > w0 : n > 0) break;
+                            seq_at += n;
+                        }
+                    }
+                    if (i == 0) {
+                        const uint32_t in = w0 - seq_at, unit = in / (uint32_t)q.steps;
+                        step_at = (int)(in - unit * q.steps), head = (int)(unit / (uint32_t)q.blocks), block = (int)unit - head * q.blocks;
+                    }
+                    const int tile = q.tile0 + step_at * kStepTiles, in_row = tile / v.block_tiles;
+                    in_block = tile - in_row * v.block_tiles, in_ids = 32;
+                    row = v.tables + (int64_t)seq * v.max_blocks + in_row, row_left = v.max_blocks - in_row;
+                    heads = v.base + (int64_t)head * v.s_head;
+                    // the unit's queries are wanted in the next round
+                    const int r0 = block * RB, r = r0 + min(lane & (RB - 1), q.rows - r0 - 1), token = token_of(a, r);
+                    const uint16_t* query = a.q.data + (int64_t)(q.q0 + token) * a.q.s_token + (int64_t)(head * a.group + r - token * a.group) * a.q.s_head;
+                    for (int x = lane / RB * 64; x < D; x += 32 / RB * 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(query + x));
+                }
+                const int left = q.tiles - step_at * kStepTiles;
+                const auto tile_at = [&](const uint8_t*& src) {  // of the next tile; false: its block is not in the pool
+                    if (in_ids == 32) {
+                        ids = lane < row_left ? row[lane] : -1;
+                        in_ids = 0, row += 32, row_left -= 32;
+                    }
+                    const int id = __shfl_sync(0xffffffffu, ids, in_ids);
+                    src = heads + (int64_t)id * v.s_block + in_block * Z::kTileBytes;
+                    if (++in_block == v.block_tiles) in_block = 0, ++in_ids;
+                    const bool there = (uint32_t)id < (uint32_t)v.nb;
+                    if (!there && lane == 0) kvq_error(v, kErrBadBlock);
+                    return there;
+                };
+                const uint8_t *src0 = heads, *src1 = heads;
+                const bool there0 = left > 0 && tile_at(src0), there1 = left > 1 && tile_at(src1);
+                absent = (there0 ? 0u : 1u) | (there1 ? 0u : 2u);
+                kvq_fetch_step<D>(src0, src1, there0, there1, v.s_kv, ring_at + (i & 1) * Z::kBuffer, lane);
+            }
+            cp_async_commit();
+            if (i == 0) continue;
+
+            // ---- work on step i - 1 ----
+            if (fresh) {  // the unit's queries: rows g (+8) are this lane's operand columns
+                const int row0 = w_block * RB, rows = wq.rows - row0;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int r = row0 + min(8 * n + g, rows - 1), token = token_of(a, r);
+                    kvq_load_queries<D>(a.q.data + (int64_t)(wq.q0 + token) * a.q.s_token +
+                                            (int64_t)(w_head * a.group + r - token * a.group) * a.q.s_head + 2 * t,
+                                        8 * n + g < rows, qf[n]);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    kvq_make_queries<D>(BF, t, qf[n], qsum[n], back[n], a.scale_log2);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        limit[n][e] = wq.first_pos + token_of(a, row0 + min(8 * n + 2 * t + e, rows - 1));
+                        ref[n][e] = kNoRef, sum[n][e] = 0.f;
+#pragma unroll
+                        for (int j = 0; j < G; ++j) low[n][j][e] = 0.f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) o[n][j][0] = o[n][j][1] = o[n][j][2] = o[n][j][3] = 0.f;
+                }
+                top_step = kTopStep, bound = 0x1p25f, fresh = false;
+            }
+            const uint8_t* buf = ring + ((i - 1) & 1) * Z::kBuffer;
+            const int key0 = (wq.tile0 + w_step * kStepTiles) * kKvqTile;
+            float s[kStepTiles][NT][4];
+            uint32_t par[kStepTiles][2][G];
 #pragma unroll
             for (int j = 0; j < kStepTiles; ++j) {
-                bool there = c.step * kStepTiles + j < c.q.tiles;
-                if (there) {
-                    if (c.s != ids_seq || in_row < ids_first || in_row >= ids_first + 32) {
-                        ids_seq = c.s, ids_first = in_row;
-                        ids = in_row + lane < v.max_blocks ? v.tables[(int64_t)c.s * v.max_blocks + in_row + lane] : -1;
-                    }
-                    const int id = __shfl_sync(0xffffffffu, ids, in_row - ids_first);
-                    there = (uint32_t)id < (uint32_t)v.nb;
-                    if (there)
-                        kvq_fetch_tile<D>(base + (int64_t)id * v.s_block + in_block * Z::kTileBytes, v.s_kv,
-                                          ring_at + buffer * Z::kBuffer + j * Z::kStage, lane);
-                    else if (lane == 0)
-                        kvq_error(v, kErrBadBlock);
-                    if (++in_block == v.block_tiles) in_block = 0, ++in_row;
-                }
-                const uint32_t bit = 1u << (buffer * kStepTiles + j);
-                absent = there ? absent & ~bit : absent | bit;
+                kvq_scores<D, NT>(buf + S::kK + j * S::kCodes, buf + S::kParK + j * S::kParams, g, t, qf, qsum, s[j]);
+                kvq_params<D>(buf + S::kParV + j * S::kParams, g, par[j]);
             }
-            if (++c.step == c.q.steps) {
-                next_unit<RB>(a, c);
-                enter();
-            }
-        };
-        long long ahead = w0 + 1;
-        issue(0);
-        cp_async_commit();
-
-        // ---- work ----
-        int buffer = 0;
-        for (long long x = w0; x < w1;) {
-            const int head = w.head, row0 = w.block * RB;
-            const int rows = min(RB, w.q.rows - row0);
-            const long long unit1 = unit0 + w.q.steps, stop = min(unit1, w1);
-
-            // queries of this lane's column g (+8): halves of the operand, their sums, and the exponent that was taken out
-            uint32_t qf[NT][D / 16][2];
-            float qsum[NT][G][2], back[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = row0 + min(8 * n + g, rows - 1);
-                const bool real = 8 * n + g < rows;
-                const uint16_t* src = a.q.data + (int64_t)(w.q.q0 + r / a.group) * a.q.s_token +
-                                      (int64_t)(head * a.group + r % a.group) * a.q.s_head + 2 * t;
-                kvq_load_queries<D>(src, a.bf != 0, real, t, qf[n], qsum[n], back[n], a.scale_log2);
-            }
-            // the positions of the first and the last row
-            const int low_limit = w.q.first_pos + row0 / a.group, high_limit = w.q.first_pos + (row0 + rows - 1) / a.group;
-            float o[NT][D / 16][4], ref[NT][2], sum[NT][2], low[NT][G][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
-                ref[n][0] = ref[n][1] = kNoRef, sum[n][0] = sum[n][1] = 0.f;
-#pragma unroll
-                for (int i = 0; i < G; ++i) low[n][i][0] = low[n][i][1] = 0.f;
-            }
-            float top_step = kTopStep, room = 25.f;  // p * top_step <= 2^15: p <= 2^room
-
-            for (; x < stop; ++x) {
-                cp_async_wait<0>();
-                __syncwarp();
-                const uint8_t* buf = ring + buffer * Z::kBuffer;
-                const uint32_t missing = absent >> (buffer * kStepTiles) & ((1u << kStepTiles) - 1);
-                buffer ^= 1;
-                if (ahead < w1) issue(buffer), ++ahead;
-                cp_async_commit();
-                const int key0 = (w.q.tile0 + w.step * kStepTiles) * kKvqTile;
-                ++w.step;
-
-                float s[kStepTiles][NT][4];
-                uint32_t par[kStepTiles][2][G];
-#pragma unroll
-                for (int j = 0; j < kStepTiles; ++j) {
-                    kvq_scores<D, NT>(buf + j * Z::kStage, g, t, qf, qsum, s[j]);
-                    kvq_params<D>(buf + j * Z::kStage + Z::kTileBytes, g, par[j]);
-                }
-                if (missing || key0 + kStepTokens - 1 > low_limit || key0 + kStepTokens > w.q.len ||
-                    (a.window > 0 && key0 <= high_limit - a.window)) {
-                    // what a row does not see gets -infinity; the steps and minima of tokens that are not there, 0
-#pragma unroll
-                    for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int key = key0 + j * kKvqTile + g + 8 * h;
-                            const bool there = key < w.q.len && !(missing >> j & 1);
-#pragma unroll
-                            for (int i = 0; i < G; ++i)
-                                if (!there) par[j][h][i] = 0;
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const int col = min(8 * n + 2 * t + e, rows - 1);
-                                    const int limit = w.q.first_pos + (row0 + col) / a.group;
-                                    if (!there || key > limit || (a.window > 0 && key <= limit - a.window))
-                                        s[j][n][2 * h + e] = -INFINITY;
-                                }
-                        }
-                }
-                float over = -INFINITY, step = 0.f;
+            if (missing || key0 + kStepTokens > wq.len || key0 + kStepTokens - 1 > wq.first_pos || a.window > 0) {
+                // what a row does not see gets -infinity; the steps and minima of tokens that are not there, 0
 #pragma unroll
                 for (int j = 0; j < kStepTiles; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        const int key = key0 + j * kKvqTile + g + 8 * h;
+                        const bool there = key < wq.len && !(missing >> j & 1);
 #pragma unroll
-                        for (int i = 0; i < G; ++i) step = fmaxf(step, bf_low(par[j][h][i]));
+                        for (int k = 0; k < G; ++k)
+                            if (!there) par[j][h][k] = 0;
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) over = fmaxf(over, fmaf(s[j][n][2 * h + e], back[n][e], -ref[n][e]));
+                            for (int e = 0; e < 2; ++e)
+                                if (!there || key > limit[n][e] || (a.window > 0 && key <= limit[n][e] - a.window))
+                                    s[j][n][2 * h + e] = -INFINITY;
                     }
-                if (__any_sync(0xffffffffu, over > room || step > top_step)) {
-                    float shift = 0.f;
-#pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, d));
-                    if (step > top_step) {  // a power of two, so that the accumulators change by one too
-                        const float now = __uint_as_float((__float_as_uint(step) & 0x7f800000u) + (5u << 23));
-                        shift = (float)((int)(__float_as_uint(now) >> 23) - (int)(__float_as_uint(top_step) >> 23));
-                        top_step = now, room -= shift;
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float top = -INFINITY;
-#pragma unroll
-                            for (int j = 0; j < kStepTiles; ++j) top = fmaxf(top, fmaxf(s[j][n][e], s[j][n][e + 2]) * back[n][e]);
-#pragma unroll
-                            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                            float now = ref[n][e] + shift;
-                            if (top - now > room) now = top + kSlack - room;
-                            const float fall = exp2f(ref[n][e] - now);
-                            ref[n][e] = now, sum[n][e] *= fall;
-#pragma unroll
-                            for (int i = 0; i < G; ++i) low[n][i][e] *= fall;
-#pragma unroll
-                            for (int i = 0; i < D / 16; ++i) o[n][i][e] *= fall, o[n][i][e + 2] *= fall;
-                        }
-                }
-#pragma unroll
-                for (int j = 0; j < kStepTiles; ++j) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            s[j][n][e] = exp2_approx(fmaf(s[j][n][e], back[n][e & 1], -ref[n][e & 1]));
-                            sum[n][e & 1] += s[j][n][e];
-                        }
-                    kvq_values<D, NT>(buf + j * Z::kStage + Z::kTileBytes, g, t, s[j], par[j], o, low);
-                }
             }
+            // probabilities against the references as they are; none above 2^room if their sums are not
+            float p[kStepTiles][NT][4], tsum[NT][2], step = 0.f;
+#pragma unroll
+            for (int k = 0; k < G; ++k) {
+                step = max3(step, bf_low(par[0][0][k]), bf_low(par[0][1][k]));
+                step = max3(step, bf_low(par[1][0][k]), bf_low(par[1][1][k]));
+            }
+#pragma unroll 1
+            for (int round = 0;; ++round) {
+                float most = 0.f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int j = 0; j < kStepTiles; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[j][n][e] = exp2_approx(fmaf(s[j][n][e], back[n][e & 1], -ref[n][e & 1]));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) tsum[n][e] = (p[0][n][e] + p[0][n][e + 2]) + (p[1][n][e] + p[1][n][e + 2]);
+                    most = max3(most, tsum[n][0], tsum[n][1]);
+                }
+                if (round || !__any_sync(0xffffffffu, most > bound || step > top_step)) break;
+                int shift = 0;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, d));
+                if (step > top_step) {  // a power of two, so that the accumulators change by one too
+                    const float now = __uint_as_float((__float_as_uint(step) & 0x7f800000u) + (5u << 23));
+                    shift = (int)(__float_as_uint(now) >> 23) - (int)(__float_as_uint(top_step) >> 23);
+                    top_step = now, bound = __uint_as_float(__float_as_uint(bound) - ((uint32_t)shift << 23));
+                }
+                const float room = (float)((int)(__float_as_uint(bound) >> 23) - 127);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(fmaxf(s[0][n][e], s[0][n][e + 2]), fmaxf(s[1][n][e], s[1][n][e + 2])) * back[n][e];
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        float now = ref[n][e] + (float)shift;
+                        if (top - now > room - 2.f) now = top + kSlack - room;  // four of them may be this large
+                        const float fall = exp2_approx(ref[n][e] - now);
+                        ref[n][e] = now, sum[n][e] *= fall;
+#pragma unroll
+                        for (int k = 0; k < G; ++k) low[n][k][e] *= fall;
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) o[n][k][e] *= fall, o[n][k][e + 2] *= fall;
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sum[n][0] += tsum[n][0], sum[n][1] += tsum[n][1];
+#pragma unroll
+            for (int j = 0; j < kStepTiles; ++j) kvq_values<D, NT>(buf + S::kV + j * S::kCodes, g, t, p[j], par[j], o, low);
 
+            const bool ended = w_step + 1 == wq.steps;
+            if (!ended && i < todo) continue;
             // ---- the unit is done, or this warp's share of it ----
-            const bool begun = unit0 >= w0, ended = unit1 <= w1;
+            const int unit0 = w0 + i - 1 - w_step;
+            const bool begun = unit0 >= w0;
+            const Unit u{unit0, unit0 + wq.steps, wq.q0, w_block * RB, min(RB, wq.rows - w_block * RB), w_head, 1};
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -409,115 +436,97 @@ __global__ void __launch_bounds__(kThreads, (D == 256 || NT == 2) ? 1 : 2) kvq_a
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], d);
 #pragma unroll
-                    for (int i = 0; i < G; ++i)
+                    for (int k = 0; k < G; ++k)
 #pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) low[n][i][e] += __shfl_xor_sync(0xffffffffu, low[n][i][e], d);
+                        for (int d = 4; d < 32; d <<= 1) low[n][k][e] += __shfl_xor_sync(0xffffffffu, low[n][k][e], d);
                 }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[n][i][e] = fmaf(o[n][i][e], e < 2 ? 1.f : 0.0625f, low[n][i / 4][e & 1]);
-            Part p{unit0, unit1, w.q.q0, row0, rows, head, 1};
+            const auto quad = [&](int n, int k) {
+                return make_float4(o[n][k][0] + low[n][k / 4][0], o[n][k][1] + low[n][k / 4][1],
+                                   fmaf(o[n][k][2], 0.0625f, low[n][k / 4][0]), fmaf(o[n][k][3], 0.0625f, low[n][k / 4][1]));
+            };
             if (begun && ended) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    float inv[2];
+                    const float inv[2] = {sum[n][0] == 0.f ? 0.f : 1.f / sum[n][0], sum[n][1] == 0.f ? 0.f : 1.f / sum[n][1]};
+                    if (a.lse && g == 0) put_lse(a, u, 8 * n + 2 * t, ref[n][0], sum[n][0]), put_lse(a, u, 8 * n + 2 * t + 1, ref[n][1], sum[n][1]);
+                    uint16_t* dst = out_row(a, u, n, g, t);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        inv[e] = sum[n][e] == 0.f ? 0.f : 1.f / sum[n][e];
-                        if (a.lse && g == 0 && 8 * n + 2 * t + e < rows) store_lse(a, p, 8 * n + 2 * t + e, ref[n][e], sum[n][e]);
-                    }
-                    const int r = row0 + 8 * n + g;
-                    uint16_t* dst = a.out.data + (int64_t)(w.q.q0 + r / a.group) * a.out.s_token +
-                                    (int64_t)(head * a.group + r % a.group) * a.out.s_head + 2 * t;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {  // dims 16i + 8h + 2t, +1 of row g
-                            const uint32_t y = transpose8(pack2(o[n][i][2 * h] * inv[0], o[n][i][2 * h + 1] * inv[1], a.bf != 0));
-                            if (8 * n + g < rows) *reinterpret_cast<uint32_t*>(dst + 16 * i + 8 * h) = y;
-                        }
+                    for (int k = 0; k < D / 16; ++k) put_quad<BF>(quad(n, k), inv, dst + 16 * k, 8 * n + g < u.rows);
                 }
             } else {
-                // a head part has a place of its own; a tail part ends the warp's share, so the ring is free
-                float* at = begun ? reinterpret_cast<float*>(ring) : head_part;
-                if (begun) {
-                    cp_async_wait<0>();
-                    __syncwarp();
-                }
+                // a head part has a place of its own; a tail part ends the warp's share, so the buffers are free
+                float* at = reinterpret_cast<float*>(ring + (begun ? 0 : Z::kRing));
+                __syncwarp();
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = 8 * n + 2 * t + e;
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            at[r * Z::kPitch + 16 * i + g] = o[n][i][e];
-                            at[r * Z::kPitch + 16 * i + 8 + g] = o[n][i][e + 2];
-                        }
-                        if (g == 0) at[RB * Z::kPitch + r] = ref[n][e], at[RB * Z::kPitch + RB + r] = sum[n][e];
+                    for (int k = 0; k < D / 16; ++k) *reinterpret_cast<float4*>(at + (n * (D / 16) + k) * 128 + lane * 4) = quad(n, k);
+                    if (g == 0) {
+                        *reinterpret_cast<float2*>(at + Z::kQuads * 128 + 8 * n + 2 * t) = make_float2(ref[n][0], ref[n][1]);
+                        *reinterpret_cast<float2*>(at + Z::kQuads * 128 + RB + 8 * n + 2 * t) = make_float2(sum[n][0], sum[n][1]);
                     }
-                if (lane == 0) parts[wid][begun] = p;
+                }
+                if (lane == 0) parts[wid][begun] = u;
             }
-            unit0 = unit1;
-            if (x < w1) next_unit<RB>(a, w);
+            fresh = true;
         }
-        cp_async_wait<0>();
     }
-    __syncthreads();
 
-    // ---- parts of one unit in this block ----
+    // ---- parts of one unit: first those in this block, then those of several blocks, by the block that arrives last ----
     uint32_t* counters = reinterpret_cast<uint32_t*>(a.workspace);
     float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
-    auto slot_of = [&](long long cta, int tail) { return slots + (2 * cta + tail) * Z::kSlotFloats; };
-    if (tid < 2) last_of[tid] = 0;
-    for (int w = -1; w < kWarps; ++w) {  // chains begin with the part that an earlier block began, or with a warp's tail
-        if (w < 0 ? !parts[0][0].live : !parts[w][1].live) continue;
-        const Part p = w < 0 ? parts[0][0] : parts[w][1];
-        const int w_first = max(w, 0);
-        int n = 1;
-        while (w_first + n < kWarps && parts[w_first + n][0].live && parts[w_first + n][0].from == p.from) ++n;
-        const bool alone = p.from >= cta0 && p.to <= cta1;
-        const auto part = [&](int i) {
-            return reinterpret_cast<const float*>(smem + (w_first + i) * Z::kWarpBytes + (w >= 0 && i == 0 ? 0 : Z::kRing));
-        };
-        if (alone) {
-            merge<D, NT>(a, p, n, Z::kPitch, part, static_cast<float*>(nullptr));
-        } else {
-            const int tail = p.from >= cta0;
-            merge<D, NT>(a, p, n, Z::kPitch, part, slot_of(blockIdx.x, tail));
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const long long first = p.from / per, last = (p.to - 1) / per;
-                const bool all = atomicAdd(&counters[first], 1u) == (uint32_t)(last - first);
-                if (all) counters[first] = 0;  // ready for the next call
-                __threadfence();
-                last_of[tail] = all;
+    bool shared = false;  // thread's chain is of a unit that other blocks have parts of
+    Chain c{};
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+        __syncthreads();
+        if (wid == 0) {
+            if (round == 0 && lane <= kWarps) {
+                // chains begin with the part that an earlier block began (lane 0), or with a warp's tail
+                const int at = max(lane - 1, 0);
+                const Unit* u = &parts[at][lane > 0];
+                if (u->live) {
+                    c.n = 1;
+#pragma unroll 1
+                    while (at + c.n < kWarps && parts[at + c.n][0].live && parts[at + c.n][0].from == u->from) ++c.n;
+                    uint8_t* warp = smem + at * Z::kWarpBytes;
+                    c.rest = reinterpret_cast<const float*>(warp + Z::kRing), c.first = lane > 0 ? reinterpret_cast<const float*>(warp) : c.rest;
+                    c.stride = Z::kWarpBytes / 4, c.unit = u;
+                    shared = u->from < cta0 || u->to > cta1;
+                    if (shared) c.slot = slots + (2 * blockIdx.x + (u->from >= cta0)) * Z::kPartFloats;
+                }
+            } else if (round == 1) {
+                c.n = 0;
+                if (shared) {
+                    const int first = (int)((uint32_t)c.unit->from / (uint32_t)per), last = (int)((uint32_t)(c.unit->to - 1) / (uint32_t)per);
+                    uint32_t before;
+                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + first) : "memory");
+                    if (before == (uint32_t)(last - first)) {
+                        counters[first] = 0;  // ready for the next call
+                        c.first = slots + (2 * first + 1) * Z::kPartFloats, c.rest = c.first - Z::kPartFloats, c.stride = 2 * Z::kPartFloats;
+                        c.slot = nullptr, c.n = last - first + 1;
+                    }
+                }
             }
-            __syncthreads();
-            if (last_of[tail]) {
-                const long long first = p.from / per;
-                const auto slot = [&](int i) { return static_cast<const float*>(slot_of(first + i, i == 0)); };
-                merge<D, NT>(a, p, (int)((p.to - 1) / per - first) + 1, D, slot, static_cast<float*>(nullptr));
-            }
+            const unsigned live = __ballot_sync(0xffffffffu, c.n > 0);
+            if (c.n > 0) chains[__popc(live & ((1u << lane) - 1))] = c;
+            if (lane == 0) num_chains = __popc(live);
         }
+        const bool any = __syncthreads_or(shared);
+        const int tasks = num_chains * Z::kQuads;
+#pragma unroll 1
+        for (int task = wid; task < tasks; task += kWarps) merge_quad<D, NT, BF>(a, chains[task / Z::kQuads], task % Z::kQuads, lane);
+        if (!any) return;
     }
 }
 
 template <int D, int NT>
-cudaError_t launch(AttendArgs& a, int sms, cudaStream_t stream) {
+cudaError_t launch(const AttendArgs& a, bool bf, int sms, cudaStream_t stream) {
     using Z = Sizes<D, NT>;
-    static_assert(Z::kBytes <= 227 * 1024, "shared memory");
-    static_assert((size_t)2 * kAttendMaxCtas * Z::kSlotFloats * 4 + kAttendCounterBytes <= kAttendWorkspace, "workspace");
-    const int per_sm = (D == 256 || NT == 2) ? 1 : 2;
-    const int grid = std::min(sms * per_sm, kAttendMaxCtas);
-    if (cudaError_t e = cudaFuncSetAttribute(kvq_attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Z::kBytes)) return e;
-    kvq_attend_kernel<D, NT><<<grid, kThreads, Z::kBytes, stream>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    static_assert(Z::kBytes <= 222 * 1024, "shared memory");
+    static_assert((size_t)2 * kAttendMaxCtas * Z::kPart + kAttendCounterBytes <= kAttendWorkspace, "workspace");
+    const int grid = std::min(sms, kAttendMaxCtas);
+    return launch_after(bf ? kvq_attend_kernel<D, NT, true> : kvq_attend_kernel<D, NT, false>, grid, Z::kThreads, Z::kBytes, stream, a);
 }
 
 }  // namespace
@@ -548,15 +557,17 @@ extern "C" remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq
     REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
     a.lse = lse, a.workspace = static_cast<uint8_t*>(workspace);
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.group = q_heads / pool->kv_heads, a.q_heads = q_heads, a.window = window, a.bf = dtype == REMP_DTYPE_BFLOAT;
-    a.spt = (a.v.num_seqs + kThreads - 1) / kThreads;
-    if ((int64_t)batch->num_tokens * a.group > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
+    a.group = q_heads / pool->kv_heads, a.q_heads = q_heads, a.window = window;
+    a.room = (int32_t)std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, 0x7fffffffLL);
+    // rows are divided by the group with one multiplication: exact while row * group stays below 2^32
+    if ((int64_t)batch->num_tokens * a.group * a.group > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
+    a.by_group = a.group == 1 ? 0 : (uint32_t)((0x100000000ULL + a.group - 1) / a.group);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const bool wide = (int64_t)batch->max_queries * a.group > 8;
     cudaError_t e;
-    if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, sms, stream) : launch<64, 1>(a, sms, stream);
-    else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, sms, stream) : launch<128, 1>(a, sms, stream);
-    else e = launch<256, 1>(a, sms, stream);
+    if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream) : launch<64, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
+    else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream) : launch<128, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
+    else e = launch<256, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
     if (e != cudaSuccess) return cuda_fail(e, "attention");
     return REMP_OK;
 }

@@ -11,7 +11,7 @@
 
 #include <algorithm>
 
-#include "remp_internal.h"
+#include "remp_launch.h"
 
 namespace remp {
 
@@ -21,8 +21,6 @@ constexpr int kChunk = 1024;  // blocks of a chunk = threads of a thread block
 
 // One launch up to here (entries: rows to write x table width). Above, the steps spread over the GPU.
 constexpr int64_t kSoloBlocks = 8192, kSoloEntries = 16384, kSoloForks = 1024;
-
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Exclusive count of `flag` over the thread block (kChunk threads).
 __device__ __forceinline__ int rank_in_block(bool flag) {
@@ -149,6 +147,7 @@ __device__ __forceinline__ void fork_row(const Fork& f, int i, int lane) {
 __global__ void __launch_bounds__(kChunk) fork_solo_kernel(Fork f, int chunks) {
     __shared__ int counts[kSoloBlocks / kChunk], nth[kSoloForks], ids[kSoloForks], words[3];
     f.counts = counts, f.nth = nth, f.ids = ids, f.words = words;
+    grid_begin();
     for (int c = 0; c < chunks; ++c) fork_count(f, c);
     fork_children(f);
     __syncthreads();
@@ -158,16 +157,16 @@ __global__ void __launch_bounds__(kChunk) fork_solo_kernel(Fork f, int chunks) {
 }
 
 __global__ void __launch_bounds__(kChunk) fork_count_kernel(Fork f, int chunks) {
-    grid_wait();
+    grid_begin();
     if ((int)blockIdx.x < chunks) fork_count(f, blockIdx.x);
     else fork_children(f);
 }
 __global__ void __launch_bounds__(kChunk) fork_ids_kernel(Fork f, int chunks) {
-    grid_wait();
+    grid_begin();
     fork_ids(f, blockIdx.x, chunks);
 }
 __global__ void __launch_bounds__(256) fork_rows_kernel(Fork f) {
-    grid_wait();
+    grid_begin();
     const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (i < f.m) fork_row(f, i, threadIdx.x & 31);
 }
@@ -223,17 +222,17 @@ __device__ __forceinline__ void free_row(const Free& f, int s, int lane) {
 }
 
 __global__ void __launch_bounds__(kChunk) free_solo_kernel(Free f) {
-    grid_wait();
+    grid_begin();
     free_begin(f, threadIdx.x, kChunk);
     __syncthreads();
     for (int s = threadIdx.x >> 5; s < f.num_seqs; s += kChunk / 32) free_row(f, s, threadIdx.x & 31);
 }
 __global__ void __launch_bounds__(256) free_begin_kernel(Free f) {
-    grid_wait();
+    grid_begin();
     free_begin(f, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 __global__ void __launch_bounds__(256) free_rows_kernel(Free f) {
-    grid_wait();
+    grid_begin();
     const int s = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (s < f.num_seqs) free_row(f, s, threadIdx.x & 31);
 }
@@ -312,7 +311,7 @@ __global__ void __launch_bounds__(kChunk) compact_solo_kernel(Compact c, int chu
     extern __shared__ int scratch[];
     __shared__ int counts[kSoloBlocks / kChunk];
     c.counts = counts, c.was = scratch, c.place = scratch + chunks * kChunk;
-    grid_wait();
+    grid_begin();
     for (int i = 0; i < chunks; ++i) compact_count(c, i);
     __syncthreads();
     for (int i = 0; i < chunks; ++i) compact_assign(c, i, chunks);
@@ -322,16 +321,16 @@ __global__ void __launch_bounds__(kChunk) compact_solo_kernel(Compact c, int chu
     for (int s = threadIdx.x >> 5; s < c.num_seqs; s += kChunk / 32) compact_row(c, s, threadIdx.x & 31, total);
 }
 __global__ void __launch_bounds__(kChunk) compact_count_kernel(Compact c) {
-    grid_wait();
+    grid_begin();
     compact_count(c, blockIdx.x);
 }
 __global__ void __launch_bounds__(kChunk) compact_assign_kernel(Compact c, int chunks) {
-    grid_wait();
+    grid_begin();
     compact_assign(c, blockIdx.x, chunks);
 }
 // Thread blocks below `chunks` write reference counts, the others table rows, 32 each.
 __global__ void __launch_bounds__(kChunk) compact_write_kernel(Compact c, int chunks) {
-    grid_wait();
+    grid_begin();
     const int total = sum_of_counts(c.counts, chunks);
     if ((int)blockIdx.x < chunks) {
         const int id = blockIdx.x * kChunk + threadIdx.x;
@@ -365,7 +364,7 @@ struct CopyArgs {
 
 template <bool DENSE>
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyArgs a) {
-    grid_wait();
+    grid_begin();
     const uint32_t n = (uint32_t)min(max(*a.count, 0), a.max_pairs);
     if (n == 0) return;
     const int lane = threadIdx.x & 31;
@@ -406,24 +405,6 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
         }
         at -= items;
     }
-}
-
-// Launch so that the kernel may be set up while the one before it in the stream finishes (each waits for it first).
-template <class... KArgs, class... Args>
-cudaError_t launch_after(void (*kernel)(KArgs...), int64_t grid, int threads, size_t smem, cudaStream_t stream, Args&&... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)grid, 1, 1);
-    cfg.blockDim = dim3((unsigned)threads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...)) return e;
-    count_launch();
-    return cudaGetLastError();
 }
 
 // Scratch of `ints` words from the library's pool, for the work that `use` enqueues on the stream.
@@ -472,9 +453,7 @@ extern "C" remp_status remp_pages_fork(int32_t* seq_lens, int32_t* block_tables,
            reinterpret_cast<int2*>(pairs), result, nullptr, nullptr, nullptr, nullptr};
     const int chunks = std::max(1, (num_blocks + kChunk - 1) / kChunk);
     if (num_blocks <= kSoloBlocks && num_forks <= kSoloForks && (int64_t)num_forks * max_blocks_per_seq <= kSoloEntries) {
-        fork_solo_kernel<<<1, kChunk, 0, stream>>>(f, chunks);
-        count_launch();
-        REMP_CUDA(cudaGetLastError());
+        REMP_CUDA(launch_after(fork_solo_kernel, 1, kChunk, 0, stream, f, chunks));
         return REMP_OK;
     }
     return with_scratch((int64_t)chunks + 2 * (int64_t)num_forks + 3, stream, [&](int* p) {
@@ -522,8 +501,6 @@ extern "C" remp_status remp_pages_compact(const int32_t* seq_lens, const int32_t
     const int chunks = std::max(1, (num_blocks + kChunk - 1) / kChunk);
     if (num_blocks <= kSoloBlocks && (int64_t)num_seqs * std::max(max_blocks_per_seq, 32) <= kSoloEntries) {
         const size_t smem = (size_t)2 * chunks * kChunk * 4;
-        if (smem > 48 * 1024)
-            REMP_CUDA(cudaFuncSetAttribute(compact_solo_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * kSoloBlocks * 4)));
         REMP_CUDA(launch_after(compact_solo_kernel, 1, kChunk, smem, stream, c, chunks));
         return REMP_OK;
     }
