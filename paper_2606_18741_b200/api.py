@@ -97,10 +97,29 @@ def _caps(dst_capacity_blocks):
     return _caps_cached(tuple(int(c) for c in dst_capacity_blocks))
 
 
+_torch = None
+_raw_stream = None
+
+
+def _load_torch():
+    """torch, imported on first use (host-only planning does without); also finds the cheapest way to ask for the current stream."""
+    global _torch, _raw_stream
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is not None and device is not None:
+        torch.cuda.init()
+        _raw_stream = lambda: raw(device())  # noqa: E731
+    else:
+        _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    _torch = torch
+    return torch
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
+        if _raw_stream is None:
+            _load_torch()
+        return _raw_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -354,9 +373,14 @@ def make_kvq_pool(buffer, num_blocks: int, kv_heads: int, head_dim: int, block_s
     return pool
 
 
-def _int32_cuda(t, name: str) -> int:
+@functools.lru_cache(maxsize=None)
+def _types():
     import torch
-    if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+    return torch.int32, torch.float32, {torch.bfloat16: REMP_DTYPE_BFLOAT, torch.float16: REMP_DTYPE_HALF}
+
+
+def _int32_cuda(t, name: str) -> int:
+    if t.dtype is not _types()[0] or not t.is_cuda or not t.is_contiguous():
         raise RempError(REMP_ERR_INVALID_ARG, f"{name} must be a contiguous int32 CUDA tensor")
     return t.data_ptr()
 
@@ -381,15 +405,9 @@ def make_kvq_workspace(device=None):
     return torch.zeros(int(_lib.load().remp_kvq_workspace_bytes()), dtype=torch.uint8, device=device or "cuda")
 
 
-@functools.lru_cache(maxsize=None)
-def _dtypes():
-    import torch
-    return {torch.bfloat16: REMP_DTYPE_BFLOAT, torch.float16: REMP_DTYPE_HALF}
-
-
 def _rows(t, name: str, num_tokens: int, heads: int, head_dim: int, dtype):
     """remp_kvq_rows of a CUDA tensor [num_tokens][heads][head_dim]."""
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (num_tokens, heads, head_dim):
+    if t.dtype is not dtype or not t.is_cuda or t.shape != (num_tokens, heads, head_dim):
         raise RempError(REMP_ERR_SHAPE, f"{name} must be a CUDA tensor [{num_tokens}][{heads}][{head_dim}] of {dtype}")
     st, sh, sd = t.stride()
     if sd != 1:
@@ -398,10 +416,9 @@ def _rows(t, name: str, num_tokens: int, heads: int, head_dim: int, dtype):
 
 
 def _f32_cuda(t, name: str, *shape) -> Optional[int]:
-    import torch
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or (shape and tuple(t.shape) != shape):
+    if t.dtype is not _types()[1] or not t.is_cuda or not t.is_contiguous() or (shape and t.shape != shape):
         raise RempError(REMP_ERR_SHAPE, f"{name} must be a contiguous float32 CUDA tensor{list(shape) if shape else ''}")
     return t.data_ptr()
 
@@ -414,7 +431,7 @@ def remp_kvq_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_no
     [num_tokens] rows of rope (default: the token's position). Only enqueues."""
     n, d = batch.num_tokens, pool.head_dim
     dtype = k.dtype
-    if dtype not in _dtypes():
+    if dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "k must be bfloat16 or float16")
     heads = int(q.shape[1]) if q is not None else 0
     tr = None
@@ -428,7 +445,7 @@ def remp_kvq_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_no
     _check(_lib.load().remp_kvq_append(
         pool, batch, _rows(q, "q", n, heads, d, dtype) if q is not None else None, _rows(k, "k", n, pool.kv_heads, d, dtype),
         _rows(v, "v", n, pool.kv_heads, d, dtype),
-        _rows(q_out, "q_out", n, heads, d, dtype) if q_out is not None else None, heads, _dtypes()[dtype], tr,
+        _rows(q_out, "q_out", n, heads, d, dtype) if q_out is not None else None, heads, _types()[2][dtype], tr,
         _stream_ptr(stream)))
 
 
@@ -439,11 +456,11 @@ def remp_kvq_read(pool: RempKvqPool, batch: RempKvqBatch, k_out, v_out, stream=N
     some = k_out if k_out is not None else v_out
     if some is None:
         return
-    if some.dtype not in _dtypes():
+    if some.dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "outputs must be bfloat16 or float16")
     _check(_lib.load().remp_kvq_read(pool, batch, _rows(k_out, "k_out", n, h, d, some.dtype) if k_out is not None else None,
                                      _rows(v_out, "v_out", n, h, d, some.dtype) if v_out is not None else None,
-                                     _dtypes()[some.dtype], _stream_ptr(stream)))
+                                     _types()[2][some.dtype], _stream_ptr(stream)))
 
 
 def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float, workspace, window: int = 0, lse=None,
@@ -452,13 +469,13 @@ def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float
     shape); window > 0: over the last `window` positions only. lse: float32 [num_tokens][heads] or None. workspace:
     make_kvq_workspace(). Only enqueues."""
     n, d = batch.num_tokens, pool.head_dim
-    if q.dtype not in _dtypes():
+    if q.dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
     heads = int(q.shape[1])
-    if not workspace.is_cuda or workspace.numel() * workspace.element_size() < _workspace_bytes():
+    if not workspace.is_cuda or workspace.nbytes < _workspace_bytes():
         raise RempError(REMP_ERR_INVALID_ARG, "the workspace is too small")
     _check(_lib.load().remp_kvq_attend(pool, batch, _rows(q, "q", n, heads, d, q.dtype), _rows(out, "out", n, heads, d, q.dtype),
-                                       heads, _dtypes()[q.dtype], scale, window, _f32_cuda(lse, "lse", n, heads),
+                                       heads, _types()[2][q.dtype], scale, window, _f32_cuda(lse, "lse", n, heads),
                                        workspace.data_ptr(), _stream_ptr(stream)))
 
 
@@ -470,10 +487,10 @@ def _workspace_bytes() -> int:
 # ---- pages between two switches ----
 
 def _tables_of(seq_lens, block_tables):
-    n = int(seq_lens.shape[0])
-    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n:
+    n, shape = seq_lens.shape[0], block_tables.shape
+    if len(shape) != 2 or shape[0] != n:
         raise RempError(REMP_ERR_INVALID_ARG, "block_tables must be [n][max_blocks]")
-    return _int32_cuda(seq_lens, "seq_lens"), _int32_cuda(block_tables, "block_tables"), n, int(block_tables.shape[1])
+    return _int32_cuda(seq_lens, "seq_lens"), _int32_cuda(block_tables, "block_tables"), n, shape[1]
 
 
 def _same(t, like, name: str) -> int:
@@ -483,7 +500,8 @@ def _same(t, like, name: str) -> int:
 
 
 def _pairs_of(pairs, result, least: int):
-    if pairs.dim() != 2 or int(pairs.shape[1]) != 2 or int(pairs.shape[0]) < least or result.numel() != 2:
+    shape = pairs.shape
+    if len(shape) != 2 or shape[1] != 2 or shape[0] < least or result.numel() != 2:
         raise RempError(REMP_ERR_INVALID_ARG, f"pairs must be [{least} or more][2] and result [2]")
     return _int32_cuda(pairs, "pairs"), _int32_cuda(result, "result")
 
