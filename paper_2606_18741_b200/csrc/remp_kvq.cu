@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, c
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
     const bool bf = bf_ != 0;
-    grid_begin();
+    grid_wait();
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
     const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     const int token = (int)(item / sets_per_token);

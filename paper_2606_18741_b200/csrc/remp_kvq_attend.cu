@@ -29,6 +29,7 @@ namespace {
 constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
+constexpr int kPromptRows = 16;  // rows of a sequence and KV head above which they are a prompt's (remp_kvq_prompt.cu)
 constexpr int kStepTiles = 2, kStepTokens = kStepTiles * kKvqTile;
 
 struct AttendArgs {
@@ -563,11 +564,15 @@ extern "C" remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq
     if ((int64_t)batch->num_tokens * a.group * a.group > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
     a.by_group = a.group == 1 ? 0 : (uint32_t)((0x100000000ULL + a.group - 1) / a.group);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const bool wide = (int64_t)batch->max_queries * a.group > 8;
+    const int64_t max_rows = (int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group;
+    const bool bf = dtype == REMP_DTYPE_BFLOAT, wide = max_rows > 8;
     cudaError_t e;
-    if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream) : launch<64, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
-    else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream) : launch<128, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
-    else e = launch<256, 1>(a, dtype == REMP_DTYPE_BFLOAT, sms, stream);
+    if (max_rows > kPromptRows)
+        e = launch_prompt(a.v, a.q, a.out, lse, workspace, a.scale_log2, pool->head_dim, q_heads, a.group, a.by_group, window, a.room, bf, sms,
+                          (int32_t)max_rows, stream);
+    else if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, bf, sms, stream) : launch<64, 1>(a, bf, sms, stream);
+    else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, bf, sms, stream) : launch<128, 1>(a, bf, sms, stream);
+    else e = launch<256, 1>(a, bf, sms, stream);
     if (e != cudaSuccess) return cuda_fail(e, "attention");
     return REMP_OK;
 }

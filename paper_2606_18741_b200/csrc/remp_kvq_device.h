@@ -11,7 +11,12 @@ namespace remp {
 
 constexpr int kAttendMaxCtas = 512;
 constexpr size_t kAttendCounterBytes = kAttendMaxCtas * 4;
-constexpr size_t kAttendWorkspace = kAttendCounterBytes + (size_t)2 * kAttendMaxCtas * 16 * (128 + 2) * 4;
+constexpr size_t kAttendWorkspace = kAttendCounterBytes + (size_t)300 * 128 * (128 + 2) * 4;  // parts of prompts are the largest
+
+// remp_kvq_prompt.cu: many queries of a sequence
+cudaError_t launch_prompt(const KvqView& v, const KvqRows& q, const KvqRows& out, float* lse, void* workspace, float scale_log2, int32_t head_dim,
+                          int32_t q_heads, int32_t group, uint32_t by_group, int32_t window, int32_t room, bool bf, int sms, int32_t max_rows,
+                          cudaStream_t stream);
 
 #ifdef __CUDACC__
 

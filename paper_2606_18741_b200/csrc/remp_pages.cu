@@ -147,7 +147,7 @@ __device__ __forceinline__ void fork_row(const Fork& f, int i, int lane) {
 __global__ void __launch_bounds__(kChunk) fork_solo_kernel(Fork f, int chunks) {
     __shared__ int counts[kSoloBlocks / kChunk], nth[kSoloForks], ids[kSoloForks], words[3];
     f.counts = counts, f.nth = nth, f.ids = ids, f.words = words;
-    grid_begin();
+    grid_wait();
     for (int c = 0; c < chunks; ++c) fork_count(f, c);
     fork_children(f);
     __syncthreads();
@@ -157,16 +157,16 @@ __global__ void __launch_bounds__(kChunk) fork_solo_kernel(Fork f, int chunks) {
 }
 
 __global__ void __launch_bounds__(kChunk) fork_count_kernel(Fork f, int chunks) {
-    grid_begin();
+    grid_wait();
     if ((int)blockIdx.x < chunks) fork_count(f, blockIdx.x);
     else fork_children(f);
 }
 __global__ void __launch_bounds__(kChunk) fork_ids_kernel(Fork f, int chunks) {
-    grid_begin();
+    grid_wait();
     fork_ids(f, blockIdx.x, chunks);
 }
 __global__ void __launch_bounds__(256) fork_rows_kernel(Fork f) {
-    grid_begin();
+    grid_wait();
     const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (i < f.m) fork_row(f, i, threadIdx.x & 31);
 }
@@ -222,17 +222,17 @@ __device__ __forceinline__ void free_row(const Free& f, int s, int lane) {
 }
 
 __global__ void __launch_bounds__(kChunk) free_solo_kernel(Free f) {
-    grid_begin();
+    grid_wait();
     free_begin(f, threadIdx.x, kChunk);
     __syncthreads();
     for (int s = threadIdx.x >> 5; s < f.num_seqs; s += kChunk / 32) free_row(f, s, threadIdx.x & 31);
 }
 __global__ void __launch_bounds__(256) free_begin_kernel(Free f) {
-    grid_begin();
+    grid_wait();
     free_begin(f, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 __global__ void __launch_bounds__(256) free_rows_kernel(Free f) {
-    grid_begin();
+    grid_wait();
     const int s = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (s < f.num_seqs) free_row(f, s, threadIdx.x & 31);
 }
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kChunk) compact_solo_kernel(Compact c, int chu
     extern __shared__ int scratch[];
     __shared__ int counts[kSoloBlocks / kChunk];
     c.counts = counts, c.was = scratch, c.place = scratch + chunks * kChunk;
-    grid_begin();
+    grid_wait();
     for (int i = 0; i < chunks; ++i) compact_count(c, i);
     __syncthreads();
     for (int i = 0; i < chunks; ++i) compact_assign(c, i, chunks);
@@ -321,16 +321,16 @@ __global__ void __launch_bounds__(kChunk) compact_solo_kernel(Compact c, int chu
     for (int s = threadIdx.x >> 5; s < c.num_seqs; s += kChunk / 32) compact_row(c, s, threadIdx.x & 31, total);
 }
 __global__ void __launch_bounds__(kChunk) compact_count_kernel(Compact c) {
-    grid_begin();
+    grid_wait();
     compact_count(c, blockIdx.x);
 }
 __global__ void __launch_bounds__(kChunk) compact_assign_kernel(Compact c, int chunks) {
-    grid_begin();
+    grid_wait();
     compact_assign(c, blockIdx.x, chunks);
 }
 // Thread blocks below `chunks` write reference counts, the others table rows, 32 each.
 __global__ void __launch_bounds__(kChunk) compact_write_kernel(Compact c, int chunks) {
-    grid_begin();
+    grid_wait();
     const int total = sum_of_counts(c.counts, chunks);
     if ((int)blockIdx.x < chunks) {
         const int id = blockIdx.x * kChunk + threadIdx.x;
@@ -364,7 +364,7 @@ struct CopyArgs {
 
 template <bool DENSE>
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyArgs a) {
-    grid_begin();
+    grid_wait();
     const uint32_t n = (uint32_t)min(max(*a.count, 0), a.max_pairs);
     if (n == 0) return;
     const int lane = threadIdx.x & 31;

@@ -121,11 +121,12 @@ class Pool:
 
 
 def attend(q, k, v, first_pos, scale, window):
-    """q [n][Hq][D], k and v [len][Hkv][D] in 64 bits (NaN rows: not there) -> out [n][Hq][D], lse [n][Hq], and the sums of
-    p*|v - min over the row| that bound what rounding p*step to 11 bits can do."""
+    """q [n][Hq][D], k and v [len][Hkv][D] in 64 bits (NaN rows: not there) -> out [n][Hq][D], lse [n][Hq], and what bounds the
+    rounding: sums of p * (spread of v's row), sums of p * (largest of v's row), and the most that a score moves where keys
+    are rounded to 11 bits."""
     n, hq, d = q.shape
     length, hk, _ = k.shape
-    out, lse, weight = np.zeros((n, hq, d)), np.full((n, hq), -np.inf), np.zeros((n, hq))
+    out, lse, weight, size, move = np.zeros((n, hq, d)), np.full((n, hq), -np.inf), np.zeros((n, hq)), np.zeros((n, hq)), np.zeros((n, hq))
     key = np.arange(length)
     for i in range(n):
         pos = first_pos + i
@@ -142,7 +143,9 @@ def attend(q, k, v, first_pos, scale, window):
             out[i, h] = e @ vv / e.sum()
             lse[i, h] = top + np.log(e.sum())
             weight[i, h] = (e @ (vv.max(-1) - vv.min(-1))) / e.sum()
-    return out, lse, weight
+            size[i, h] = (e @ np.abs(vv).max(-1)) / e.sum()
+            move[i, h] = scale * (np.abs(kk) @ np.abs(q[i, h])).max() * 2.0 ** -11
+    return out, lse, weight, size, move
 
 
 # ---- pages ----

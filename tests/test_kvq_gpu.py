@@ -5,6 +5,9 @@ are one float32 multiply-add, rounded once to 16 bits. Attention: p*step is roun
 codes it meets are at most the row's spread), scores carry the float32 sums of the matrix instructions (a few 2^-20), the
 output is rounded once to its type: |error| <= half an ulp of the output + 2^-10 * sum of p * spread of V's row.
 lse: 2e-5, from float32 sums of scores up to a few tens.
+With more than 16 rows of a sequence and KV head (PROMPT_ROWS), keys, values and probabilities are rounded to half: a value
+and a probability by 2^-11 of themselves, a score by at most `move` = scale * sum |q||k| * 2^-11, a probability's share by
+twice that: |error| <= half an ulp + (2^-10 + 2 move) * sum of p * largest of V's row; lse: 2e-5 + move.
 """
 import math
 
@@ -17,6 +20,7 @@ from tests import kvq_reference as ref
 
 pytestmark = pytest.mark.gpu
 
+PROMPT_ROWS = 16
 ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 
 
@@ -214,15 +218,17 @@ def _check(out, lse, q, pool, layer, lens, new, tables, scale, window, dtype):
         n, length = int(new[s]), max(0, int(lens[s]))
         length = min(length, tables.shape[1] * pool.bs)
         k, v = (pool.rows(layer, kv, tables[s], length) for kv in (0, 1))
-        want, want_lse, weight = ref.attend(q[at:at + n].double().cpu().numpy(), k, v, int(lens[s]) - n, scale, window)
+        want, want_lse, weight, size, move = ref.attend(q[at:at + n].double().cpu().numpy(), k, v, int(lens[s]) - n, scale, window)
         got = out[at:at + n].double().cpu().numpy()
-        tol = ULP[dtype] / 2 * np.abs(want) + 2.0 ** -10 * weight[..., None] + 2.0 ** -24
+        prompt = int(new.max()) * q.shape[1] // pool.heads > PROMPT_ROWS
+        rounding = (2.0 ** -10 + 2 * move) * size if prompt else 2.0 ** -10 * weight
+        tol = ULP[dtype] / 2 * np.abs(want) + rounding[..., None] + 2.0 ** -24
         assert (np.abs(got - want) <= tol).all(), (s, n, length, np.abs(got - want).max())
         if lse is not None:
             g = lse[at:at + n].double().cpu().numpy()
             assert np.array_equal(np.isinf(g), np.isinf(want_lse))
             f = np.isfinite(want_lse)
-            assert (np.abs(g[f] - want_lse[f]) <= 2e-5 * np.maximum(1, np.abs(want_lse[f]))).all()
+            assert (np.abs(g[f] - want_lse[f]) <= 2e-5 * np.maximum(1, np.abs(want_lse[f])) + (move[f] if prompt else 0)).all()
         at += n
 
 
@@ -303,6 +309,68 @@ def test_attend_query_sizes(q_scale):
 
 def test_attend_layer_of_a_pool():
     _attend_case(128, 8, 2, 16, torch.bfloat16, [100, 33], [1, 1], layers=3, layer=2, seed=4)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hq,hk,lens,new", [
+    (8, 1, [40], [40]), (8, 1, [16], [16]), (5, 1, [150, 30, 200], [37, 30, 1]), (2, 2, [130, 128, 129, 127], [130, 64, 65, 127]),
+    (16, 2, [300, 0, 17, 5], [20, 0, 17, 9]), (1, 1, [700], [260]), (7, 1, [64, 65], [19, 65])])
+def test_attend_prompts(d, hq, hk, lens, new):
+    _attend_case(d, hq, hk, 16, torch.bfloat16, lens, new, seed=d + hq)
+
+
+@pytest.mark.parametrize("window", [1, 15, 64, 200])
+def test_attend_prompts_window_blocks_and_half(window):
+    _attend_case(128, 4, 1, 32, torch.float16, [150, 90, 333], [150, 33, 40], window=window, seed=window)
+    _attend_case(64, 4, 2, 48, torch.bfloat16, [150, 90, 33], [15, 90, 40], window=window, seed=window, layers=2, layer=1)
+
+
+def test_attend_prompts_whole_gpu_and_few_units_one_workspace():
+    # more thread blocks than the GPU holds, then one unit whose keys are split, then single tokens, all on one workspace
+    ws = _attend_case(128, 32, 32, 16, torch.bfloat16, [40] * 12, [40] * 12, seed=1)
+    _attend_case(128, 8, 1, 16, torch.bfloat16, [1500], [5], seed=2, ws=ws)
+    _attend_case(256, 8, 1, 16, torch.bfloat16, [900], [5], seed=2, ws=ws)
+    _attend_case(128, 8, 1, 16, torch.bfloat16, [1500], [1], seed=2, ws=ws)
+    _attend_case(64, 8, 2, 16, torch.bfloat16, [800, 10], [30, 10], seed=3, ws=ws)
+
+
+@pytest.mark.parametrize("q_scale", [1e-6, 1e4])
+def test_attend_prompts_query_sizes(q_scale):
+    _attend_case(128, 8, 2, 16, torch.bfloat16, [100, 33], [30, 10], q_scale=q_scale, seed=4)
+
+
+def test_attend_prompts_sharp_scores():
+    # scores that grow along the keys: references move again and again, in the first 32 keys of a block and behind
+    rng = np.random.default_rng(0)
+    d, bs, length, n = 64, 16, 400, 30
+    lens, new, tables, start, batch = _batch([length], [n], bs, 25, rng)
+    pool = ref.Pool(1, 25, 1, d, bs)
+    base = rng.standard_normal(d)
+    q = torch.from_numpy(np.tile(base, (n, 1, 1)) + 0.1 * rng.standard_normal((n, 1, d))).bfloat16().cuda()
+    for p in range(length):
+        pool.write(0, 0, tables[0, p // bs], p, (base * (p / 16)).astype(np.float32)[None])
+        pool.write(0, 1, tables[0, p // bs], p, rng.standard_normal((1, d)).astype(np.float32))
+    buf, dev = _dev_pool(pool)
+    out, lse = torch.empty_like(q), torch.empty(n, 1, device="cuda")
+    remp.remp_kvq_attend(dev, batch, q, out, d ** -0.5, remp.make_kvq_workspace(), lse=lse)
+    _check(out, lse, q, pool, 0, lens, new, tables, d ** -0.5, 0, torch.bfloat16)
+
+
+def test_attend_prompts_bad_blocks():
+    rng = np.random.default_rng(6)
+    d, bs, hk, n = 128, 16, 1, 24
+    pool = _filled(6, hk, d, bs, rng)
+    error = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lens, new = np.array([90, 70], dtype=np.int32), np.array([n, n], dtype=np.int32)
+    tables = np.array([[0, 77, 2, 1, 4, 5], [-1, 1, 2, 3, 1 << 30, 0]], dtype=np.int32)
+    start = np.array([0, n, 2 * n], dtype=np.int32)
+    batch = _dev_batch(lens, tables, start, new, error)
+    buf, dev = _dev_pool(pool)
+    q = torch.randn(2 * n, 4, d, device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(2 * n, 4, device="cuda")
+    remp.remp_kvq_attend(dev, batch, q, out, d ** -0.5, remp.make_kvq_workspace(), lse=lse)
+    _check(out, lse, q, pool, 0, lens, new, tables, d ** -0.5, 0, torch.bfloat16)
+    assert int(error) == 8
 
 
 def test_attend_sharp_scores():
