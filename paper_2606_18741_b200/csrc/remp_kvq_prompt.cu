@@ -117,17 +117,21 @@ __device__ __forceinline__ void for_tensor_cores() { asm volatile("fence.proxy.a
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
 __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 
-// A quarter of a step and of a minimum, kept where step * 15 + minimum is a finite half.
-__device__ __forceinline__ float quarter_step(uint32_t par) { return fminf(bf_low(par) * 0.25f, 4000.f); }
-__device__ __forceinline__ float quarter_low(uint32_t par) {
-    const float m = bf_high(par) * 0.25f;
-    return fabsf(m) > 62000.f ? copysignf(62000.f, m) : m;  // NaN stays
+// Two numbers as halves, kept finite (NaN stays).
+__device__ __forceinline__ __half2 finite_halves(float lo, float hi) {
+    uint32_t x;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
+    return as_half2(x);
 }
-// codes at bits 0..3 (4..7 with UPPER) of both halves of x, times step, plus low
-template <bool UPPER>
+// codes at bits 0..3 of both halves of x, times step, plus low
 __device__ __forceinline__ uint32_t halves_of(uint32_t x, __half2 step, __half2 low) {
-    const __half2 c = __hsub2(as_half2((x & (UPPER ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u), __half2half2(__ushort_as_half(0x6400)));
-    return as_word(__hfma2(c, step, low));
+    uint32_t y;  // 1024 + code: one instruction takes the bits and sets the others
+    asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(0x64006400u));
+    return as_word(__hfma2(__hsub2(as_half2(y), __half2half2(__ushort_as_half(0x6400))), step, low));
+}
+// the four codes of either half of w
+__device__ __forceinline__ void four_halves(uint32_t w, __half2 step, __half2 low, uint32_t (&z)[4]) {
+    z[0] = halves_of(w, step, low), z[1] = halves_of(w >> 4, step, low), z[2] = halves_of(w >> 8, step, low), z[3] = halves_of(w >> 12, step, low);
 }
 
 struct PromptArgs {
@@ -164,84 +168,70 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
     }
 }
 
-// The tile of K, the one of V `kv` behind it; null: nothing is there; the tokens from `valid` on are not.
+// A lane's words of a tile of K, or of V; `tile` null: nothing is there.
 template <int D>
 __device__ __forceinline__ void load_k(const uint8_t* tile, int g, int t, RawK<D>& r) {
+    if (tile) {
+        const uint8_t *codes = tile + g * (D / 2) + t * (D / 8), *params = tile + kKvqTile * D / 2 + g * (D / 16);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (tile) {
-            load_words(tile + (g + 8 * h) * (D / 2) + t * (D / 8), r.w[h]);
-            load_words(tile + kKvqTile * D / 2 + (g + 8 * h) * (D / 16), r.par[h]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) r.w[h][i] = 0;
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) r.par[h][i] = 0;
-        }
+        for (int h = 0; h < 2; ++h) load_words(codes + h * 4 * D, r.w[h]), load_words(params + h * (D / 2), r.par[h]);
     }
 }
+// The tokens from `valid` on are not there: their values are 0, whatever their slots hold.
 template <int D>
-__device__ __forceinline__ void load_v(const uint8_t* k_tile, int64_t kv, int valid, int g, int t, RawV<D>& r) {
+__device__ __forceinline__ void load_v(const uint8_t* tile, int valid, int g, int t, RawV<D>& r) {
+    if (tile) {
+        const uint8_t *codes = tile + t * D + g * (D / 16), *params = tile + kKvqTile * D / 2 + t * (D / 8);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int token = 2 * t + (j & 1) + (j >> 1) * 8;
-        if (k_tile && token < valid) {
-            const uint8_t* tile = k_tile + kv;
-            load_words(tile + token * (D / 2) + g * (D / 16), r.w[j]);
-            load_words(tile + kKvqTile * D / 2 + token * (D / 16), r.par[j]);
-        } else {
+        for (int j = 0; j < 4; ++j)
+            load_words(codes + (j >> 1) * 4 * D + (j & 1) * (D / 2), r.w[j]), load_words(params + (j >> 1) * (D / 2) + (j & 1) * (D / 16), r.par[j]);
+    }
+    if (!tile || valid < kKvqTile) {
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) r.w[j][i] = r.par[j][i] = 0;
-        }
+        for (int j = 0; j < 4; ++j)
+            if (!tile || 2 * t + (j & 1) + (j >> 1) * 8 >= valid)
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) r.par[j][i] = 0;
     }
 }
 
-// Rows of K: key tile * 16 + g (+ 8), dims in pieces of 8.
+// Rows of K, a key each: place[c] is where piece c of this lane's 8 keys' rows begins, for its words of the pieces. i: the
+// tile of the warp's.
 template <int D>
-__device__ __forceinline__ void store_k(uint8_t* k, int tile, int g, int t, const RawK<D>& r) {
-    constexpr int kKeys = Prompt<D>::kKeys;
+__device__ __forceinline__ void store_k(uint8_t* const (&place)[8], int i, const RawK<D>& r) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int key = tile * kKvqTile + g + 8 * h;
-        uint8_t* row = k + key * 128 + t * 4;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int grp = 0; grp < D / 64; ++grp) {
-            const __half2 step = __float2half2_rn(quarter_step(r.par[h][grp])), low = __float2half2_rn(quarter_low(r.par[h][grp]));
+            const float s = bf_low(r.par[h][grp]) * 0.25f, m = bf_high(r.par[h][grp]) * 0.25f;
+            const __half2 step = finite_halves(s, s), low = finite_halves(m, m);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t x = r.w[h][2 * grp + i], y = x >> 8;
-                const uint32_t z[4] = {halves_of<false>(x, step, low), halves_of<false>(x >> 4, step, low), halves_of<false>(y, step, low),
-                                       halves_of<false>(y >> 4, step, low)};
+            for (int x = 0; x < 2; ++x) {
+                uint32_t z[4];
+                four_halves(r.w[h][2 * grp + x], step, low, z);
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    *reinterpret_cast<uint32_t*>(row + grp * (kKeys * 128) + (((4 * i + b) ^ g) << 4)) = z[b];
+                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(place[4 * x + b] + (i * kKvqTile + 8 * h + grp * Prompt<D>::kKeys) * 128) = z[b];
             }
         }
-    }
 }
 
-// Rows of V^T: dims 64 grp + 8 n + g, keys tile * 16 + 2t, +1 (+ 8).
+// Rows of V^T, a dim each: row 8n + g from `place` on, two keys to a word.
 template <int D>
-__device__ __forceinline__ void store_v(uint8_t* v, int tile, int g, int t, const RawV<D>& r) {
+__device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D>& r) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int piece = (tile % 4) * 2 + h;
-        uint8_t* row = v + (tile / 4) * (D * 128) + g * 128 + ((piece ^ g) << 4) + t * 4;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int grp = 0; grp < D / 64; ++grp) {
             const uint32_t p0 = r.par[2 * h][grp], p1 = r.par[2 * h + 1][grp];
-            const __half2 step = __floats2half2_rn(quarter_step(p0), quarter_step(p1)), low = __floats2half2_rn(quarter_low(p0), quarter_low(p1));
-            const uint32_t w0 = r.w[2 * h][grp], w1 = r.w[2 * h + 1][grp];
+            const __half2 step = finite_halves(bf_low(p0) * 0.25f, bf_low(p1) * 0.25f), low = finite_halves(bf_high(p0) * 0.25f, bf_high(p1) * 0.25f);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t x = __byte_perm(w0, w1, i ? 0x7632 : 0x5410), y = x >> 8;
-                const uint32_t z[4] = {halves_of<false>(x, step, low), halves_of<false>(x >> 4, step, low), halves_of<false>(y, step, low),
-                                       halves_of<false>(y >> 4, step, low)};
+            for (int x = 0; x < 2; ++x) {
+                uint32_t z[4];
+                four_halves(__byte_perm(r.w[2 * h][grp], r.w[2 * h + 1][grp], x ? 0x7632 : 0x5410), step, low, z);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(row + (grp * 64 + 8 * (4 * i + b)) * 128) = z[b];
+                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(place[h] + (grp * 64 + 8 * (4 * x + b)) * 128) = z[b];
             }
         }
-    }
 }
 
 template <int D, bool BF>
@@ -278,7 +268,7 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
     const int b0 = (int)((long long)blocks_all * split / a.splits), b1 = (int)((long long)blocks_all * (split + 1) / a.splits);
     const int blocks = b1 - b0, first_key = begin + b0 * Z::kKeys;
 
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_) + 1023) & ~(uintptr_t)1023);
+    uint8_t* smem = smem_ + ((1024u - ((uint32_t)__cvta_generic_to_shared(smem_) & 1023u)) & 1023u);
     uint8_t *sq = smem, *sk = smem + Z::kQ, *sv = sk + Z::kK;
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t k_full = bar, v_full = bar + 8, s_full = bar + 16, p_full = bar + 24, o_done = bar + 32, q_full = bar + 40;
@@ -521,13 +511,19 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
 #pragma unroll
         for (int i = 0; i < Z::kWarpTiles; ++i) load_k<D>(at[i], g, t, rk[i]);
 #pragma unroll
-        for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i], v.s_kv, valid(0, i), g, t, rv[i]);
+        for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i] ? at[i] + v.s_kv : nullptr, valid(0, i), g, t, rv[i]);
 #pragma unroll 1
         for (int j = 0; j < blocks; ++j) {
             find(j + 1);
             if (j > 0) bar_wait(s_full, (j - 1) & 1, &dead);
+            {
+                uint8_t* place[8];
+                const int at0 = (w * Z::kWarpTiles * kKvqTile + g) * 128 + (g << 4) + t * 4;
 #pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) store_k<D>(sk, w * Z::kWarpTiles + i, g, t, rk[i]);
+                for (int c = 0; c < 8; ++c) place[c] = sk + (at0 ^ (c << 4));
+#pragma unroll
+                for (int i = 0; i < Z::kWarpTiles; ++i) store_k<D>(place, i, rk[i]);
+            }
             for_tensor_cores();
             if (lane == 0) gone[j & 1][w] = away;
             __syncwarp();
@@ -537,12 +533,16 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
             for (int i = 0; i < Z::kWarpTiles; ++i) load_k<D>(at[i], g, t, rk[i]);
             if (j > 0) bar_wait(o_done, (j - 1) & 1, &dead);
 #pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) store_v<D>(sv, w * Z::kWarpTiles + i, g, t, rv[i]);
+            for (int i = 0; i < Z::kWarpTiles; ++i) {
+                const int tile = w * Z::kWarpTiles + i, at0 = (tile / 4 * D + g) * 128 + ((tile % 4 * 2 ^ g) << 4) + t * 4;
+                uint8_t* const place[2] = {sv + at0, sv + (at0 ^ 16)};
+                store_v<D>(place, rv[i]);
+            }
             for_tensor_cores();
             __syncwarp();
             if (lane == 0) bar_arrive(v_full);
 #pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i], v.s_kv, valid(j + 1, i), g, t, rv[i]);
+            for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i] ? at[i] + v.s_kv : nullptr, valid(j + 1, i), g, t, rv[i]);
         }
     } else if (lane == 0 && blocks > 0) {
         // ---- matrix instructions ----
