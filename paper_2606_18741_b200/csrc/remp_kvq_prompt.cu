@@ -1,20 +1,21 @@
 // Attention over the 4-bit cache for many queries per sequence (prompts and their chunks), on the tensor cores' own memory.
 //
-// Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 128 rows (tokens x query heads of one KV head) and a
-// range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*back - ref), O += P.V, with a running reference for
-// each row that moves only when the probabilities of 32 keys outgrow kBound.
+// Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
+// matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*back - ref), O += P.V, with a
+// running reference for each row that moves only when the probabilities of 32 keys outgrow kBound.
 // Rounding: q is exact in half after a power of two per row; keys and values s*c + m are rounded to half (a quarter of them,
-// so that every 16-bit input stays finite) and so is P; S, O, sums and references are in 32 bits.
+// so that every 16-bit input up to 262016 stays finite) and so is P; S, O, sums and references are in 32 bits.
 //
-// Bound: tensor cores (4*D flops for each row and key), then issue slots: four warps turn codes into halves, four compute
-// P, one thread issues the matrix instructions; two thread blocks to an SM take turns on the tensor cores. Q, K and V^T lie in
-// shared memory in rows of 128 bytes, 16-byte pieces exchanged within 8 rows (piece ^ (row & 7)); K's codes are stored so
-// that a word gives neighbouring dims and V's words of two tokens give a pair of keys, so each 4-byte store of a warp meets
-// 32 different banks. S and P share their columns of the tensor memory, O has its own.
+// Bound: tensor cores (4*D flops for each row and key), then issue slots and exponentials: eight warps turn codes into halves
+// once for both matrices, eight compute P (a row to a thread), one thread issues the matrix instructions, which run for
+// one matrix while P of the other is made. Q, two blocks of K and two of V^T lie in shared memory in rows of 128 bytes,
+// 16-byte pieces exchanged within 8 rows (piece ^ (row & 7)); K's codes are stored so that a word gives neighbouring dims
+// and V's words of two tokens give a pair of keys, so each 4-byte store of a warp meets 32 different banks. S and P share
+// their columns of the tensor memory, O has its own. With 256 dims O takes so much of it that one matrix of 128 rows and
+// blocks of 64 keys are left.
 //
-// Order: K of the next block is made while P of this one is computed (its place is free once S is complete), V while the
-// next S is. Every wait is on a barrier in shared memory and bounded: a block that gives up sets error bit 4, goes on
-// without waiting, and ends.
+// Every wait is on a barrier in shared memory and bounded: a block that gives up sets error bit 4, goes on without
+// waiting, and ends.
 
 #include "remp_kvq_device.h"
 
@@ -23,7 +24,6 @@ namespace remp {
 namespace {
 
 constexpr int kRowsM = 128;
-constexpr int kSoftmaxWarps = 4, kUnpackWarps = 4, kPromptThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
 constexpr float kUnset = -1e30f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
@@ -31,12 +31,14 @@ constexpr uint32_t kWaitTries = 1u << 18;
 
 template <int D>
 struct Prompt {
-    static constexpr int kKeys = D == 256 ? 64 : 128, kTiles = kKeys / kKvqTile, kWarpTiles = kTiles / kUnpackWarps;
-    static constexpr int kQ = kRowsM * D * 2, kK = kKeys * D * 2, kV = kKeys * D * 2;  // bytes
-    static constexpr int kBytes = kQ + kK + kV + 1024;
-    static constexpr int kColumns = D == 256 ? 512 : 256, kO = kKeys;  // of the tensor memory: S and P from 0, O behind
-    static constexpr int kCtas = D == 256 ? 1 : 2;
-    static constexpr int kPartFloats = kRowsM * (D + 2);
+    static constexpr int kMats = D == 256 ? 1 : 2, kRows = kMats * kRowsM;
+    static constexpr int kKeys = D == 256 ? 64 : 128, kUnpackWarps = kKeys / kKvqTile;  // a tile to a warp
+    static constexpr int kQ = kRowsM * D * 2, kK = kKeys * D * 2, kV = kKeys * D * 2;  // bytes of a matrix, of a block
+    static constexpr int kBytes = kMats * kQ + 2 * (kK + kV) + 1024;
+    // columns of the tensor memory: S and P of each matrix, then O of each
+    static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
+    static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
+    static constexpr int kPartFloats = kRows * (D + 2);
 };
 
 // ---- barriers and tensor memory ----
@@ -63,8 +65,10 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile
 }
 __device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void commit_to(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t leads) {
+    asm volatile("{ .reg .pred q; setp.ne.b32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar),
+                 "r"(leads)
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
     asm volatile(
@@ -93,22 +97,29 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Rows of 128 bytes, 16-byte pieces exchanged within 8 rows: a matrix of 64 halves a row, rows along M or N.
-__device__ __forceinline__ uint64_t operand(uint32_t at) {
-    return (uint64_t)(at >> 4 & 0x3fff) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
-// halves times halves into 32 bits, 128 rows, n columns, both operands along K
-__host__ __device__ constexpr uint32_t shape_of(int n) { return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(kRowsM >> 4) << 24; }
+// Descriptors of operands in rows of 128 bytes (64 halves) along K, 16-byte pieces exchanged within 8 rows: the low word goes
+// by the address, in units of 16 bytes, the high word is the same for all. Halves times halves into 32 bits, 128 rows.
+__device__ __forceinline__ uint32_t operand_low(uint32_t at) { return (at >> 4 & 0x3fff) | 1u << 16; }
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+template <int N>
+constexpr uint32_t kShape = 1u << 4 | (uint32_t)(N >> 3) << 17 | (uint32_t)(kRowsM >> 4) << 24;
 
-__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b),
-                 "r"(shape), "r"((uint32_t)add)
-                 : "memory");
+// The whole warp gets here with the same operands (so they stay in uniform registers); the lane with `leads` issues.
+template <int N>
+__device__ __forceinline__ void mma_smem(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t add, uint32_t leads) {
+    asm volatile(
+        "{ .reg .pred p, q; .reg .b64 a, b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5};"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a_low), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
+        "r"(leads)
+        : "memory");
 }
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b),
-                 "r"(shape), "r"((uint32_t)add)
-                 : "memory");
+template <int N>
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b_low, uint32_t add, uint32_t leads) {
+    asm volatile(
+        "{ .reg .pred p, q; .reg .b64 b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 b, {%2, %5};"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
+        "r"(leads)
+        : "memory");
 }
 __device__ __forceinline__ void for_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -142,7 +153,8 @@ struct PromptArgs {
     float scale_log2;
     int32_t group, q_heads, window, room;
     uint32_t by_group;
-    int32_t row_blocks, splits;  // of a sequence and KV head at most; parts of its keys
+    int32_t row_blocks;        // of a sequence and KV head at most
+    int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
 };
 
 __device__ __forceinline__ int prompt_token(const PromptArgs& a, int row) { return a.by_group ? (int)__umulhi((uint32_t)row, a.by_group) : row; }
@@ -195,10 +207,9 @@ __device__ __forceinline__ void load_v(const uint8_t* tile, int valid, int g, in
     }
 }
 
-// Rows of K, a key each: place[c] is where piece c of this lane's 8 keys' rows begins, for its words of the pieces. i: the
-// tile of the warp's.
+// Rows of K, a key each: place[c] is where piece c of this lane's 8 keys' rows begins, for its words of the pieces.
 template <int D>
-__device__ __forceinline__ void store_k(uint8_t* const (&place)[8], int i, const RawK<D>& r) {
+__device__ __forceinline__ void store_k(uint8_t* const (&place)[8], const RawK<D>& r) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -210,7 +221,7 @@ __device__ __forceinline__ void store_k(uint8_t* const (&place)[8], int i, const
                 uint32_t z[4];
                 four_halves(r.w[h][2 * grp + x], step, low, z);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(place[4 * x + b] + (i * kKvqTile + 8 * h + grp * Prompt<D>::kKeys) * 128) = z[b];
+                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(place[4 * x + b] + (8 * h + grp * Prompt<D>::kKeys) * 128) = z[b];
             }
         }
 }
@@ -235,14 +246,15 @@ __device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D
 }
 
 template <int D, bool BF>
-__global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_kernel(const __grid_constant__ PromptArgs a) {
+__global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(const __grid_constant__ PromptArgs a) {
     using Z = Prompt<D>;
     extern __shared__ uint8_t smem_[];
-    __shared__ __align__(8) uint64_t bars[6];
+    __shared__ __align__(8) uint64_t bars[15];
     __shared__ uint32_t tmem_at;
     __shared__ int dead;
     __shared__ int is_last;
-    __shared__ __align__(4) uint8_t gone[2][kUnpackWarps];  // of a block of keys: bit i, tile i of the warp's is not there
+    constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kUnpackWarps = Z::kUnpackWarps, kRows = Z::kRows;
+    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const KvqView& v = a.v;
@@ -250,33 +262,38 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
 
     // ---- this block's rows and keys ----
     // row blocks from the last to the first: the last sees the most keys
-    int unit = blockIdx.x;
-    const int split = unit % a.splits;
-    unit /= a.splits;
+    const int part_of = (int)blockIdx.x - a.whole, splits = part_of < 0 ? 1 : a.splits, split = part_of < 0 ? 0 : part_of % splits;
+    int unit = part_of < 0 ? (int)blockIdx.x : a.whole + part_of / splits;
     const int head = unit % v.kv_heads;
     unit /= v.kv_heads;
     const int seq = unit % v.num_seqs, block = a.row_blocks - 1 - unit / v.num_seqs;
     const int qs = max(0, v.query_start[seq]), qe = min(v.num_tokens, v.query_start[seq + 1]);
-    const int queries = max(0, qe - qs), rows_all = queries * a.group, row0 = block * kRowsM;
+    const int queries = max(0, qe - qs), rows_all = queries * a.group, row0 = block * kRows;
     if (row0 >= rows_all) return;
-    const int rows = min(kRowsM, rows_all - row0), len_ = v.seq_lens[seq], len = min(max(len_, 0), a.room);
+    const int rows = min(kRows, rows_all - row0), len_ = v.seq_lens[seq], len = min(max(len_, 0), a.room);
     if (len != len_ && tid == 0) kvq_error(v, kErrBadLength);
     const int first_pos = len_ - queries;
     const int low_limit = first_pos + prompt_token(a, row0), high_limit = first_pos + prompt_token(a, row0 + rows - 1);
     const int end = max(0, min(len, high_limit + 1)), begin = min(end, a.window > 0 ? max(0, low_limit - a.window + 1) : 0) / kKvqTile * kKvqTile;
     const int blocks_all = (end - begin + Z::kKeys - 1) / Z::kKeys;
-    const int b0 = (int)((long long)blocks_all * split / a.splits), b1 = (int)((long long)blocks_all * (split + 1) / a.splits);
+    const int b0 = (int)((long long)blocks_all * split / splits), b1 = (int)((long long)blocks_all * (split + 1) / splits);
     const int blocks = b1 - b0, first_key = begin + b0 * Z::kKeys;
 
     uint8_t* smem = smem_ + ((1024u - ((uint32_t)__cvta_generic_to_shared(smem_) & 1023u)) & 1023u);
-    uint8_t *sq = smem, *sk = smem + Z::kQ, *sv = sk + Z::kK;
+    uint8_t *sq = smem, *sk = smem + Z::kMats * Z::kQ, *sv = sk + 2 * Z::kK;
+    // blocks of K and V come and go (two places each); scores, probabilities and outputs of each matrix; queries
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
-    const uint32_t k_full = bar, v_full = bar + 8, s_full = bar + 16, p_full = bar + 24, o_done = bar + 32, q_full = bar + 40;
+    const uint32_t k_full = bar, k_free = bar + 16, v_full = bar + 32, v_free = bar + 48, s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, q_full = bar + 112;
+    const int mats = rows > kRowsM ? 2 : 1;
     if (tid == 0) {
-        bar_init(k_full, kUnpackWarps), bar_init(v_full, kUnpackWarps), bar_init(s_full, 1), bar_init(p_full, kSoftmaxWarps), bar_init(o_done, 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(k_full + 8 * i, kUnpackWarps), bar_init(v_full + 8 * i, kUnpackWarps), bar_init(k_free + 8 * i, 1), bar_init(v_free + 8 * i, 1);
+            bar_init(s_full + 8 * i, 1), bar_init(p_full + 8 * i, 4), bar_init(o_done + 8 * i, 1);
+        }
         bar_init(q_full, kSoftmaxWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead = 0, is_last = 0;
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(gone[i]) = 0;
     }
     if (wid == kSoftmaxWarps + kUnpackWarps) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_at)),
@@ -291,7 +308,8 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
 
     if (wid < kSoftmaxWarps) {
         // ---- P and the output: one row to a thread ----
-        const uint32_t lanes = tmem + ((uint32_t)(wid * 32) << 16);
+        const int mat = wid >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), s_at = lanes + mat * Z::kKeys, o_at = lanes + Z::kO + mat * D;
         const int row = row0 + min(tid, rows - 1), token = prompt_token(a, row), q_head = head * a.group + row - token * a.group;
         const bool real = tid < rows;
         const int limit = min(first_pos + token, len - 1), from = a.window > 0 ? first_pos + token - a.window + 1 : 0;
@@ -318,7 +336,7 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
                     const float2 f = BF ? make_float2(bf_low(w[k]), bf_high(w[k])) : __half22float2(as_half2(w[k]));
                     w[k] = pack2(f.x * up, f.y * up, false);
                 }
-                *reinterpret_cast<uint4*>(sq + (i / 8) * (kRowsM * 128) + tid * 128 + (((i % 8) ^ (tid & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(sq + mat * Z::kQ + (i / 8) * (kRowsM * 128) + (tid & 127) * 128 + (((i % 8) ^ (tid & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
             for_tensor_cores();
             __syncwarp();
@@ -326,24 +344,22 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
         }
         float ref = kUnset, sum = 0.f;
 #pragma unroll 1
-        for (int j = 0; j < blocks; ++j) {
-            bar_wait(s_full, j & 1, &dead);
+        for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
+            bar_wait(s_full + 8 * mat, j & 1, &dead);
             tmem_after();
             const int key0 = first_key + j * Z::kKeys;
-            const uint32_t missing = *reinterpret_cast<const volatile uint32_t*>(gone[j & 1]);
+            const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
             const bool whole = missing == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || key0 > high_limit - a.window);
 #pragma unroll 1
             for (int c = 0; c < Z::kKeys / 32; ++c) {
                 uint32_t s[32];
-                tmem_load32(lanes + 32 * c, s);
+                tmem_load32(s_at + 32 * c, s);
                 if (!whole) {
                     const int last = limit - key0 - 32 * c, first = from - key0 - 32 * c;
                     uint32_t hidden = 0;  // keys of blocks that are not there
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int tile = 2 * c + i;
-                        if (missing >> (tile / Z::kWarpTiles * 8 + tile % Z::kWarpTiles) & 1) hidden |= 0xffffu << (16 * i);
-                    }
+                    for (int i = 0; i < 2; ++i)
+                        if (missing >> (8 * (2 * c + i)) & 1) hidden |= 0xffffu << (16 * i);
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (i > last || i < first || (hidden >> i & 1)) s[i] = 0xff800000u;  // -infinity
@@ -368,48 +384,49 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
                     const float now = part > kBound ? top * back - kStart : ref, fall = exp2_approx(ref - now);
                     ref = now, sum *= fall;
                     if (j > 0) {
-                        bar_wait(o_done, (j - 1) & 1, &dead);
+                        bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead);
                         tmem_after();
 #pragma unroll 1
                         for (int i = 0; i < D; i += 16) {
                             uint32_t o[16];
-                            tmem_load16(lanes + Z::kO + i, o);
+                            tmem_load16(o_at + i, o);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
-                            tmem_store16(lanes + Z::kO + i, o);
+                            tmem_store16(o_at + i, o);
                         }
                     }
                     tmem_stored();
 #pragma unroll 1
                     for (int i = 0; i < c; ++i) {
                         uint32_t x[16];
-                        tmem_load16(lanes + 16 * i, x);
+                        tmem_load16(s_at + 16 * i, x);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) x[k] = as_word(__hmul2(as_half2(x[k]), __float2half2_rn(fall)));
-                        tmem_store16(lanes + 16 * i, x);
+                        tmem_store16(s_at + 16 * i, x);
                     }
                     tmem_stored();
                 }
                 sum += part;
-                tmem_store16(lanes + 16 * c, p);
+                tmem_store16(s_at + 16 * c, p);
             }
             tmem_stored();
             tmem_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full);
+            if (lane == 0) bar_arrive(p_full + 8 * mat);
         }
-        if (blocks > 0) {
-            bar_wait(o_done, (blocks - 1) & 1, &dead);
+        const bool some = blocks > 0 && mat < mats;
+        if (some) {
+            bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead);
             tmem_after();
         }
         uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
-        if (a.splits == 1) {
+        if (splits == 1) {
             const float inv = sum == 0.f ? 0.f : 4.f / sum;
 #pragma unroll 1
             for (int i = 0; i < D; i += 32) {
                 uint32_t o[32];
-                if (blocks > 0) {
-                    tmem_load32(lanes + Z::kO + i, o);
+                if (some) {
+                    tmem_load32(o_at + i, o);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = 0;
@@ -427,49 +444,49 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
         } else {
             // a part: [dim][row], then references and sums; the block that comes last adds the parts up in their order
             float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
-            float* mine = slots + (int64_t)blockIdx.x * Z::kPartFloats;
+            float* mine = slots + (int64_t)part_of * Z::kPartFloats;
 #pragma unroll 1
             for (int i = 0; i < D; i += 32) {
                 uint32_t o[32];
-                if (blocks > 0) {
-                    tmem_load32(lanes + Z::kO + i, o);
+                if (some) {
+                    tmem_load32(o_at + i, o);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = 0;
                 }
 #pragma unroll
-                for (int k = 0; k < 32; ++k) mine[(i + k) * kRowsM + tid] = __uint_as_float(o[k]);
+                for (int k = 0; k < 32; ++k) mine[(i + k) * kRows + tid] = __uint_as_float(o[k]);
             }
-            mine[D * kRowsM + tid] = ref, mine[(D + 1) * kRowsM + tid] = sum;
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            mine[D * kRows + tid] = ref, mine[(D + 1) * kRows + tid] = sum;
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
             if (tid == 0) {
-                uint32_t* counter = reinterpret_cast<uint32_t*>(a.workspace) + blockIdx.x / a.splits;
+                uint32_t* counter = reinterpret_cast<uint32_t*>(a.workspace) + part_of / splits;
                 uint32_t before;
                 asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
-                is_last = before == (uint32_t)a.splits - 1;
+                is_last = before == (uint32_t)splits - 1;
                 if (is_last) *counter = 0;  // ready for the next call
             }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
             if (is_last) {
-                const float* part = slots + (int64_t)(blockIdx.x - split) * Z::kPartFloats;
+                const float* part = slots + (int64_t)(part_of - split) * Z::kPartFloats;
                 float top = kUnset;
 #pragma unroll 4
-                for (int i = 0; i < a.splits; ++i) top = fmaxf(top, __ldcg(part + (int64_t)i * Z::kPartFloats + D * kRowsM + tid));
+                for (int i = 0; i < splits; ++i) top = fmaxf(top, __ldcg(part + (int64_t)i * Z::kPartFloats + D * kRows + tid));
                 float all = 0.f;
 #pragma unroll 4
-                for (int i = 0; i < a.splits; ++i)
-                    all = fmaf(exp2_approx(__ldcg(part + (int64_t)i * Z::kPartFloats + D * kRowsM + tid) - top),
-                               __ldcg(part + (int64_t)i * Z::kPartFloats + (D + 1) * kRowsM + tid), all);
+                for (int i = 0; i < splits; ++i)
+                    all = fmaf(exp2_approx(__ldcg(part + (int64_t)i * Z::kPartFloats + D * kRows + tid) - top),
+                               __ldcg(part + (int64_t)i * Z::kPartFloats + (D + 1) * kRows + tid), all);
                 const float inv = all == 0.f ? 0.f : 4.f / all;
 #pragma unroll 1
                 for (int d = 0; d < D; d += 8) {
                     float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 2
-                    for (int i = 0; i < a.splits; ++i) {
+                    for (int i = 0; i < splits; ++i) {
                         const float* x = part + (int64_t)i * Z::kPartFloats;
-                        const float f = exp2_approx(__ldcg(x + D * kRowsM + tid) - top);
+                        const float f = exp2_approx(__ldcg(x + D * kRows + tid) - top);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) o[k] = fmaf(f, __ldcg(x + (d + k) * kRowsM + tid), o[k]);
+                        for (int k = 0; k < 8; ++k) o[k] = fmaf(f, __ldcg(x + (d + k) * kRows + tid), o[k]);
                     }
                     uint32_t w[4];
 #pragma unroll
@@ -480,99 +497,99 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
             }
         }
     } else if (wid < kSoftmaxWarps + kUnpackWarps) {
-        // ---- keys and values: kWarpTiles tiles of a block to a warp ----
+        // ---- keys and values: a tile of every block to a warp ----
         const int w = wid - kSoftmaxWarps, g = lane >> 2, t = lane & 3;
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
         const uint8_t* slice = v.base + (int64_t)head * v.s_head;
-        RawK<D> rk[Z::kWarpTiles];
-        RawV<D> rv[Z::kWarpTiles];
-        const uint8_t* at[Z::kWarpTiles];
-        const auto find = [&](int j) {  // where the tiles of block j are
-#pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) {
-                const int key = first_key + j * Z::kKeys + (w * Z::kWarpTiles + i) * kKvqTile, tile = key / kKvqTile;
-                at[i] = nullptr;
-                if (j < blocks && key < end) {
-                    const int in_row = tile / v.block_tiles, id = __ldcg(row + in_row);
-                    if ((uint32_t)id < (uint32_t)v.nb) at[i] = slice + (int64_t)id * v.s_block + (tile - in_row * v.block_tiles) * (kKvqTile * kvq_token_bytes(D));
-                    else if (lane == 0) kvq_error(v, kErrBadBlock);
-                }
-            }
+        const int k_at0 = (w * kKvqTile + g) * 128 + (g << 4) + t * 4, v_at0 = (w / 4 * D + g) * 128 + ((w % 4 * 2 ^ g) << 4) + t * 4;
+        RawK<D> rk;
+        RawV<D> rv;
+        const auto find = [&](int j) -> const uint8_t* {  // the warp's tile of block j
+            const int key = first_key + j * Z::kKeys + w * kKvqTile, tile = key / kKvqTile;
+            if (j >= blocks || key >= end) return nullptr;
+            const int in_row = tile / v.block_tiles, id = __ldcg(row + in_row);
+            if ((uint32_t)id < (uint32_t)v.nb) return slice + (int64_t)id * v.s_block + (tile - in_row * v.block_tiles) * (kKvqTile * kvq_token_bytes(D));
+            if (lane == 0) kvq_error(v, kErrBadBlock);
+            return nullptr;
         };
-        const auto absent = [&]() {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) m |= at[i] ? 0u : 1u << i;
-            return (uint8_t)m;
-        };
-        const auto valid = [&](int j, int i) { return len - (first_key + j * Z::kKeys + (w * Z::kWarpTiles + i) * kKvqTile); };
-        find(0);
-        uint8_t away = absent();
-#pragma unroll
-        for (int i = 0; i < Z::kWarpTiles; ++i) load_k<D>(at[i], g, t, rk[i]);
-#pragma unroll
-        for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i] ? at[i] + v.s_kv : nullptr, valid(0, i), g, t, rv[i]);
+        const auto valid = [&](int j) { return len - (first_key + j * Z::kKeys + w * kKvqTile); };
+        const uint8_t* at = find(0);
+        load_k<D>(at, g, t, rk);
+        load_v<D>(at ? at + v.s_kv : nullptr, valid(0), g, t, rv);
 #pragma unroll 1
         for (int j = 0; j < blocks; ++j) {
-            find(j + 1);
-            if (j > 0) bar_wait(s_full, (j - 1) & 1, &dead);
+            const int place_of = j & 1, turn = (j >> 1) & 1;
+            const uint8_t* next = find(j + 1);
+            if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead);
             {
                 uint8_t* place[8];
-                const int at0 = (w * Z::kWarpTiles * kKvqTile + g) * 128 + (g << 4) + t * 4;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) place[c] = sk + (at0 ^ (c << 4));
-#pragma unroll
-                for (int i = 0; i < Z::kWarpTiles; ++i) store_k<D>(place, i, rk[i]);
+                for (int c = 0; c < 8; ++c) place[c] = sk + place_of * Z::kK + (k_at0 ^ (c << 4));
+                store_k<D>(place, rk);
             }
             for_tensor_cores();
-            if (lane == 0) gone[j & 1][w] = away;
+            if (lane == 0) gone[j & 3][w] = at == nullptr;
             __syncwarp();
-            if (lane == 0) bar_arrive(k_full);
-            away = absent();
-#pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) load_k<D>(at[i], g, t, rk[i]);
-            if (j > 0) bar_wait(o_done, (j - 1) & 1, &dead);
-#pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) {
-                const int tile = w * Z::kWarpTiles + i, at0 = (tile / 4 * D + g) * 128 + ((tile % 4 * 2 ^ g) << 4) + t * 4;
-                uint8_t* const place[2] = {sv + at0, sv + (at0 ^ 16)};
-                store_v<D>(place, rv[i]);
+            if (lane == 0) bar_arrive(k_full + 8 * place_of);
+            load_k<D>(next, g, t, rk);
+            if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead);
+            {
+                uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
+                store_v<D>(place, rv);
             }
             for_tensor_cores();
             __syncwarp();
-            if (lane == 0) bar_arrive(v_full);
-#pragma unroll
-            for (int i = 0; i < Z::kWarpTiles; ++i) load_v<D>(at[i] ? at[i] + v.s_kv : nullptr, valid(j + 1, i), g, t, rv[i]);
+            if (lane == 0) bar_arrive(v_full + 8 * place_of);
+            load_v<D>(next ? next + v.s_kv : nullptr, valid(j + 1), g, t, rv);
+            at = next;
         }
-    } else if (lane == 0 && blocks > 0) {
-        // ---- matrix instructions ----
-        const uint32_t q_at = (uint32_t)__cvta_generic_to_shared(sq), k_at = (uint32_t)__cvta_generic_to_shared(sk), v_at = (uint32_t)__cvta_generic_to_shared(sv);
-        const auto scores = [&](int j) {
-            bar_wait(k_full, j & 1, &dead);
-            tmem_after();
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                mma_smem(tmem, operand(q_at + (k / 4) * (kRowsM * 128) + (k % 4) * 32), operand(k_at + (k / 4) * (Z::kKeys * 128) + (k % 4) * 32),
-                         shape_of(Z::kKeys), k > 0);
-            commit_to(s_full);
-        };
+    } else if (blocks > 0) {
+        // ---- matrix instructions: one lane issues them, three wait for what they need at the same time ----
+        const uint32_t leads = lane == 0;
+        const int n = __shfl_sync(0xffffffffu, blocks, 0), live = __shfl_sync(0xffffffffu, mats, 0);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t q_low = operand_low((uint32_t)__cvta_generic_to_shared(sq)), k_low = operand_low((uint32_t)__cvta_generic_to_shared(sk)),
+                       v_low = operand_low((uint32_t)__cvta_generic_to_shared(sv));
         bar_wait(q_full, 0, &dead);
-        scores(0);
 #pragma unroll 1
-        for (int j = 0; j < blocks; ++j) {
-            bar_wait(v_full, j & 1, &dead);
-            bar_wait(p_full, j & 1, &dead);
-            tmem_after();
+        for (int j = -1; j < n; ++j) {
+            // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
+            // the order of issue, so the scores may take the place of the probabilities before them.
+            const uint32_t place = j & 1, next = place ^ 1;
+            const uint32_t v_block = v_low + place * (Z::kV >> 4), k_block = k_low + next * (Z::kK >> 4);
+            const bool values = j >= 0, scores = j + 1 < n;
+            if (lane == 1 ? scores : values)
+                bar_wait(lane == 1 ? k_full + 8 * next : lane == 2 ? v_full + 8 * place : p_full, (lane == 1 ? j + 1 >> 1 : lane == 2 ? j >> 1 : j) & 1, &dead);
+            __syncwarp();
 #pragma unroll
-            for (int k = 0; k < Z::kKeys / 16; ++k)
-                mma_tmem(tmem + Z::kO, tmem + 8 * k, operand(v_at + (k / 4) * (D * 128) + (k % 4) * 32), shape_of(D), j > 0 || k > 0);
-            commit_to(o_done);
-            if (j + 1 < blocks) {
-                bar_wait(o_done, j & 1, &dead);  // the next scores take the place of these probabilities
-                scores(j + 1);
+            for (int mat = 0; mat < Z::kMats; ++mat) {
+                if (mat >= live) break;
+                const uint32_t s = tm + mat * Z::kKeys;
+                if (values) {
+                    if (mat > 0) {
+                        bar_wait(p_full + 8 * mat, j & 1, &dead);
+                        __syncwarp();
+                    }
+                    tmem_after();
+#pragma unroll
+                    for (int k = 0; k < Z::kKeys / 16; ++k)
+                        mma_tmem<D>(tm + Z::kO + mat * D, s + 8 * k, v_block + ((k / 4) * (D * 128) + (k % 4) * 32 >> 4), k ? 1 : j, leads);
+                    commit_to(o_done + 8 * mat, leads);
+                }
+                if (scores) {
+                    if (!values) tmem_after();
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_smem<Z::kKeys>(s, q_low + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
+                                           k_block + ((k / 4) * (Z::kKeys * 128) + (k % 4) * 32 >> 4), k > 0, leads);
+                    commit_to(s_full + 8 * mat, leads);
+                }
             }
+            if (values) commit_to(v_free + 8 * place, leads);
+            if (scores) commit_to(k_free + 8 * next, leads);
         }
-        for (uint32_t i = 0; i < kWaitTries && !bar_try(o_done, (blocks - 1) & 1); ++i) {}  // nothing stays in flight, whatever happened
+        for (int mat = 0; mat < mats; ++mat)  // nothing stays in flight, whatever happened
+            for (uint32_t i = 0; i < kWaitTries && !bar_try(o_done + 8 * mat, (blocks - 1) & 1); ++i) {}
     }
     tmem_before();
     __syncthreads();
@@ -586,14 +603,19 @@ __global__ void __launch_bounds__(kPromptThreads, Prompt<D>::kCtas) kvq_prompt_k
 template <int D>
 cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t stream) {
     using Z = Prompt<D>;
-    a.row_blocks = (max_rows + kRowsM - 1) / kRowsM;
+    a.row_blocks = (max_rows + Z::kRows - 1) / Z::kRows;
     const int64_t units = (int64_t)a.row_blocks * a.v.num_seqs * a.v.kv_heads;
-    // too few units to fill the GPU: each one's keys are split, one part to a thread block
+    // a unit is a thread block's work; those that are left when the others have filled the GPU whole times share it, each
+    // one's keys split (2048 queries over 8191 keys on 148 SMs: 512 units, 68 of them in two parts each)
     constexpr int kParts = (int)((kAttendWorkspace - kAttendCounterBytes) / (Z::kPartFloats * 4));
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min(sms * Z::kCtas, kParts) / units));
-    static_assert(kParts >= 148 * Z::kCtas && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
+    const int places = std::min(sms, kParts);
+    const int64_t rest = units % sms;
+    a.splits = rest ? (int)std::min<int64_t>(16, places / rest) : 1;
+    if (a.splits < 2) a.splits = 1;
+    a.whole = (int)(a.splits > 1 ? units - rest : units);
+    static_assert(kParts >= 148 && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
     if (units > 0x7fffffff / 16) return cudaErrorInvalidConfiguration;
-    return launch_after(bf ? kvq_prompt_kernel<D, true> : kvq_prompt_kernel<D, false>, units * a.splits, kPromptThreads, Z::kBytes, stream, a);
+    return launch_after(bf ? kvq_prompt_kernel<D, true> : kvq_prompt_kernel<D, false>, a.whole + (units - a.whole) * a.splits, Z::kThreads, Z::kBytes, stream, a);
 }
 
 }  // namespace
@@ -601,7 +623,7 @@ cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t s
 cudaError_t launch_prompt(const KvqView& v, const KvqRows& q, const KvqRows& out, float* lse, void* workspace, float scale_log2, int32_t head_dim,
                           int32_t q_heads, int32_t group, uint32_t by_group, int32_t window, int32_t room, bool bf, int sms, int32_t max_rows,
                           cudaStream_t stream) {
-    PromptArgs a{v, q, out, lse, static_cast<uint8_t*>(workspace), scale_log2, group, q_heads, window, room, by_group, 0, 1};
+    PromptArgs a{v, q, out, lse, static_cast<uint8_t*>(workspace), scale_log2, group, q_heads, window, room, by_group, 0, 0, 1};
     return head_dim == 64 ? launch<64>(a, bf, sms, max_rows, stream)
            : head_dim == 128 ? launch<128>(a, bf, sms, max_rows, stream) : launch<256>(a, bf, sms, max_rows, stream);
 }
