@@ -6,10 +6,14 @@
 // and the squares are added neighbours first, so that any program that follows the formula in that order gets the same
 // codes (a contracted multiply-add would move values on the edge between two codes).
 //
-// Bound: HBM (each row is read and written once). A row is held by head_dim/8 lanes, 8 dims (16 bytes) each: the norm is
-// a butterfly over these lanes, a turn's partner dim is in the same lane (interleaved) or one shuffle away, and a group
-// of 64 dims is 8 lanes. A warp takes kRowSets sets of rows of ONE token and issues all their loads before it looks up
-// where the token belongs (two or three dependent loads), so the look-up hides behind them.
+// Bound: HBM (each row is read and written once), and issue slots close behind. A row is held by head_dim/8 lanes, 8 dims (16
+// bytes) each: the norm is a butterfly over these lanes, a turn's partner dim is in the same lane (interleaved) or one
+// shuffle away, and a group of 64 dims is 8 lanes. A warp takes the rows of ONE token, kSets sets at a time: it looks up
+// where the token belongs and loads its cosines and sines once, asks for the next sets' rows as soon as this one's are
+// unpacked, and takes the square roots and reciprocals of all its sets' norms at once. Where tokens are too few to
+// fill the GPU that way, every kSets sets get a warp of their own.
+
+#include <algorithm>
 
 #include "remp_kvq.h"
 #include "remp_launch.h"
@@ -18,8 +22,9 @@ namespace remp {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
+constexpr int kSets = 4;
 
 struct Transform {
     const float* q_norm;
@@ -55,11 +60,12 @@ __device__ __forceinline__ Slot find_slot(const KvqView& v, int token, int tile_
     return r;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& raw, bool bf, float (&x)[8]) {
+template <bool BF>
+__device__ __forceinline__ void unpack8(const uint4& raw, float (&x)[8]) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (bf) {
+        if (BF) {
             x[2 * i] = bf_low(w[i]), x[2 * i + 1] = bf_high(w[i]);
         } else {
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
@@ -68,11 +74,12 @@ __device__ __forceinline__ void unpack8(const uint4& raw, bool bf, float (&x)[8]
     }
 }
 
-__device__ __forceinline__ uint4 pack8(const float (&x)[8], bool bf) {
+template <bool BF>
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (bf) {
+        if (BF) {
             const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
             w[i] = *reinterpret_cast<const uint32_t*>(&h);
         } else {
@@ -102,163 +109,183 @@ __device__ __forceinline__ int word_at(int l, bool is_v) {
     return is_v ? (l & 7) * (D / 16) + (l >> 3) * 4 : (l & 3) * (D / 8) + (l >> 2) * 4;
 }
 
-template <int D, int kRowSets>
+// The code of y = x - minimum in steps: rint of the quotient. The product with the reciprocal is within 2^-19 of it, so only
+// near the middle between two codes (and where the reciprocal of a tiny step is none: `inverse` 0) it has to be divided.
+__device__ __forceinline__ float code_of(float y, float step, float inverse) {
+    const float q = __fmul_rn(y, inverse), r = rintf(q);
+    return fabsf(q - r) > 0.5f - 0x1p-16f || inverse == 0.f ? rintf(__fdiv_rn(y, step)) : r;
+}
+
+// A warp's work: the sets [first, last) of kSets * (rows of a warp) rows of a token.
+template <int D, bool BF>
 __global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, const KvqRows q, const KvqRows k,
                                                               const KvqRows val, const KvqRows q_out,
-                                                              const Transform tr, const int q_heads, const int bf_,
-                                                              const int sets_per_token) {
+                                                              const Transform tr, const int q_heads, const int sets_per_token,
+                                                              const int sets_per_warp) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
-    const bool bf = bf_ != 0;
     grid_wait();
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int token = (int)(item / sets_per_token);
-    if (token >= v.num_tokens) return;
-    const int row0 = (int)(item - (int64_t)token * sets_per_token) * (kRows * kRowSets) + sub;
-    const int rows = q_heads + 2 * v.kv_heads;
+    const int rows = q_heads + 2 * v.kv_heads, shares = (sets_per_token + sets_per_warp - 1) / sets_per_warp;
+    const int64_t all = (int64_t)v.num_tokens * shares, step_of_grid = (int64_t)gridDim.x * kWarps;
+    const auto load = [&](int token, int row) {
+        if (row >= rows) return make_uint4(0, 0, 0, 0);
+        const uint16_t* p = row < q_heads ? q.data + token * q.s_token + row * q.s_head
+                            : row < q_heads + v.kv_heads ? k.data + token * k.s_token + (row - q_heads) * k.s_head
+                                                         : val.data + token * val.s_token + (row - q_heads - v.kv_heads) * val.s_head;
+        return *reinterpret_cast<const uint4*>(p + 8 * l);
+    };
+    const bool any_norm = tr.q_norm || tr.k_norm;
 
-    uint4 raw[kRowSets];
+    for (int64_t share = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); share < all; share += step_of_grid) {
+        const int token = (int)(share / shares), first = (int)(share - (int64_t)token * shares) * sets_per_warp;
+        const int last = min(sets_per_token, first + sets_per_warp);
+        uint4 raw[kSets];
 #pragma unroll
-    for (int u = 0; u < kRowSets; ++u) {
-        const int row = row0 + u * kRows;
-        raw[u] = make_uint4(0, 0, 0, 0);
-        if (row < rows) {
-            const uint16_t* p = row < q_heads ? q.data + token * q.s_token + row * q.s_head
-                                : row < q_heads + v.kv_heads
-                                    ? k.data + token * k.s_token + (row - q_heads) * k.s_head
-                                    : val.data + token * val.s_token + (row - q_heads - v.kv_heads) * val.s_head;
-            raw[u] = *reinterpret_cast<const uint4*>(p + 8 * l);
+        for (int u = 0; u < kSets; ++u) raw[u] = load(token, (first * kSets + u) * kRows + sub);
+
+        const Slot slot = find_slot(v, token, kTileBytes);
+        bool known = slot.known;
+        int turn_row = slot.pos;
+        if (tr.rope && known) {
+            if (tr.positions) turn_row = tr.positions[token];
+            known = turn_row >= 0 && turn_row < tr.rope_rows;
         }
-    }
-
-    const Slot slot = find_slot(v, token, kTileBytes);
-    bool known = slot.known;
-    int turn_row = slot.pos;
-    if (tr.rope && known) {
-        if (tr.positions) turn_row = tr.positions[token];
-        known = turn_row >= 0 && turn_row < tr.rope_rows;
-    }
-    if (!known || !slot.stored) {
-        if (lane == 0) kvq_error(v, known ? kErrBadBlock : kErrBadLength);
-        if (!known) return;
-    }
-
-    // cosines and sines of this lane's dims, the same for every head of the token
-    const int half = tr.rotary_dim / 2;
-    const bool turns = tr.rope && 8 * l < tr.rotary_dim;
-    float cs[8], sn[8];
-    int partner = lane;
-    float sign = 1.f;
-    if (turns) {
-        const float* row = tr.rope + (int64_t)turn_row * tr.rotary_dim;
-        if (tr.interleaved) {
-            const float4 c = *reinterpret_cast<const float4*>(row + 4 * l);
-            const float4 s = *reinterpret_cast<const float4*>(row + half + 4 * l);
-            cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
-        } else {
-            const bool upper = 8 * l >= half;
-            const float* c = row + 8 * l - (upper ? half : 0);
-#pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(c + i), b = *reinterpret_cast<const float4*>(c + half + i);
-                cs[i] = a.x, cs[i + 1] = a.y, cs[i + 2] = a.z, cs[i + 3] = a.w;
-                sn[i] = b.x, sn[i + 1] = b.y, sn[i + 2] = b.z, sn[i + 3] = b.w;
-            }
-            partner = lane + (upper ? -half / 8 : half / 8);
-            sign = upper ? 1.f : -1.f;
-        }
-    }
-
-#pragma unroll
-    for (int u = 0; u < kRowSets; ++u) {
-        const int row = row0 + u * kRows;
-        const bool is_q = row < q_heads, is_v = row >= q_heads + v.kv_heads, real = row < rows;
-        float x[8];
-        unpack8(raw[u], bf, x);
-
-        const float* weight = is_q ? tr.q_norm : is_v ? nullptr : tr.k_norm;
-        if (__any_sync(0xffffffffu, weight != nullptr)) {
-            float q2[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q2[i] = __fmul_rn(x[i], x[i]);
-            float sum = __fadd_rn(__fadd_rn(__fadd_rn(q2[0], q2[1]), __fadd_rn(q2[2], q2[3])),
-                                  __fadd_rn(__fadd_rn(q2[4], q2[5]), __fadd_rn(q2[6], q2[7])));
-#pragma unroll
-            for (int s = 1; s < kLanes; s <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, s));
-            if (weight) {
-                const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.f / D), tr.eps)));
-                const float4 a = *reinterpret_cast<const float4*>(weight + 8 * l);
-                const float4 b = *reinterpret_cast<const float4*>(weight + 8 * l + 4);
-                const float wt[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], r), wt[i]);
-            }
+        if (!known || !slot.stored) {
+            if (lane == 0) kvq_error(v, known ? kErrBadBlock : kErrBadLength);
+            if (!known) continue;
         }
 
-        if (tr.rope) {
+        // cosines and sines of this lane's dims, the same for every head of the token; the sines with the sign of their product
+        const int half = tr.rotary_dim / 2;
+        const bool turns = tr.rope && 8 * l < tr.rotary_dim;
+        float cs[8], sn[8];
+        int partner = lane;
+        if (turns) {
+            const float* row = tr.rope + (int64_t)turn_row * tr.rotary_dim;
             if (tr.interleaved) {
-                if (turns && !is_v) {
+                const float4 c = *reinterpret_cast<const float4*>(row + 4 * l);
+                const float4 s = *reinterpret_cast<const float4*>(row + half + 4 * l);
+                cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
+            } else {
+                const bool upper = 8 * l >= half;
+                const float* c = row + 8 * l - (upper ? half : 0);
+                const float sign = upper ? 1.f : -1.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = x[2 * i], b = x[2 * i + 1];
-                        x[2 * i] = __fsub_rn(__fmul_rn(a, cs[i]), __fmul_rn(b, sn[i]));
-                        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cs[i]), __fmul_rn(a, sn[i]));
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 a = *reinterpret_cast<const float4*>(c + i), b = *reinterpret_cast<const float4*>(c + half + i);
+                    cs[i] = a.x, cs[i + 1] = a.y, cs[i + 2] = a.z, cs[i + 3] = a.w;
+                    sn[i] = b.x * sign, sn[i + 1] = b.y * sign, sn[i + 2] = b.z * sign, sn[i + 3] = b.w * sign;
+                }
+                partner = lane + (upper ? -half / 8 : half / 8);
+            }
+        }
+
+#pragma unroll 1
+        for (int set = first; set < last; ++set) {
+            const int row0 = set * kSets * kRows + sub;
+            float scales = 0.f;  // 1 / root mean square: of set u in the lanes with lane % 4 = u
+            if (any_norm) {
+                float mean = 0.f;
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) {
+                    float x[8];
+                    unpack8<BF>(raw[u], x);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], x[i]);
+                    float sum = __fadd_rn(__fadd_rn(__fadd_rn(x[0], x[1]), __fadd_rn(x[2], x[3])),
+                                          __fadd_rn(__fadd_rn(x[4], x[5]), __fadd_rn(x[6], x[7])));
+#pragma unroll
+                    for (int s = 1; s < kLanes; s <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, s));
+                    if ((lane & 3) == u) mean = sum;
+                }
+                scales = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(mean, 1.f / D), tr.eps)));
+            }
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) {
+                const int row = row0 + u * kRows;
+                const bool is_q = row < q_heads, is_v = row >= q_heads + v.kv_heads, real = row < rows;
+                float x[8];
+                unpack8<BF>(raw[u], x);
+                if (set + 1 < last) raw[u] = load(token, row + kSets * kRows);
+
+                if (any_norm) {
+                    const float r = __shfl_sync(0xffffffffu, scales, (lane & ~3) | u);
+                    const float* weight = is_q ? tr.q_norm : is_v ? nullptr : tr.k_norm;
+                    if (weight) {
+                        const float4 a = *reinterpret_cast<const float4*>(weight + 8 * l);
+                        const float4 b = *reinterpret_cast<const float4*>(weight + 8 * l + 4);
+                        const float wt[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], r), wt[i]);
                     }
                 }
-            } else {
+
+                if (tr.rope && __any_sync(0xffffffffu, !is_v)) {
+                    if (tr.interleaved) {
+                        if (turns && !is_v) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float a = x[2 * i], b = x[2 * i + 1];
+                                x[2 * i] = __fsub_rn(__fmul_rn(a, cs[i]), __fmul_rn(b, sn[i]));
+                                x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cs[i]), __fmul_rn(a, sn[i]));
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float other = __shfl_sync(0xffffffffu, x[i], partner);
+                            if (turns && !is_v) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i]), __fmul_rn(other, sn[i]));
+                        }
+                    }
+                }
+
+                if (is_q)
+                    *reinterpret_cast<uint4*>(q_out.data + token * q_out.s_token + row * q_out.s_head + 8 * l) = pack8<BF>(x);
+                if (!__any_sync(0xffffffffu, real && !is_q)) continue;
+
+                float lo = x[0], hi = x[0];
+                bool odd = false;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float other = __shfl_sync(0xffffffffu, x[i], partner);
-                    if (turns && !is_v) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i]), __fmul_rn(sign, __fmul_rn(other, sn[i])));
+                    lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
+                    odd |= !(fabsf(x[i]) <= 3.402823466e38f);  // NaN or infinity
+                }
+#pragma unroll
+                for (int s = 1; s < 8; s <<= 1) {
+                    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+                    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+                }
+                odd = __ballot_sync(0xffffffffu, odd) & (0xffu << (lane & 24));
+                uint32_t m_bits = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
+                const float m = bf_low(m_bits);
+                const float span = fmaxf(__fmul_rn(__fsub_rn(hi, m), 1.f / 15.f), 0.f);
+                uint32_t s_bits = __bfloat16_as_ushort(__float2bfloat16_ru(fminf(span, 65280.f)));
+                if (odd) m_bits = 0x7fc0u, s_bits = 0;
+                const float step = bf_low(s_bits), inverse = step >= 0x1p-100f ? __frcp_rn(step) : 0.f;
+                uint32_t word = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float c = step > 0.f ? fminf(fmaxf(code_of(__fsub_rn(x[i], m), step, inverse), 0.f), 15.f) : 0.f;
+                    word |= (uint32_t)c << (4 * (is_v ? i : k_place(i)));
+                }
+                const uint32_t of_k = k_transpose(word, lane), of_v = nibble_step(of_k, 4, 0x0000ffffu, lane);
+                if (!is_q && real && slot.stored) {
+                    const int head = is_v ? row - q_heads - v.kv_heads : row - q_heads;
+                    uint8_t* tile = v.base + slot.off + head * v.s_head + (is_v ? v.s_kv : 0);
+                    const int in_tile = slot.pos & 15;
+                    *reinterpret_cast<uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, is_v)) = is_v ? of_v : of_k;
+                    if ((l & 7) == 0)
+                        *reinterpret_cast<uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4) = s_bits | m_bits << 16;
                 }
             }
-        }
-
-        if (is_q)
-            *reinterpret_cast<uint4*>(q_out.data + token * q_out.s_token + row * q_out.s_head + 8 * l) = pack8(x, bf);
-        if (!__any_sync(0xffffffffu, real && !is_q)) continue;
-
-        float lo = x[0], hi = x[0];
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
-            odd |= !(fabsf(x[i]) <= 3.402823466e38f);  // NaN or infinity
-        }
-#pragma unroll
-        for (int s = 1; s < 8; s <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
-        }
-        odd = __ballot_sync(0xffffffffu, odd) & (0xffu << (lane & 24));
-        uint32_t m_bits = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
-        const float m = bf_low(m_bits);
-        const float span = fmaxf(__fmul_rn(__fsub_rn(hi, m), 1.f / 15.f), 0.f);
-        uint32_t s_bits = __bfloat16_as_ushort(__float2bfloat16_ru(fminf(span, 65280.f)));
-        if (odd) m_bits = 0x7fc0u, s_bits = 0;
-        const float step = bf_low(s_bits);
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = step > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], m), step)), 0.f), 15.f) : 0.f;
-            word |= (uint32_t)c << (4 * (is_v ? i : k_place(i)));
-        }
-        const uint32_t of_k = k_transpose(word, lane), of_v = nibble_step(of_k, 4, 0x0000ffffu, lane);
-        if (!is_q && real && slot.stored) {
-            const int head = is_v ? row - q_heads - v.kv_heads : row - q_heads;
-            uint8_t* tile = v.base + slot.off + head * v.s_head + (is_v ? v.s_kv : 0);
-            const int in_tile = slot.pos & 15;
-            *reinterpret_cast<uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, is_v)) = is_v ? of_v : of_k;
-            if ((l & 7) == 0)
-                *reinterpret_cast<uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4) = s_bits | m_bits << 16;
         }
     }
 }
 
-template <int D, int kRowSets>
-__global__ void __launch_bounds__(kThreads) kvq_read_kernel(const KvqView v, const KvqRows k, const KvqRows val,
-                                                            const int bf, const int sets_per_token) {
+template <int D, bool BF>
+__global__ void __launch_bounds__(kThreads) kvq_read_kernel(const KvqView v, const KvqRows k, const KvqRows val, const int sets_per_token) {
+    constexpr int kRowSets = kSets;
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
     grid_begin();
@@ -296,16 +323,14 @@ __global__ void __launch_bounds__(kThreads) kvq_read_kernel(const KvqView v, con
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = __fadd_rn(__fmul_rn((float)((w >> (4 * (is_v ? i : k_place(i)))) & 15), s), m);
-            if (!bf && fabsf(x[i]) > 65504.f) x[i] = copysignf(65504.f, x[i]);  // the span's ends were rounded outwards
+            if (!BF && fabsf(x[i]) > 65504.f) x[i] = copysignf(65504.f, x[i]);  // the span's ends were rounded outwards
         }
         const KvqRows& out = is_v ? val : k;
         if (row < 2 * v.kv_heads && out.data)
             *reinterpret_cast<uint4*>(out.data + token * out.s_token + (is_v ? row - v.kv_heads : row) * out.s_head + 8 * l) =
-                pack8(x, bf);
+                pack8<BF>(x);
     }
 }
-
-constexpr int kAppendSets = 4, kReadSets = 4;
 
 }  // namespace
 
@@ -395,13 +420,21 @@ extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq
     if (remp_status st = kvq_rows(k, pool->kv_heads, d, "k", &rk)) return st;
     if (remp_status st = kvq_rows(v, pool->kv_heads, d, "v", &rv)) return st;
     const int64_t rows = (int64_t)q_heads + 2 * (int64_t)pool->kv_heads;
-    const int per_item = 32 / (d / 8) * kAppendSets;
-    const int64_t sets = (rows + per_item - 1) / per_item, grid = (view.num_tokens * sets + kWarps - 1) / kWarps;
-    if (grid > 0x7fffffffLL || rows > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
-    const auto kernel = d == 64 ? kvq_append_kernel<64, kAppendSets>
-                        : d == 128 ? kvq_append_kernel<128, kAppendSets> : kvq_append_kernel<256, kAppendSets>;
-    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads,
-                           (int)(dtype == REMP_DTYPE_BFLOAT), (int)sets));
+    const int per_set = 32 / (d / 8) * kSets;
+    if (rows > 0x7fffffffLL - per_set) return fail(REMP_ERR_SHAPE, "too many heads");
+    int device = -1, sms = 0;
+    REMP_CUDA(cudaGetDevice(&device));
+    REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    const int sets = (int)((rows + per_set - 1) / per_set), warps = sms * 20;
+    // a token to a warp when that fills the GPU, else a set
+    const int per_warp = view.num_tokens >= warps ? sets : 1;
+    const int64_t shares = (int64_t)view.num_tokens * ((sets + per_warp - 1) / per_warp);
+    const int64_t grid = std::min<int64_t>((shares + kWarps - 1) / kWarps, (int64_t)sms * 40);
+    const bool bf = dtype == REMP_DTYPE_BFLOAT;
+    const auto kernel = d == 64    ? (bf ? kvq_append_kernel<64, true> : kvq_append_kernel<64, false>)
+                        : d == 128 ? (bf ? kvq_append_kernel<128, true> : kvq_append_kernel<128, false>)
+                                   : (bf ? kvq_append_kernel<256, true> : kvq_append_kernel<256, false>);
+    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads, sets, per_warp));
     return REMP_OK;
 }
 
@@ -417,13 +450,14 @@ extern "C" remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_b
         if (remp_status st = kvq_rows(k_out, pool->kv_heads, d, "k_out", &rk)) return st;
     if (v_out)
         if (remp_status st = kvq_rows(v_out, pool->kv_heads, d, "v_out", &rv)) return st;
-    const int per_item = 32 / (d / 8) * kReadSets;
+    const int per_item = 32 / (d / 8) * kSets;
     const int64_t sets = (2 * (int64_t)pool->kv_heads + per_item - 1) / per_item;
     const int64_t grid = (view.num_tokens * sets + kWarps - 1) / kWarps;
     if (grid > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many rows for one call");
-    const auto kernel = d == 64 ? kvq_read_kernel<64, kReadSets>
-                        : d == 128 ? kvq_read_kernel<128, kReadSets> : kvq_read_kernel<256, kReadSets>;
-    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rk, rv, (int)(dtype == REMP_DTYPE_BFLOAT),
-                           (int)sets));
+    const bool bf = dtype == REMP_DTYPE_BFLOAT;
+    const auto kernel = d == 64    ? (bf ? kvq_read_kernel<64, true> : kvq_read_kernel<64, false>)
+                        : d == 128 ? (bf ? kvq_read_kernel<128, true> : kvq_read_kernel<128, false>)
+                                   : (bf ? kvq_read_kernel<256, true> : kvq_read_kernel<256, false>);
+    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rk, rv, (int)sets));
     return REMP_OK;
 }

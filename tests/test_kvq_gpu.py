@@ -165,6 +165,25 @@ def test_append_special_values():
     assert np.abs(got[5] - x[5, 0]).max() <= 65504 * 2.0 ** -8
 
 
+@pytest.mark.parametrize("size", [1e-38, 1e-30, 1e-3, 1.0, 1e30])
+def test_append_codes_on_the_edge(size):
+    # values of few bits: many quotients lie exactly between two codes, and steps of every size
+    rng = np.random.default_rng(11)
+    d, bs, n = 128, 16, 64
+    lens, new, tables, start, batch = _batch([n], [n], bs, 4, rng)
+    x = (rng.integers(-15, 16, (n, 2, d)) * 0.5 * size).astype(np.float32)
+    x[::3] *= rng.choice([1.0, 0.75, 3.0], (len(x[::3]), 1, 1)).astype(np.float32)
+    v = torch.from_numpy(x).bfloat16().cuda()
+    pool = ref.Pool(1, 4, 1, d, bs)
+    buf, dev = _dev_pool(pool)
+    remp.remp_kvq_append(dev, batch, None, v[:, :1], v[:, 1:], None)
+    f = v.float().cpu().numpy()
+    for i in range(n):
+        for kv in (0, 1):
+            pool.write(0, kv, tables[0, i // bs], i, f[i, kv:kv + 1])
+    assert np.array_equal(buf.cpu().numpy(), pool.bytes.reshape(-1))
+
+
 def test_append_and_read_skip_what_is_not_there():
     rng = np.random.default_rng(5)
     d, bs, hk = 64, 16, 2
