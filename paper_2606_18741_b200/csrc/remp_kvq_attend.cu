@@ -29,7 +29,7 @@ namespace {
 constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
-constexpr int kPromptRows = 16;  // rows of a sequence and KV head above which they are a prompt's (remp_kvq_prompt.cu)
+constexpr int kPromptRows = 32;
 constexpr int kStepTiles = 2, kStepTokens = kStepTiles * kKvqTile;
 
 struct AttendArgs {

@@ -27,6 +27,7 @@ constexpr int kRowsM = 128;
 constexpr float kUnset = -1e30f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
+constexpr int kMostSplits = 16;
 constexpr uint32_t kWaitTries = 1u << 18;
 
 template <int D>
@@ -445,8 +446,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             // a part: [dim][row], then references and sums; the block that comes last adds the parts up in their order
             float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
             float* mine = slots + (int64_t)part_of * Z::kPartFloats;
+            const bool rows_here = (tid & ~31) < rows;  // of this warp
 #pragma unroll 1
-            for (int i = 0; i < D; i += 32) {
+            for (int i = 0; i < (rows_here ? D : 0); i += 32) {
                 uint32_t o[32];
                 if (some) {
                     tmem_load32(o_at + i, o);
@@ -468,32 +470,44 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             }
             asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
             if (is_last) {
+                // 32 rows and 16 dims to a warp at a time, four parts' loads in flight
                 const float* part = slots + (int64_t)(part_of - split) * Z::kPartFloats;
-                float top = kUnset;
-#pragma unroll 4
-                for (int i = 0; i < splits; ++i) top = fmaxf(top, __ldcg(part + (int64_t)i * Z::kPartFloats + D * kRows + tid));
-                float all = 0.f;
-#pragma unroll 4
-                for (int i = 0; i < splits; ++i)
-                    all = fmaf(exp2_approx(__ldcg(part + (int64_t)i * Z::kPartFloats + D * kRows + tid) - top),
-                               __ldcg(part + (int64_t)i * Z::kPartFloats + (D + 1) * kRows + tid), all);
-                const float inv = all == 0.f ? 0.f : 4.f / all;
 #pragma unroll 1
-                for (int d = 0; d < D; d += 8) {
-                    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-                    for (int i = 0; i < splits; ++i) {
-                        const float* x = part + (int64_t)i * Z::kPartFloats;
-                        const float f = exp2_approx(__ldcg(x + D * kRows + tid) - top);
+                for (int task = wid; task < (rows + 31) / 32 * (D / 16); task += kSoftmaxWarps) {
+                    const int r = task / (D / 16) * 32 + lane, d = task % (D / 16) * 16;
+                    const int my_row = row0 + min(r, rows - 1), my_token = prompt_token(a, my_row), my_head = head * a.group + my_row - my_token * a.group;
+                    float f[kMostSplits], top = kUnset, all = 0.f;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) o[k] = fmaf(f, __ldcg(x + (d + k) * kRows + tid), o[k]);
+                    for (int i = 0; i < kMostSplits; ++i) f[i] = i < splits ? __ldcg(part + (int64_t)i * Z::kPartFloats + D * kRows + r) : kUnset;
+#pragma unroll
+                    for (int i = 0; i < kMostSplits; ++i) top = fmaxf(top, f[i]);
+#pragma unroll
+                    for (int i = 0; i < kMostSplits; ++i) {
+                        f[i] = exp2_approx(f[i] - top);
+                        if (i < splits) all = fmaf(f[i], __ldcg(part + (int64_t)i * Z::kPartFloats + (D + 1) * kRows + r), all);
                     }
-                    uint32_t w[4];
+                    float o[16];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) w[x] = pack2(o[2 * x] * inv, o[2 * x + 1] * inv, BF);
-                    if (real) *reinterpret_cast<uint4*>(dst + d) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int k = 0; k < 16; ++k) o[k] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kMostSplits; ++i) {
+                        if (i >= splits) break;
+                        const float* x = part + (int64_t)i * Z::kPartFloats + d * kRows + r;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = fmaf(f[i], __ldcg(x + k * kRows), o[k]);
+                    }
+                    const float inv = all == 0.f ? 0.f : 4.f / all;
+                    if (r < rows) {
+                        uint16_t* to = a.out.data + (int64_t)(qs + my_token) * a.out.s_token + (int64_t)my_head * a.out.s_head + d;
+                        uint32_t w[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) w[x] = pack2(o[2 * x] * inv, o[2 * x + 1] * inv, BF);
+                        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                        if (a.lse && d == 0)
+                            a.lse[(int64_t)(qs + my_token) * a.q_heads + my_head] = all == 0.f ? -INFINITY : (top + log2f(all)) * 0.69314718055994531f;
+                    }
                 }
-                if (real && a.lse) a.lse[(int64_t)(qs + token) * a.q_heads + q_head] = all == 0.f ? -INFINITY : (top + log2f(all)) * 0.69314718055994531f;
             }
         }
     } else if (wid < kSoftmaxWarps + kUnpackWarps) {
@@ -610,11 +624,11 @@ cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t s
     constexpr int kParts = (int)((kAttendWorkspace - kAttendCounterBytes) / (Z::kPartFloats * 4));
     const int places = std::min(sms, kParts);
     const int64_t rest = units % sms;
-    a.splits = rest ? (int)std::min<int64_t>(16, places / rest) : 1;
+    a.splits = rest ? (int)std::min<int64_t>(kMostSplits, places / rest) : 1;
     if (a.splits < 2) a.splits = 1;
     a.whole = (int)(a.splits > 1 ? units - rest : units);
     static_assert(kParts >= 148 && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
-    if (units > 0x7fffffff / 16) return cudaErrorInvalidConfiguration;
+    if (units > 0x7fffffff / kMostSplits) return cudaErrorInvalidConfiguration;
     return launch_after(bf ? kvq_prompt_kernel<D, true> : kvq_prompt_kernel<D, false>, a.whole + (units - a.whole) * a.splits, Z::kThreads, Z::kBytes, stream, a);
 }
 

@@ -5,7 +5,7 @@ are one float32 multiply-add, rounded once to 16 bits. Attention: p*step is roun
 codes it meets are at most the row's spread), scores carry the float32 sums of the matrix instructions (a few 2^-20), the
 output is rounded once to its type: |error| <= half an ulp of the output + 2^-10 * sum of p * spread of V's row.
 lse: 2e-5, from float32 sums of scores up to a few tens.
-With more than 16 rows of a sequence and KV head (PROMPT_ROWS), keys, values and probabilities are rounded to half: a value
+With more than 32 rows of a sequence and KV head (PROMPT_ROWS), keys, values and probabilities are rounded to half: a value
 and a probability by 2^-11 of themselves, a score by at most `move` = scale * sum |q||k| * 2^-11, a probability's share by
 twice that: |error| <= half an ulp + (2^-10 + 2 move) * sum of p * largest of V's row; lse: 2e-5 + move.
 """
@@ -20,7 +20,7 @@ from tests import kvq_reference as ref
 
 pytestmark = pytest.mark.gpu
 
-PROMPT_ROWS = 16
+PROMPT_ROWS = 32
 ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 
 
@@ -358,10 +358,11 @@ def test_attend_prompts_query_sizes(q_scale):
     _attend_case(128, 8, 2, 16, torch.bfloat16, [100, 33], [30, 10], q_scale=q_scale, seed=4)
 
 
-def test_attend_prompts_sharp_scores():
+@pytest.mark.parametrize("n", [30, 50])
+def test_attend_prompts_sharp_scores(n):
     # scores that grow along the keys: references move again and again, in the first 32 keys of a block and behind
     rng = np.random.default_rng(0)
-    d, bs, length, n = 64, 16, 400, 30
+    d, bs, length = 64, 16, 400
     lens, new, tables, start, batch = _batch([length], [n], bs, 25, rng)
     pool = ref.Pool(1, 25, 1, d, bs)
     base = rng.standard_normal(d)
