@@ -109,64 +109,149 @@ __device__ __forceinline__ int word_at(int l, bool is_v) {
     return is_v ? (l & 7) * (D / 16) + (l >> 3) * 4 : (l & 3) * (D / 8) + (l >> 2) * 4;
 }
 
-// The code of y = x - minimum in steps: rint of the quotient. The product with the reciprocal is within 2^-19 of it, so only
-// near the middle between two codes (and where the reciprocal of a tiny step is none: `inverse` 0) it has to be divided.
-__device__ __forceinline__ float code_of(float y, float step, float inverse) {
-    const float q = __fmul_rn(y, inverse), r = rintf(q);
-    return fabsf(q - r) > 0.5f - 0x1p-16f || inverse == 0.f ? rintf(__fdiv_rn(y, step)) : r;
+struct Turn {  // cosines and sines of a lane's dims, the sines with the sign of their product; partner lane of pairs half a row apart
+    float cs[8], sn[8];
+    int partner;
+    bool here, interleaved, any;
+};
+
+// Norm (r: 1 / root mean square) and turn of a row's 8 dims in this lane.
+__device__ __forceinline__ void turn_row(float (&x)[8], float r, const float4* weight, const Turn& t) {
+    if (weight) {
+        const float4 a = weight[0], b = weight[1];
+        const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], r), w[i]);
+    }
+    if (!t.any) return;
+    if (t.interleaved) {
+        if (t.here) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = x[2 * i], b = x[2 * i + 1];
+                x[2 * i] = __fsub_rn(__fmul_rn(a, t.cs[i]), __fmul_rn(b, t.sn[i]));
+                x[2 * i + 1] = __fadd_rn(__fmul_rn(b, t.cs[i]), __fmul_rn(a, t.sn[i]));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float other = __shfl_sync(0xffffffffu, x[i], t.partner);
+            if (t.here) x[i] = __fadd_rn(__fmul_rn(x[i], t.cs[i]), __fmul_rn(other, t.sn[i]));
+        }
+    }
 }
 
-// A warp's work: the sets [first, last) of kSets * (rows of a warp) rows of a token.
+// 1 / root mean square of kSets rows at once: of raw[u]'s in the lanes with lane % 4 = u.
 template <int D, bool BF>
-__global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, const KvqRows q, const KvqRows k,
-                                                              const KvqRows val, const KvqRows q_out,
-                                                              const Transform tr, const int q_heads, const int sets_per_token,
-                                                              const int sets_per_warp) {
-    constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
+__device__ __forceinline__ float row_scales(const uint4 (&raw)[kSets], float eps, int lane) {
+    float mean = 0.f;
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        float x[8];
+        unpack8<BF>(raw[u], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], x[i]);
+        float sum = __fadd_rn(__fadd_rn(__fadd_rn(x[0], x[1]), __fadd_rn(x[2], x[3])), __fadd_rn(__fadd_rn(x[4], x[5]), __fadd_rn(x[6], x[7])));
+#pragma unroll
+        for (int s = 1; s < D / 8; s <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, s));
+        if ((lane & 3) == u) mean = sum;
+    }
+    return __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(mean, 1.f / D), eps)));
+}
+
+// A row's codes and parameters to its tile (`tile` null: nowhere).
+template <int D, bool IS_V>
+__device__ __forceinline__ void store_codes(const float (&x)[8], uint8_t* tile, int in_tile, int lane, int l) {
+    float lo = x[0], hi = x[0];
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
+        odd |= !(fabsf(x[i]) <= 3.402823466e38f);  // NaN or infinity
+    }
+#pragma unroll
+    for (int s = 1; s < 8; s <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+    }
+    odd = __ballot_sync(0xffffffffu, odd) & (0xffu << (lane & 24));
+    uint32_t m_bits = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
+    const float m = bf_low(m_bits);
+    const float span = fmaxf(__fmul_rn(__fsub_rn(hi, m), 1.f / 15.f), 0.f);
+    uint32_t s_bits = __bfloat16_as_ushort(__float2bfloat16_ru(fminf(span, 65280.f)));
+    if (odd) m_bits = 0x7fc0u, s_bits = 0;
+    const float step = bf_low(s_bits), inverse = step >= 0x1p-100f ? __frcp_rn(step) : 0.f;
+    float c[8];
+    bool edge = inverse == 0.f;  // some quotient is close to the middle between two codes, or the step is tiny
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float q = __fmul_rn(__fsub_rn(x[i], m), inverse);
+        c[i] = rintf(q), edge |= fabsf(q - c[i]) > 0.5f - 0x1p-16f;
+    }
+    if (edge) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = step > 0.f ? rintf(__fdiv_rn(__fsub_rn(x[i], m), step)) : 0.f;
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) word |= (uint32_t)fminf(fmaxf(c[i], 0.f), 15.f) << (4 * (IS_V ? i : k_place(i)));
+    word = k_transpose(word, lane);
+    if (IS_V) word = nibble_step(word, 4, 0x0000ffffu, lane);
+    if (tile) {
+        *reinterpret_cast<uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, IS_V)) = word;
+        if ((l & 7) == 0) *reinterpret_cast<uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4) = s_bits | m_bits << 16;
+    }
+}
+
+// The work is in groups of kSets sets of rows: a token's groups of query heads, then of K, then of V; a warp takes
+// `per_warp` groups of one token.
+template <int D, bool BF>
+__global__ void __launch_bounds__(kThreads, 5) kvq_append_kernel(const KvqView v, const KvqRows q, const KvqRows k, const KvqRows val,
+                                                              const KvqRows q_out, const Transform tr, const int q_heads,
+                                                              const int q_groups, const int kv_groups, const int per_warp) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kStep = kSets * kRows;  // lanes of a row, rows of a warp, heads of a group
     constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
     grid_wait();
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
-    const int rows = q_heads + 2 * v.kv_heads, shares = (sets_per_token + sets_per_warp - 1) / sets_per_warp;
+    const int groups = q_groups + 2 * kv_groups, shares = (groups + per_warp - 1) / per_warp;
     const int64_t all = (int64_t)v.num_tokens * shares, step_of_grid = (int64_t)gridDim.x * kWarps;
-    const auto load = [&](int token, int row) {
-        if (row >= rows) return make_uint4(0, 0, 0, 0);
-        const uint16_t* p = row < q_heads ? q.data + token * q.s_token + row * q.s_head
-                            : row < q_heads + v.kv_heads ? k.data + token * k.s_token + (row - q_heads) * k.s_head
-                                                         : val.data + token * val.s_token + (row - q_heads - v.kv_heads) * val.s_head;
-        return *reinterpret_cast<const uint4*>(p + 8 * l);
-    };
-    const bool any_norm = tr.q_norm || tr.k_norm;
 
     for (int64_t share = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); share < all; share += step_of_grid) {
-        const int token = (int)(share / shares), first = (int)(share - (int64_t)token * shares) * sets_per_warp;
-        const int last = min(sets_per_token, first + sets_per_warp);
-        uint4 raw[kSets];
+        const int token = (int)(share / shares), first = (int)(share - (int64_t)token * shares) * per_warp;
+        const int last = min(groups, first + per_warp);
+        const auto load = [&](int group, uint4 (&raw)[kSets]) {
+            const bool of_q = group < q_groups, of_v = group >= q_groups + kv_groups;
+            const KvqRows& from = of_q ? q : of_v ? val : k;
+            const int heads = of_q ? q_heads : v.kv_heads, head0 = (of_q ? group : of_v ? group - q_groups - kv_groups : group - q_groups) * kStep + sub;
+            const uint16_t* p = from.data + token * from.s_token + head0 * from.s_head + 8 * l;
+            const int64_t step = kRows * from.s_head;
 #pragma unroll
-        for (int u = 0; u < kSets; ++u) raw[u] = load(token, (first * kSets + u) * kRows + sub);
+            for (int u = 0; u < kSets; ++u) raw[u] = head0 + u * kRows < heads ? *reinterpret_cast<const uint4*>(p + u * step) : make_uint4(0, 0, 0, 0);
+        };
+        uint4 raw[kSets];
+        load(first, raw);
 
         const Slot slot = find_slot(v, token, kTileBytes);
         bool known = slot.known;
-        int turn_row = slot.pos;
+        int rope_row = slot.pos;
         if (tr.rope && known) {
-            if (tr.positions) turn_row = tr.positions[token];
-            known = turn_row >= 0 && turn_row < tr.rope_rows;
+            if (tr.positions) rope_row = tr.positions[token];
+            known = rope_row >= 0 && rope_row < tr.rope_rows;
         }
         if (!known || !slot.stored) {
             if (lane == 0) kvq_error(v, known ? kErrBadBlock : kErrBadLength);
             if (!known) continue;
         }
-
-        // cosines and sines of this lane's dims, the same for every head of the token; the sines with the sign of their product
+        Turn turn;
         const int half = tr.rotary_dim / 2;
-        const bool turns = tr.rope && 8 * l < tr.rotary_dim;
-        float cs[8], sn[8];
-        int partner = lane;
-        if (turns) {
-            const float* row = tr.rope + (int64_t)turn_row * tr.rotary_dim;
+        turn.any = tr.rope != nullptr, turn.here = tr.rope && 8 * l < tr.rotary_dim, turn.interleaved = tr.interleaved, turn.partner = lane;
+        if (turn.here) {
+            const float* row = tr.rope + (int64_t)rope_row * tr.rotary_dim;
             if (tr.interleaved) {
                 const float4 c = *reinterpret_cast<const float4*>(row + 4 * l);
                 const float4 s = *reinterpret_cast<const float4*>(row + half + 4 * l);
-                cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
+                turn.cs[0] = c.x, turn.cs[1] = c.y, turn.cs[2] = c.z, turn.cs[3] = c.w, turn.sn[0] = s.x, turn.sn[1] = s.y, turn.sn[2] = s.z, turn.sn[3] = s.w;
             } else {
                 const bool upper = 8 * l >= half;
                 const float* c = row + 8 * l - (upper ? half : 0);
@@ -174,109 +259,53 @@ __global__ void __launch_bounds__(kThreads) kvq_append_kernel(const KvqView v, c
 #pragma unroll
                 for (int i = 0; i < 8; i += 4) {
                     const float4 a = *reinterpret_cast<const float4*>(c + i), b = *reinterpret_cast<const float4*>(c + half + i);
-                    cs[i] = a.x, cs[i + 1] = a.y, cs[i + 2] = a.z, cs[i + 3] = a.w;
-                    sn[i] = b.x * sign, sn[i + 1] = b.y * sign, sn[i + 2] = b.z * sign, sn[i + 3] = b.w * sign;
+                    turn.cs[i] = a.x, turn.cs[i + 1] = a.y, turn.cs[i + 2] = a.z, turn.cs[i + 3] = a.w;
+                    turn.sn[i] = b.x * sign, turn.sn[i + 1] = b.y * sign, turn.sn[i + 2] = b.z * sign, turn.sn[i + 3] = b.w * sign;
                 }
-                partner = lane + (upper ? -half / 8 : half / 8);
+                turn.partner = lane + (upper ? -half / 8 : half / 8);
             }
         }
+        uint8_t* const tile0 = slot.stored ? v.base + slot.off : nullptr;
+        const int in_tile = slot.pos & 15;
 
 #pragma unroll 1
-        for (int set = first; set < last; ++set) {
-            const int row0 = set * kSets * kRows + sub;
-            float scales = 0.f;  // 1 / root mean square: of set u in the lanes with lane % 4 = u
-            if (any_norm) {
-                float mean = 0.f;
+        for (int group = first; group < last; ++group) {
+            uint4 now[kSets];
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) now[u] = raw[u];
+            if (group + 1 < last) load(group + 1, raw);
+            if (group < q_groups) {
+                const float scales = tr.q_norm ? row_scales<D, BF>(now, tr.eps, lane) : 0.f;
+                const float4* weight = tr.q_norm ? reinterpret_cast<const float4*>(tr.q_norm + 8 * l) : nullptr;
+                const int head0 = group * kStep + sub;
+                uint16_t* p = q_out.data + token * q_out.s_token + head0 * q_out.s_head + 8 * l;
 #pragma unroll
                 for (int u = 0; u < kSets; ++u) {
                     float x[8];
-                    unpack8<BF>(raw[u], x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], x[i]);
-                    float sum = __fadd_rn(__fadd_rn(__fadd_rn(x[0], x[1]), __fadd_rn(x[2], x[3])),
-                                          __fadd_rn(__fadd_rn(x[4], x[5]), __fadd_rn(x[6], x[7])));
-#pragma unroll
-                    for (int s = 1; s < kLanes; s <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, s));
-                    if ((lane & 3) == u) mean = sum;
+                    unpack8<BF>(now[u], x);
+                    turn_row(x, weight ? __shfl_sync(0xffffffffu, scales, (lane & ~3) | u) : 0.f, weight, turn);
+                    if (head0 + u * kRows < q_heads) *reinterpret_cast<uint4*>(p + u * kRows * q_out.s_head) = pack8<BF>(x);
                 }
-                scales = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(mean, 1.f / D), tr.eps)));
-            }
-#pragma unroll
-            for (int u = 0; u < kSets; ++u) {
-                const int row = row0 + u * kRows;
-                const bool is_q = row < q_heads, is_v = row >= q_heads + v.kv_heads, real = row < rows;
-                float x[8];
-                unpack8<BF>(raw[u], x);
-                if (set + 1 < last) raw[u] = load(token, row + kSets * kRows);
-
-                if (any_norm) {
-                    const float r = __shfl_sync(0xffffffffu, scales, (lane & ~3) | u);
-                    const float* weight = is_q ? tr.q_norm : is_v ? nullptr : tr.k_norm;
-                    if (weight) {
-                        const float4 a = *reinterpret_cast<const float4*>(weight + 8 * l);
-                        const float4 b = *reinterpret_cast<const float4*>(weight + 8 * l + 4);
-                        const float wt[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], r), wt[i]);
-                    }
+            } else if (group < q_groups + kv_groups) {
+                const float scales = tr.k_norm ? row_scales<D, BF>(now, tr.eps, lane) : 0.f;
+                const float4* weight = tr.k_norm ? reinterpret_cast<const float4*>(tr.k_norm + 8 * l) : nullptr;
+                const int head0 = (group - q_groups) * kStep + sub;
+#pragma unroll 1
+                for (int u = 0; u < kSets && head0 - sub + u * kRows < v.kv_heads; ++u) {
+                    float x[8];
+                    unpack8<BF>(u == 0 ? now[0] : u == 1 ? now[1] : u == 2 ? now[2] : now[3], x);
+                    turn_row(x, weight ? __shfl_sync(0xffffffffu, scales, (lane & ~3) | u) : 0.f, weight, turn);
+                    const int head = head0 + u * kRows;
+                    store_codes<D, false>(x, tile0 && head < v.kv_heads ? tile0 + head * v.s_head : nullptr, in_tile, lane, l);
                 }
-
-                if (tr.rope && __any_sync(0xffffffffu, !is_v)) {
-                    if (tr.interleaved) {
-                        if (turns && !is_v) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float a = x[2 * i], b = x[2 * i + 1];
-                                x[2 * i] = __fsub_rn(__fmul_rn(a, cs[i]), __fmul_rn(b, sn[i]));
-                                x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cs[i]), __fmul_rn(a, sn[i]));
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float other = __shfl_sync(0xffffffffu, x[i], partner);
-                            if (turns && !is_v) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i]), __fmul_rn(other, sn[i]));
-                        }
-                    }
-                }
-
-                if (is_q)
-                    *reinterpret_cast<uint4*>(q_out.data + token * q_out.s_token + row * q_out.s_head + 8 * l) = pack8<BF>(x);
-                if (!__any_sync(0xffffffffu, real && !is_q)) continue;
-
-                float lo = x[0], hi = x[0];
-                bool odd = false;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]);
-                    odd |= !(fabsf(x[i]) <= 3.402823466e38f);  // NaN or infinity
-                }
-#pragma unroll
-                for (int s = 1; s < 8; s <<= 1) {
-                    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
-                    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
-                }
-                odd = __ballot_sync(0xffffffffu, odd) & (0xffu << (lane & 24));
-                uint32_t m_bits = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
-                const float m = bf_low(m_bits);
-                const float span = fmaxf(__fmul_rn(__fsub_rn(hi, m), 1.f / 15.f), 0.f);
-                uint32_t s_bits = __bfloat16_as_ushort(__float2bfloat16_ru(fminf(span, 65280.f)));
-                if (odd) m_bits = 0x7fc0u, s_bits = 0;
-                const float step = bf_low(s_bits), inverse = step >= 0x1p-100f ? __frcp_rn(step) : 0.f;
-                uint32_t word = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float c = step > 0.f ? fminf(fmaxf(code_of(__fsub_rn(x[i], m), step, inverse), 0.f), 15.f) : 0.f;
-                    word |= (uint32_t)c << (4 * (is_v ? i : k_place(i)));
-                }
-                const uint32_t of_k = k_transpose(word, lane), of_v = nibble_step(of_k, 4, 0x0000ffffu, lane);
-                if (!is_q && real && slot.stored) {
-                    const int head = is_v ? row - q_heads - v.kv_heads : row - q_heads;
-                    uint8_t* tile = v.base + slot.off + head * v.s_head + (is_v ? v.s_kv : 0);
-                    const int in_tile = slot.pos & 15;
-                    *reinterpret_cast<uint32_t*>(tile + in_tile * (D / 2) + word_at<D>(l, is_v)) = is_v ? of_v : of_k;
-                    if ((l & 7) == 0)
-                        *reinterpret_cast<uint32_t*>(tile + kKvqTile * D / 2 + in_tile * (D / 16) + (l >> 3) * 4) = s_bits | m_bits << 16;
+            } else {
+                const int head0 = (group - q_groups - kv_groups) * kStep + sub;
+#pragma unroll 1
+                for (int u = 0; u < kSets && head0 - sub + u * kRows < v.kv_heads; ++u) {
+                    float x[8];
+                    unpack8<BF>(u == 0 ? now[0] : u == 1 ? now[1] : u == 2 ? now[2] : now[3], x);
+                    const int head = head0 + u * kRows;
+                    store_codes<D, true>(x, tile0 && head < v.kv_heads ? tile0 + v.s_kv + head * v.s_head : nullptr, in_tile, lane, l);
                 }
             }
         }
@@ -420,21 +449,22 @@ extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq
     if (remp_status st = kvq_rows(k, pool->kv_heads, d, "k", &rk)) return st;
     if (remp_status st = kvq_rows(v, pool->kv_heads, d, "v", &rv)) return st;
     const int64_t rows = (int64_t)q_heads + 2 * (int64_t)pool->kv_heads;
-    const int per_set = 32 / (d / 8) * kSets;
-    if (rows > 0x7fffffffLL - per_set) return fail(REMP_ERR_SHAPE, "too many heads");
+    const int heads = 32 / (d / 8) * kSets;  // of a group
+    if (rows > 0x7fffffffLL - 3 * heads) return fail(REMP_ERR_SHAPE, "too many heads");
     int device = -1, sms = 0;
     REMP_CUDA(cudaGetDevice(&device));
     REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    const int sets = (int)((rows + per_set - 1) / per_set), warps = sms * 20;
-    // a token to a warp when that fills the GPU, else a set
-    const int per_warp = view.num_tokens >= warps ? sets : 1;
-    const int64_t shares = (int64_t)view.num_tokens * ((sets + per_warp - 1) / per_warp);
+    const int q_groups = (q_heads + heads - 1) / heads, kv_groups = (pool->kv_heads + heads - 1) / heads, groups = q_groups + 2 * kv_groups;
+    // a token to a warp when that fills the GPU, else a group
+    const int per_warp = view.num_tokens >= sms * 20 ? groups : 1;
+    const int64_t shares = (int64_t)view.num_tokens * ((groups + per_warp - 1) / per_warp);
     const int64_t grid = std::min<int64_t>((shares + kWarps - 1) / kWarps, (int64_t)sms * 40);
     const bool bf = dtype == REMP_DTYPE_BFLOAT;
     const auto kernel = d == 64    ? (bf ? kvq_append_kernel<64, true> : kvq_append_kernel<64, false>)
                         : d == 128 ? (bf ? kvq_append_kernel<128, true> : kvq_append_kernel<128, false>)
                                    : (bf ? kvq_append_kernel<256, true> : kvq_append_kernel<256, false>);
-    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads, sets, per_warp));
+    REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads, q_groups, kv_groups,
+                           per_warp));
     return REMP_OK;
 }
 
