@@ -226,7 +226,9 @@ __device__ __forceinline__ void kvq_scores(const uint8_t* codes, const uint8_t* 
 
 // c - 8 (codes at bits 0..3 of each half) or 16 (c - 8) (at bits 4..7), as halves: 1024 + c has the code in its last bits.
 __device__ __forceinline__ uint32_t centred(uint32_t x, bool upper) {
-    const uint32_t y = (x & (upper ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    uint32_t y;  // one instruction takes the bits and sets the others
+    if (upper) asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(y) : "r"(x), "r"(0x64006400u));
+    else asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(0x64006400u));
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), __half2half2(__ushort_as_half(upper ? 0x6480 : 0x6408)));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
