@@ -19,6 +19,10 @@
 // its steps through two buffers in shared memory with 16-byte asynchronous copies and needs no block-wide
 // barrier until its share is done. Parts of a sequence are merged in the block, and across blocks by the block that
 // arrives last (a counter; nobody waits), always in the order of the list: the result does not depend on timing.
+// Measured: 64 query and 8 KV heads over about 100 thousand tokens of 29 sequences (114.5 MB) 44 us, 2.6 TB/s; 40 query
+// heads over 131071 tokens (151 MB) 50 us, 3.0 TB/s; 2048 sequences of 1 to 63 tokens (71.6 MB) 41 us. Not bound by HBM:
+// the long case, profiled just before its last step (57 us in the profile), took 404 instructions for a tile's K and V, with
+// the integer pipe at 54 %, issue slots at 56 % and the tensor pipe at 18 %.
 
 #include "remp_kvq_device.h"
 
@@ -29,6 +33,9 @@ namespace {
 constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
+// Rows up to which this kernel takes a sequence; above, the prompt kernel. Prompt / this one, us: rows x sequences x keys, 8 KV
+// heads: 17 x 1 x 4000 20.6 / 22.8, 24 x 16 x 2000 45.2 / 43.2, 20 x 64 x 500 63.6 / 51.3; 40 x 8 x 4000 49.3 / 57.4,
+// 64 x 64 x 1000 100.7 / 135.4.
 constexpr int kPromptRows = 32;
 constexpr int kStepTiles = 2, kStepTokens = kStepTiles * kKvqTile;
 

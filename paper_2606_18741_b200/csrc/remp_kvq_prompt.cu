@@ -14,6 +14,11 @@
 // their columns of the tensor memory, O has its own. With 256 dims O takes so much of it that one matrix of 128 rows and
 // blocks of 64 keys are left.
 //
+// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 559 to 584 us in different
+// runs: 824 to 860 TFLOP/s, 50 to 53 % of a library product in bf16. Now bound by the chain of one matrix, scores to P to products to the next scores: some 4750 cycles for
+// a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each, which break the chain, took
+// 779 us (both timed with clock reads in the kernel).
+//
 // Every wait is on a barrier in shared memory and bounded: a block that gives up sets error bit 4, goes on without
 // waiting, and ends.
 
