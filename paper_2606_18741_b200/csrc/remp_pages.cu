@@ -7,8 +7,8 @@
 // itself. No block waits for another, and the result is the same in any order.
 //
 // Bound: latency of the launches (tables and counts are a few MB at most), so small inputs take ONE launch of one thread
-// block that walks the chunks, large ones a launch for each step. Measured: fork of 8 children 7.4 us, free and compaction
-// of about 4000 blocks and 128 sequences 13.5 and 17 us. The copy is bound by HBM: 1.05 GB in 166 us, 6.3 TB/s.
+// block that walks the chunks, large ones a launch for each step. Measured: fork of 8 children 7.4 us (profiled);
+// free and compaction of 4096 blocks and 128 sequences of 32 blocks 3.3 and 6.7 us each in a graph. The copy is bound by HBM: 1.05 GB in 166 us, 6.3 TB/s.
 
 #include <algorithm>
 
@@ -20,8 +20,11 @@ namespace {
 
 constexpr int kChunk = 1024;  // blocks of a chunk = threads of a thread block
 
-// One launch up to here (entries: rows to write x table width). Above, the steps spread over the GPU.
-constexpr int64_t kSoloBlocks = 8192, kSoloEntries = 16384, kSoloForks = 1024;
+// One launch up to here (entries: rows to write x table width). Above, the steps spread over the GPU. A call from an idle
+// GPU, one launch / spread, us (free, compact, fork): 600 blocks and 32 x 16 entries 13.3 / 15.4, 13.7 / 20.9, 14.5 / 21.4;
+// 2048 and 64 x 32 13.6 / 15.3, 17.5 / 21.0, 15.9 / 21.2; 4096 and 128 x 32 17.4 / 15.2, 23.9 / 21.0, 18.2 / 21.3; 8192 and
+// 256 x 32 23.7 / 15.3, 32.1 / 21.0, 24.1 / 21.3. In a graph spread wins from 2048 blocks (compact 6.9 / 6.6, at 8192 22.1 / 6.9).
+constexpr int64_t kSoloBlocks = 2048, kSoloEntries = 2048, kSoloForks = 1024;
 
 // Exclusive count of `flag` over the thread block (kChunk threads).
 __device__ __forceinline__ int rank_in_block(bool flag) {
