@@ -409,12 +409,16 @@ remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_batch* batch
  * With at most 32 rows (max_queries * q_heads / kv_heads) keys and values are used as the codes stand for them; with more,
  * they are rounded to half on the way (|x| up to 262016). A NaN in V reaches every row of its sequence that the call computes
  * together with it, also rows whose mask hides it; a NaN in K or in a query only what sees it. 2^30 steps of 32 tokens of
- * a KV head (4 TB of cache) and more are refused on the device (bit 2); a wait that runs out is reported as bit 4.
+ * a KV head (4 TB of cache) and more are refused on the device (bit 2); where a wait runs out the outputs are NaN (bit 4).
  * The result does not depend on the order in which thread blocks run. */
 int64_t remp_kvq_workspace_bytes(void);
 remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
                             const remp_kvq_rows* out, int32_t q_heads, int32_t dtype, float scale, int32_t window,
                             float* lse, void* workspace, void* stream);
+
+/* A test aid, for the whole process: how often a wait of remp_kvq_attend polls its barrier before its thread block gives up (0: never
+ * polls; negative: the built-in limit). A thread block that gives up writes NaN to its outputs and sets error bit 4. */
+void remp_kvq_set_wait_limit(int32_t tries);
 
 /* ---- pages between two switches: fork, free, compact, copy ----
  *

@@ -479,6 +479,12 @@ def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float
                                        workspace.data_ptr(), _stream_ptr(stream)))
 
 
+def remp_kvq_set_wait_limit(tries: int) -> None:
+    """A test aid, for the whole process: polls of a barrier before remp_kvq_attend's thread blocks give up (0: none, negative: the
+    built-in limit). What gave up is NaN, and bit 4 of the batch's error word."""
+    _lib.load().remp_kvq_set_wait_limit(tries)
+
+
 @functools.lru_cache(maxsize=None)
 def _workspace_bytes() -> int:
     return int(_lib.load().remp_kvq_workspace_bytes())

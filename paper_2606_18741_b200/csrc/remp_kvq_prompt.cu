@@ -19,8 +19,11 @@
 // a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each, which break the chain, took
 // 779 us (both timed with clock reads in the kernel).
 //
-// Every wait is on a barrier in shared memory and bounded: a block that gives up sets error bit 4, goes on without
-// waiting, and ends.
+// Every wait is on a barrier in shared memory and bounded. A block that gives up issues no more matrix instructions, goes on
+// without waiting, writes NaN and sets error bit 4. Whatever happens, the issuing warp leaves when everything that it has
+// issued is done and every barrier that it has committed to has been arrived at, so nothing runs on in freed memory.
+
+#include <atomic>
 
 #include "remp_kvq_device.h"
 
@@ -33,7 +36,8 @@ constexpr float kUnset = -1e30f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
 constexpr int kMostSplits = 16;
-constexpr uint32_t kWaitTries = 1u << 18;
+constexpr int32_t kWaitTries = 1 << 18;
+std::atomic<int32_t> g_wait_tries{kWaitTries};  // remp_kvq_set_wait_limit
 
 template <int D>
 struct Prompt {
@@ -62,11 +66,18 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok;
 }
 // Bounded: a wait that runs out marks the block, and nothing in it waits any more.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-    for (uint32_t i = 0; i < kWaitTries; ++i) {
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int32_t tries) {
+    for (int32_t i = 0; i < tries; ++i) {
         if (bar_try(bar, parity)) return;
         if (*dead) return;
     }
+    *dead = 1;
+}
+// The last of `times` commits to a barrier has arrived. Always with the full limit.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t times, volatile int* dead) {
+    if (times == 0) return;
+    for (int32_t i = 0; i < kWaitTries; ++i)
+        if (bar_try(bar, (times - 1) & 1)) return;
     *dead = 1;
 }
 __device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -161,6 +172,7 @@ struct PromptArgs {
     uint32_t by_group;
     int32_t row_blocks;        // of a sequence and KV head at most
     int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
+    int32_t tries;             // of a wait
 };
 
 __device__ __forceinline__ int prompt_token(const PromptArgs& a, int row) { return a.by_group ? (int)__umulhi((uint32_t)row, a.by_group) : row; }
@@ -351,7 +363,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         float ref = kUnset, sum = 0.f;
 #pragma unroll 1
         for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
-            bar_wait(s_full + 8 * mat, j & 1, &dead);
+            bar_wait(s_full + 8 * mat, j & 1, &dead, a.tries);
+            __syncwarp();
             tmem_after();
             const int key0 = first_key + j * Z::kKeys;
             const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
@@ -390,7 +403,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                     const float now = part > kBound ? top * back - kStart : ref, fall = exp2_approx(ref - now);
                     ref = now, sum *= fall;
                     if (j > 0) {
-                        bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead);
+                        bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead, a.tries);
+                        __syncwarp();
                         tmem_after();
 #pragma unroll 1
                         for (int i = 0; i < D; i += 16) {
@@ -422,9 +436,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         }
         const bool some = blocks > 0 && mat < mats;
         if (some) {
-            bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead);
+            bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead, a.tries);
+            __syncwarp();
             tmem_after();
         }
+        // Whoever gave up said so before its next arrival, so no output that went wrong gets here without the mark.
+        if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
         uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
         if (splits == 1) {
             const float inv = sum == 0.f ? 0.f : 4.f / sum;
@@ -539,7 +556,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         for (int j = 0; j < blocks; ++j) {
             const int place_of = j & 1, turn = (j >> 1) & 1;
             const uint8_t* next = find(j + 1);
-            if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead);
+            if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead, a.tries);
             {
                 uint8_t* place[8];
 #pragma unroll
@@ -551,7 +568,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             __syncwarp();
             if (lane == 0) bar_arrive(k_full + 8 * place_of);
             load_k<D>(next, g, t, rk);
-            if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead);
+            if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead, a.tries);
             {
                 uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
                 store_v<D>(place, rv);
@@ -569,31 +586,42 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const uint32_t q_low = operand_low((uint32_t)__cvta_generic_to_shared(sq)), k_low = operand_low((uint32_t)__cvta_generic_to_shared(sk)),
                        v_low = operand_low((uint32_t)__cvta_generic_to_shared(sv));
-        bar_wait(q_full, 0, &dead);
+        const auto given_up = [&] { return __any_sync(0xffffffffu, *static_cast<volatile int*>(&dead)) != 0; };
+        uint32_t scored[2] = {0, 0}, summed[2] = {0, 0}, left_k = 0, left_v = 0;  // commits so far
+        bar_wait(q_full, 0, &dead, a.tries);
+        __syncwarp();
+        bool go = !given_up();
 #pragma unroll 1
-        for (int j = -1; j < n; ++j) {
+        for (int j = -1; go && j < n; ++j) {
             // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
             // the order of issue, so the scores may take the place of the probabilities before them.
             const uint32_t place = j & 1, next = place ^ 1;
             const uint32_t v_block = v_low + place * (Z::kV >> 4), k_block = k_low + next * (Z::kK >> 4);
             const bool values = j >= 0, scores = j + 1 < n;
             if (lane == 1 ? scores : values)
-                bar_wait(lane == 1 ? k_full + 8 * next : lane == 2 ? v_full + 8 * place : p_full, (lane == 1 ? j + 1 >> 1 : lane == 2 ? j >> 1 : j) & 1, &dead);
+                bar_wait(lane == 1 ? k_full + 8 * next : lane == 2 ? v_full + 8 * place : p_full, (lane == 1 ? j + 1 >> 1 : lane == 2 ? j >> 1 : j) & 1, &dead,
+                         a.tries);
             __syncwarp();
+            if (given_up()) break;
 #pragma unroll
             for (int mat = 0; mat < Z::kMats; ++mat) {
                 if (mat >= live) break;
                 const uint32_t s = tm + mat * Z::kKeys;
                 if (values) {
                     if (mat > 0) {
-                        bar_wait(p_full + 8 * mat, j & 1, &dead);
+                        bar_wait(p_full + 8 * mat, j & 1, &dead, a.tries);
                         __syncwarp();
+                        if (given_up()) {
+                            go = false;
+                            break;
+                        }
                     }
                     tmem_after();
 #pragma unroll
                     for (int k = 0; k < Z::kKeys / 16; ++k)
                         mma_tmem<D>(tm + Z::kO + mat * D, s + 8 * k, v_block + ((k / 4) * (D * 128) + (k % 4) * 32 >> 4), k ? 1 : j, leads);
                     commit_to(o_done + 8 * mat, leads);
+                    ++summed[mat];
                 }
                 if (scores) {
                     if (!values) tmem_after();
@@ -602,13 +630,20 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                         mma_smem<Z::kKeys>(s, q_low + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
                                            k_block + ((k / 4) * (Z::kKeys * 128) + (k % 4) * 32 >> 4), k > 0, leads);
                     commit_to(s_full + 8 * mat, leads);
+                    ++scored[mat];
                 }
             }
-            if (values) commit_to(v_free + 8 * place, leads);
-            if (scores) commit_to(k_free + 8 * next, leads);
+            if (go && values) commit_to(v_free + 8 * place, leads), ++left_v;
+            if (go && scores) commit_to(k_free + 8 * next, leads), ++left_k;
         }
-        for (int mat = 0; mat < mats; ++mat)  // nothing stays in flight, whatever happened
-            for (uint32_t i = 0; i < kWaitTries && !bar_try(o_done + 8 * mat, (blocks - 1) & 1); ++i) {}
+        // Nothing stays in flight, whatever happened. A block of keys is issued when its place has been left, so each barrier is
+        // at most one phase behind. Block b is in place b & 1.
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            bar_drain(s_full + 8 * i, scored[i], &dead), bar_drain(o_done + 8 * i, summed[i], &dead);
+            bar_drain(k_free + 8 * i, (left_k + 1 - i) >> 1, &dead), bar_drain(v_free + 8 * i, (left_v + 1 - i) >> 1, &dead);
+        }
+        __syncwarp();
     }
     tmem_before();
     __syncthreads();
@@ -634,6 +669,7 @@ cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t s
     a.whole = (int)(a.splits > 1 ? units - rest : units);
     static_assert(kParts >= 148 && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
     if (units > 0x7fffffff / kMostSplits) return cudaErrorInvalidConfiguration;
+    a.tries = g_wait_tries.load(std::memory_order_relaxed);
     return launch_after(bf ? kvq_prompt_kernel<D, true> : kvq_prompt_kernel<D, false>, a.whole + (units - a.whole) * a.splits, Z::kThreads, Z::kBytes, stream, a);
 }
 
@@ -642,9 +678,13 @@ cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t s
 cudaError_t launch_prompt(const KvqView& v, const KvqRows& q, const KvqRows& out, float* lse, void* workspace, float scale_log2, int32_t head_dim,
                           int32_t q_heads, int32_t group, uint32_t by_group, int32_t window, int32_t room, bool bf, int sms, int32_t max_rows,
                           cudaStream_t stream) {
-    PromptArgs a{v, q, out, lse, static_cast<uint8_t*>(workspace), scale_log2, group, q_heads, window, room, by_group, 0, 0, 1};
+    PromptArgs a{v, q, out, lse, static_cast<uint8_t*>(workspace), scale_log2, group, q_heads, window, room, by_group, 0, 0, 1, kWaitTries};
     return head_dim == 64 ? launch<64>(a, bf, sms, max_rows, stream)
            : head_dim == 128 ? launch<128>(a, bf, sms, max_rows, stream) : launch<256>(a, bf, sms, max_rows, stream);
 }
 
 }  // namespace remp
+
+extern "C" void remp_kvq_set_wait_limit(int32_t tries) {
+    remp::g_wait_tries.store(tries < 0 ? remp::kWaitTries : std::min(tries, remp::kWaitTries), std::memory_order_relaxed);
+}
