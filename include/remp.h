@@ -407,7 +407,7 @@ remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_batch* batch
  *   workspace  DEVICE, remp_kvq_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call
  *              leaves it ready for the next. Calls that may overlap need workspaces of their own.
  * With at most 32 rows (max_queries * q_heads / kv_heads) keys and values are used as the codes stand for them; with more,
- * they are rounded to half on the way (|x| up to 262016). A NaN in V reaches every row of its sequence that the call computes
+ * they are rounded to 11 bits on the way, of any size up to 2^110 (dims below 2^-24 of their token's largest to fewer). A NaN in V reaches every row of its sequence that the call computes
  * together with it, also rows whose mask hides it; a NaN in K or in a query only what sees it. 2^30 steps of 32 tokens of
  * a KV head (4 TB of cache) and more are refused on the device (bit 2); where a wait runs out the outputs are NaN (bit 4).
  * The result does not depend on the order in which thread blocks run. */

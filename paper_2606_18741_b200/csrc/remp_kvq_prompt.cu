@@ -3,8 +3,13 @@
 // Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
 // matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*back - ref), O += P.V, with a
 // running reference for each row that moves only when the probabilities of 32 keys outgrow kBound.
-// Rounding: q is exact in half after a power of two per row; keys and values s*c + m are rounded to half (a quarter of them,
-// so that every 16-bit input up to 262016 stays finite) and so is P; S, O, sums and references are in 32 bits.
+// Rounding: q is exact in half after a power of two per row; keys and values s*c + m are rounded to half and so is P (twice
+// where a reference moves in the middle of its block of keys); S, O, sums and references are in 32 bits.
+// Range: halves hold K/4 and 8 V where every token of a tile has its largest step or minimum in a range that allows it (2^-7 to
+// 2^13, 2^-12 to 2^8). In other tiles each token has a power of two of its own, which brings that to [2^10, 2^11), so that a
+// value is rounded to 11 bits down to 2^-24 of the token's largest. S is multiplied with K's powers; V's go into P, and the
+// reference bounds P with them in it, so a row that sees only tokens of small values is as exact as any other. The sums of P
+// are without them.
 //
 // Bound: tensor cores (4*D flops for each row and key), then issue slots and exponentials: eight warps turn codes into halves
 // once for both matrices, eight compute P (a row to a thread), one thread issues the matrix instructions, which run for
@@ -14,10 +19,11 @@
 // their columns of the tensor memory, O has its own. With 256 dims O takes so much of it that one matrix of 128 rows and
 // blocks of 64 keys are left.
 //
-// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 559 to 584 us in different
-// runs: 824 to 860 TFLOP/s, 50 to 53 % of a library product in bf16. Now bound by the chain of one matrix, scores to P to products to the next scores: some 4750 cycles for
-// a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each, which break the chain, took
-// 779 us (both timed with clock reads in the kernel).
+// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 594 to 607 us in different
+// runs: 792 to 809 TFLOP/s, 48 to 50 % of a library product in bf16. Bound by the chain of one matrix, scores to P to products to
+// the next scores: some 4750 cycles for a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each,
+// which break the chain, took 779 us (both timed with clock reads in the kernel). Where every tile has powers of its own the
+// same call takes 1.21 ms (K's) and 1.75 ms (V's); with them inside the loop that makes P every call took 870 us.
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up issues no more matrix instructions, goes on
 // without waiting, writes NaN and sets error bit 4. Whatever happens, the issuing warp leaves when everything that it has
@@ -35,6 +41,13 @@ constexpr int kRowsM = 128;
 constexpr float kUnset = -1e30f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
+// What K and V are multiplied with to become halves, as powers of two, where all tokens of a tile allow it: the larger of
+// step and minimum is from 2^kLeast to below 2^kMost. Below, steps lose bits as halves, above, 16 times as much is no half.
+// Keys are wide (biases, outliers), values small: K from 2^-7 to 2^13, V from 2^-12 to 2^8.
+constexpr int kUpK = -2, kUpV = 3;
+__host__ __device__ constexpr int least_of(int up) { return -9 - up; }
+__host__ __device__ constexpr int most_of(int up) { return 11 - up; }
+enum : uint8_t { kGone = 1, kOwnK = 2, kOwnV = 4 };  // marks of a tile: not there; K's, V's tokens have powers of their own
 constexpr int kMostSplits = 16;
 constexpr int32_t kWaitTries = 1 << 18;
 std::atomic<int32_t> g_wait_tries{kWaitTries};  // remp_kvq_set_wait_limit
@@ -44,7 +57,9 @@ struct Prompt {
     static constexpr int kMats = D == 256 ? 1 : 2, kRows = kMats * kRowsM;
     static constexpr int kKeys = D == 256 ? 64 : 128, kUnpackWarps = kKeys / kKvqTile;  // a tile to a warp
     static constexpr int kQ = kRowsM * D * 2, kK = kKeys * D * 2, kV = kKeys * D * 2;  // bytes of a matrix, of a block
-    static constexpr int kBytes = kMats * kQ + 2 * (kK + kV) + 1024;
+    static constexpr int kPowers = 4 * 2 * kKeys * 4;  // of K and V, four blocks of keys
+    static constexpr int kApart = kRows * 8;          // a reference and a sum for each row
+    static constexpr int kBytes = kMats * kQ + 2 * (kK + kV) + kPowers + kApart + 1024;
     // columns of the tensor memory: S and P of each matrix, then O of each
     static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
     static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
@@ -225,14 +240,42 @@ __device__ __forceinline__ void load_v(const uint8_t* tile, int valid, int g, in
     }
 }
 
+// The larger of step and minimum of a token's groups, as bits of a bfloat16: a value is at most 16 times as large.
+template <int G>
+__device__ __forceinline__ uint32_t largest_of(const uint32_t (&par)[G]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < G; ++i) most = __vmaxu2(most, par[i] & 0x7fff7fffu);
+    return max(most >> 16, most & 0xffffu);
+}
+template <int UP>
+__device__ __forceinline__ bool out_of_range(uint32_t largest) {
+    constexpr uint32_t kLeast = (uint32_t)(127 + least_of(UP)) << 7, kMost = (uint32_t)(127 + most_of(UP)) << 7;  // as bits of bfloat16
+    return largest != 0 && largest - kLeast >= kMost - kLeast;
+}
+// A token's power of two, over that of all tokens. Groups of NaN and infinity do not count. Of V 2^-78 to 2^103: sums of P
+// without the powers stay inside 32 bits' range.
+template <int UP, int G>
+__device__ __forceinline__ float power_of(const uint32_t (&par)[G]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+        if ((par[i] & 0x7f800000u) != 0x7f800000u) most = max(most, max((par[i] & 0x7fffffffu) >> 16, par[i] & 0x7fffu));
+    return most ? __uint_as_float((uint32_t)(127 + UP + max(-81, min(100, (int)(most >> 7) - 127 - 10))) << 23) : 1.f;
+}
+__host__ __device__ constexpr float two_to(int e) { return e < 0 ? 1.f / (float)(1 << -e) : (float)(1 << e); }
+// What steps and minima are multiplied with: 2^UP / power.
+template <int UP>
+__device__ __forceinline__ float down_of(float power) { return __uint_as_float(((uint32_t)(254 + UP) << 23) - __float_as_uint(power)); }
+
 // Rows of K, a key each: place[c] is where piece c of this lane's 8 keys' rows begins, for its words of the pieces.
 template <int D>
-__device__ __forceinline__ void store_k(uint8_t* const (&place)[8], const RawK<D>& r) {
+__device__ __forceinline__ void store_k(uint8_t* const (&place)[8], const RawK<D>& r, const float (&down)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int grp = 0; grp < D / 64; ++grp) {
-            const float s = bf_low(r.par[h][grp]) * 0.25f, m = bf_high(r.par[h][grp]) * 0.25f;
+            const float s = bf_low(r.par[h][grp]) * down[h], m = bf_high(r.par[h][grp]) * down[h];
             const __half2 step = finite_halves(s, s), low = finite_halves(m, m);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -246,13 +289,14 @@ __device__ __forceinline__ void store_k(uint8_t* const (&place)[8], const RawK<D
 
 // Rows of V^T, a dim each: row 8n + g from `place` on, two keys to a word.
 template <int D>
-__device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D>& r) {
+__device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D>& r, const float (&down)[4]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int grp = 0; grp < D / 64; ++grp) {
             const uint32_t p0 = r.par[2 * h][grp], p1 = r.par[2 * h + 1][grp];
-            const __half2 step = finite_halves(bf_low(p0) * 0.25f, bf_low(p1) * 0.25f), low = finite_halves(bf_high(p0) * 0.25f, bf_high(p1) * 0.25f);
+            const float d0 = down[2 * h], d1 = down[2 * h + 1];
+            const __half2 step = finite_halves(bf_low(p0) * d0, bf_low(p1) * d1), low = finite_halves(bf_high(p0) * d0, bf_high(p1) * d1);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint32_t z[4];
@@ -261,6 +305,48 @@ __device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D
                 for (int b = 0; b < 4; ++b) *reinterpret_cast<uint32_t*>(place[h] + (grp * 64 + 8 * (4 * x + b)) * 128) = z[b];
             }
         }
+}
+
+// Scores of keys whose tokens have powers of their own, as the loop that makes P wants them: multiplied with K's powers, and with
+// the logarithms of V's added (over `back`, which it multiplies with), so that its P has these in it. What the keys add to the
+// sum, which is without V's powers, is kept in `apart`: a reference and a sum of the row. The loop takes 32 keys at a time, so
+// both of their tiles count here when one has the mark. marked: the block's marks; key_powers: K's, V's kKeys behind; last,
+// first: the row's keys, counted in the block.
+template <int D>
+__device__ __forceinline__ void put_powers(uint32_t s_at, unsigned long long marked, const float* key_powers, int last, int first, float back, float2* apart) {
+    constexpr int kTiles = Prompt<D>::kKeys / kKvqTile;
+    const float per = 1.f / back;
+    float2 state = *apart;
+#pragma unroll 1
+    for (int i = 0; i < kTiles; ++i) {
+        const uint32_t mark = (uint32_t)(marked >> (8 * i)) & 0xffu;
+        const bool own_v = marked >> (16 * (i / 2)) & kOwnV * 0x101u;  // of one of the two tiles
+        if (!(mark & kOwnK) && !own_v) continue;
+        uint32_t s[kKvqTile];
+        tmem_load16(s_at + kKvqTile * i, s);
+        const float* const f = key_powers + kKvqTile * i;
+        float top = -INFINITY, now[kKvqTile];
+#pragma unroll
+        for (int k = 0; k < kKvqTile; ++k) {
+            float x = __uint_as_float(s[k]);
+            if (mark & kOwnK) x *= f[k];
+            const int key = kKvqTile * i + k;
+            now[k] = key > last || key < first || (mark & kGone) ? -INFINITY : x * back;
+            top = fmaxf(top, now[k]);
+            if (mark & kOwnV) x = fmaf((float)((int)(__float_as_uint(f[Prompt<D>::kKeys + k]) >> 23) - 127), per, x);
+            s[k] = __float_as_uint(x);
+        }
+        tmem_store16(s_at + kKvqTile * i, s);
+        if (own_v) {
+            top = fmaxf(top, state.x);
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < kKvqTile; ++k) sum += exp2_approx(now[k] - top);
+            state = make_float2(top, fmaf(state.y, exp2_approx(state.x - top), sum));
+        }
+    }
+    tmem_stored();
+    *apart = state;
 }
 
 template <int D, bool BF>
@@ -272,7 +358,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     __shared__ int dead;
     __shared__ int is_last;
     constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kUnpackWarps = Z::kUnpackWarps, kRows = Z::kRows;
-    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there
+    __shared__ __align__(8) uint8_t marks[4][8];  // of the tiles of a block of keys
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const KvqView& v = a.v;
@@ -299,6 +385,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
 
     uint8_t* smem = smem_ + ((1024u - ((uint32_t)__cvta_generic_to_shared(smem_) & 1023u)) & 1023u);
     uint8_t *sq = smem, *sk = smem + Z::kMats * Z::kQ, *sv = sk + 2 * Z::kK;
+    float* const powers = reinterpret_cast<float*>(sv + 2 * Z::kV);  // [block & 3][K, V][key], of tiles with the mark
+    float2* const apart = reinterpret_cast<float2*>(sv + 2 * Z::kV + Z::kPowers);  // see put_powers
     // blocks of K and V come and go (two places each); scores, probabilities and outputs of each matrix; queries
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t k_full = bar, k_free = bar + 16, v_full = bar + 32, v_free = bar + 48, s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, q_full = bar + 112;
@@ -311,7 +399,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         bar_init(q_full, kSoftmaxWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead = 0, is_last = 0;
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(gone[i]) = 0;
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(marks[i]) = 0;
     }
     if (wid == kSoftmaxWarps + kUnpackWarps) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_at)),
@@ -344,7 +432,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             const float top = BF ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
             const int e = most ? max(-120, min(93, 3 - ((int)(__float_as_uint(top) >> 23) - 127))) : 0;
             const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-            back = a.scale_log2 * 4.f * __uint_as_float((uint32_t)(127 - e) << 23);
+            back = a.scale_log2 * two_to(-kUpK) * __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll 4
             for (int i = 0; i < D / 8; ++i) {
                 const uint4 x = reinterpret_cast<const uint4*>(src)[i];
@@ -361,14 +449,17 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             if (lane == 0) bar_arrive(q_full);
         }
         float ref = kUnset, sum = 0.f;
+        apart[tid] = make_float2(kUnset, 0.f);
 #pragma unroll 1
         for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
             bar_wait(s_full + 8 * mat, j & 1, &dead, a.tries);
             __syncwarp();
             tmem_after();
             const int key0 = first_key + j * Z::kKeys;
-            const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
-            const bool whole = missing == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || key0 > high_limit - a.window);
+            const unsigned long long marked = *reinterpret_cast<const volatile unsigned long long*>(marks[j & 3]);
+            const bool whole = (marked & kGone * 0x0101010101010101ull) == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || key0 > high_limit - a.window);
+            if (marked & (kOwnK | kOwnV) * 0x0101010101010101ull)
+                put_powers<D>(s_at, marked, powers + (j & 3) * 2 * Z::kKeys, limit - key0, from - key0, back, apart + tid);
 #pragma unroll 1
             for (int c = 0; c < Z::kKeys / 32; ++c) {
                 uint32_t s[32];
@@ -378,7 +469,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                     uint32_t hidden = 0;  // keys of blocks that are not there
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        if (missing >> (8 * (2 * c + i)) & 1) hidden |= 0xffffu << (16 * i);
+                        if (marked >> (8 * (2 * c + i)) & kGone) hidden |= 0xffffu << (16 * i);
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (i > last || i < first || (hidden >> i & 1)) s[i] = 0xff800000u;  // -infinity
@@ -426,7 +517,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                     }
                     tmem_stored();
                 }
-                sum += part;
+                sum += marked >> (16 * c) & kOwnV * 0x101u ? 0.f : part;
                 tmem_store16(s_at + 16 * c, p);
             }
             tmem_stored();
@@ -440,11 +531,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             __syncwarp();
             tmem_after();
         }
+        if (apart[tid].y != 0.f) sum = fmaf(apart[tid].y, exp2_approx(apart[tid].x - ref), sum);
         // Whoever gave up said so before its next arrival, so no output that went wrong gets here without the mark.
         if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
         uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
         if (splits == 1) {
-            const float inv = sum == 0.f ? 0.f : 4.f / sum;
+            const float inv = sum == 0.f ? 0.f : two_to(-kUpV) / sum;
 #pragma unroll 1
             for (int i = 0; i < D; i += 32) {
                 uint32_t o[32];
@@ -518,7 +610,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
 #pragma unroll
                         for (int k = 0; k < 16; ++k) o[k] = fmaf(f[i], __ldcg(x + k * kRows), o[k]);
                     }
-                    const float inv = all == 0.f ? 0.f : 4.f / all;
+                    const float inv = all == 0.f ? 0.f : two_to(-kUpV) / all;
                     if (r < rows) {
                         uint16_t* to = a.out.data + (int64_t)(qs + my_token) * a.out.s_token + (int64_t)my_head * a.out.s_head + d;
                         uint32_t w[8];
@@ -557,21 +649,46 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             const int place_of = j & 1, turn = (j >> 1) & 1;
             const uint8_t* next = find(j + 1);
             if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+            // tokens of sizes that halves do not hold: powers of two, told to the warps that make P before K is
+            float down_k[2] = {two_to(kUpK), two_to(kUpK)};
+            float* const my_powers = powers + (j & 3) * 2 * Z::kKeys + w * kKvqTile;
+            uint8_t mark = at ? 0 : kGone;
+            if (__any_sync(0xffffffffu, at && (out_of_range<kUpK>(largest_of(rk.par[0])) || out_of_range<kUpK>(largest_of(rk.par[1]))))) {
+                mark |= kOwnK;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float f = power_of<kUpK>(rk.par[h]);
+                    down_k[h] = down_of<kUpK>(f);
+                    if (t == 0) my_powers[g + 8 * h] = f;
+                }
+            }
             {
                 uint8_t* place[8];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) place[c] = sk + place_of * Z::kK + (k_at0 ^ (c << 4));
-                store_k<D>(place, rk);
+                store_k<D>(place, rk, down_k);
             }
             for_tensor_cores();
-            if (lane == 0) gone[j & 3][w] = at == nullptr;
+            if (__any_sync(0xffffffffu, out_of_range<kUpV>(largest_of(rv.par[0])) || out_of_range<kUpV>(largest_of(rv.par[1])) || out_of_range<kUpV>(largest_of(rv.par[2])) ||
+                                            out_of_range<kUpV>(largest_of(rv.par[3])))) {
+                mark |= kOwnV;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (g == 0) my_powers[Z::kKeys + 2 * t + (i & 1) + (i >> 1) * 8] = power_of<kUpV>(rv.par[i]);
+            }
+            if (lane == 0) marks[j & 3][w] = mark;
             __syncwarp();
             if (lane == 0) bar_arrive(k_full + 8 * place_of);
             load_k<D>(next, g, t, rk);
             if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+            float down_v[4] = {two_to(kUpV), two_to(kUpV), two_to(kUpV), two_to(kUpV)};
+            if (mark & kOwnV) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) down_v[i] = down_of<kUpV>(power_of<kUpV>(rv.par[i]));
+            }
             {
                 uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
-                store_v<D>(place, rv);
+                store_v<D>(place, rv, down_v);
             }
             for_tensor_cores();
             __syncwarp();

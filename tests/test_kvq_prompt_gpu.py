@@ -49,3 +49,73 @@ def test_a_wait_that_runs_out_gives_nan_and_is_reported(wait_limit, d, hq, hk, l
     error.zero_()
     remp.remp_kvq_attend(pool, batch, q, again, d ** -0.5, ws)
     assert torch.equal(again, want) and int(error) == 0
+
+
+# ---- the range of the numbers ----
+
+def _sized(blocks, heads, d, bs, rng, k_size, v_size):
+    """A pool whose tokens have K and V of the given sizes (numbers, or arrays [blocks][bs] for each slot)."""
+    p = base.ref.Pool(1, blocks, heads, d, bs)
+    for kv, size in enumerate((k_size, v_size)):
+        size = np.broadcast_to(np.asarray(size, dtype=np.float32), (blocks, bs)).reshape(blocks, 1, bs // 16, 16, 1)
+        c, s, m = base.ref.quantise(rng.standard_normal((blocks, heads, bs // 16, 16, d)).astype(np.float32) * size)
+        c = c[..., base.ref.place_of(d, kv == 1)]
+        b = (c[..., 0::2] | c[..., 1::2] << 4).reshape(blocks, heads, bs // 16, -1)
+        p.bytes[0, kv] = np.concatenate([b, np.stack([s, m], -1).reshape(blocks, heads, bs // 16, -1).view(np.uint8)], -1)
+    return p
+
+
+def _check_range(out, lse, q, pool, lens, new, tables, scale):
+    """As base._check, with nothing that does not shrink with the values: half an ulp of the output, what rounding
+    probabilities and values to 11 bits does to sums of p * (largest of V's row), and what rounding keys does to scores."""
+    at = 0
+    for s in range(len(lens)):
+        n, length = int(new[s]), int(lens[s])
+        k, v = (pool.rows(0, kv, tables[s], length) for kv in (0, 1))
+        want, want_lse, _, size, move = base.ref.attend(q[at:at + n].double().cpu().numpy(), k, v, length - n, scale, 0)
+        tol = base.ULP[out.dtype] / 2 * np.abs(want) + ((2.0 ** -10 + 2 * move) * size)[..., None]
+        err = np.abs(out[at:at + n].double().cpu().numpy() - want)
+        assert (err <= tol).all(), (s, (err / tol).max())
+        assert (np.abs(lse[at:at + n].double().cpu().numpy() - want_lse) <= 2e-5 * np.maximum(1, np.abs(want_lse)) + move).all()
+        at += n
+
+
+def _range_case(d, hq, hk, lens, new, k_size, v_size, q_size, score=1.0, seed=0, per_token=None):
+    rng = np.random.default_rng(seed)
+    blocks = int((-(-np.asarray(lens) // 16)).sum())
+    lens, new, tables, start, batch = base._batch(lens, new, 16, blocks, rng)
+    if per_token:
+        k_size, v_size = (x * 10.0 ** rng.uniform(*per_token[i], (blocks, 16)) for i, x in enumerate((k_size, v_size)))
+    pool = _sized(blocks, hk, d, 16, rng, k_size, v_size)
+    buf, dev = base._dev_pool(pool)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    q = (torch.randn(int(start[-1]), hq, d, device="cuda", generator=gen) * q_size).bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    scale = score * d ** -0.5
+    remp.remp_kvq_attend(dev, batch, q, out, scale, remp.make_kvq_workspace(), lse=lse)
+    _check_range(out, lse, q, pool, lens, new, tables, scale)
+
+
+# prompts of more than 32 rows: one matrix, two matrices, keys in parts
+PROMPTS = [(64, 2, 1, [70, 150], [70, 33]), (128, 4, 1, [200, 40], [80, 20]), (256, 1, 1, [60, 130], [60, 40])]
+
+
+@pytest.mark.parametrize("size", [1e-3, 1e-5, 1e-7, 1e-12, 1e-25, 1e7, 1e20])
+@pytest.mark.parametrize("d,hq,hk,lens,new", PROMPTS)
+def test_prompt_values_of_any_size(d, hq, hk, lens, new, size):
+    _range_case(d, hq, hk, lens, new, 1.0, size, 1.0, seed=d)
+
+
+@pytest.mark.parametrize("size", [1e-3, 1e-5, 1e-7, 1e-12, 1e7, 1e12])
+@pytest.mark.parametrize("d,hq,hk,lens,new", PROMPTS)
+def test_prompt_keys_of_any_size(d, hq, hk, lens, new, size):
+    _range_case(d, hq, hk, lens, new, size, 1.0, 1 / size, seed=d + 1)
+
+
+@pytest.mark.parametrize("d,hq,hk,lens,new", PROMPTS)
+def test_prompt_tokens_of_different_sizes(d, hq, hk, lens, new):
+    # a row that sees only small values is as exact as one that sees large ones
+    _range_case(d, hq, hk, lens, new, 1.0, 1.0, 1.0, seed=d + 2, per_token=((-3, 0.5), (-9, 6)))
+    _range_case(d, hq, hk, lens, new, 1.0, 1.0, 1.0, seed=d + 3, per_token=((-3, -1), (-5, -2)))  # around where the kernel changes its way
+    _range_case(d, hq, hk, lens, new, 1.0, 1.0, 1.0, seed=d + 5, per_token=((0, 0), (1, 4)))
+    _range_case(d, hq, hk, lens, new, 1e-2, 1.0, 100.0, seed=d + 4, per_token=((-1.5, 0.5), (3, 6)))
