@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
         int limit[NT][2];  // positions of columns 2t, 2t+1
         float o[NT][D / 16][4], ref[NT][2], sum[NT][2], low[NT][G][2];
         float top_step = kTopStep, bound = 0x1p25f;  // p * top_step <= 2^15: p <= bound
+        uint32_t lift = 0;                       // columns whose scores take the 2^20 that `back` does not hold, bit 2n + e
         bool fresh = true;                       // the next step is the first of its unit here
 
 #pragma unroll 1
@@ -339,8 +340,10 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     kvq_make_queries<D>(BF, t, qf[n], qsum[n], back[n], a.scale_log2);
+                    lift = n ? lift : 0;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
+                        if (back[n][e] < 0.f) lift |= 1u << (2 * n + e), back[n][e] = -back[n][e];
                         limit[n][e] = wq.first_pos + token_of(a, row0 + min(8 * n + 2 * t + e, rows - 1));
                         ref[n][e] = kNoRef, sum[n][e] = 0.f;
 #pragma unroll
@@ -359,6 +362,15 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
             for (int j = 0; j < kStepTiles; ++j) {
                 kvq_scores<D, NT>(buf + S::kK + j * S::kCodes, buf + S::kParK + j * S::kParams, g, t, qf, qsum, s[j]);
                 kvq_params<D>(buf + S::kParV + j * S::kParams, g, par[j]);
+            }
+            if (__any_sync(0xffffffffu, lift != 0)) {
+#pragma unroll
+                for (int j = 0; j < kStepTiles; ++j)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (lift >> (2 * n + (e & 1)) & 1) s[j][n][e] *= 1048576.f;
             }
             if (missing || key0 + kStepTokens > wq.len || key0 + kStepTokens - 1 > wq.first_pos || a.window > 0) {
                 // what a row does not see gets -infinity; the steps and minima of tokens that are not there, 0

@@ -116,8 +116,10 @@ __device__ __forceinline__ void kvq_load_queries(const uint16_t* src, bool real,
 
 // Makes them the operand columns, in halves. Slots 0..7 of each 16 dims are taken 16-fold: they meet codes at bits 0..3, the
 // others codes at bits 4..7. A power of two brings the row's largest value to [8, 16), so that halves hold 16-bit
-// queries of any size exactly (down to 2^-28 of the largest). qsum: what codes of 1 in every dim would score in each
+// queries of any size from 2^-117 on exactly (down to 2^-28 of the largest). qsum: what codes of 1 in every dim would score in each
 // group (the sums of the queries, in the units of a score); back: what a score is multiplied with; both for columns 2t and 2t+1.
+// Rows of very large queries (2^115 at a scale of 128^-0.5) have a negative `back`: its 2^20 does not fit into it, and the
+// scores have to take it before they meet -back.
 template <int D>
 __device__ __forceinline__ void kvq_make_queries(bool bf, int t, uint32_t (&qf)[D / 16][2], float (&qsum)[D / kKvqGroup][2],
                                                  float (&back)[2], float scale_log2) {
@@ -130,11 +132,12 @@ __device__ __forceinline__ void kvq_make_queries(bool bf, int t, uint32_t (&qf)[
     most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 2));
     most = max(most >> 16, most & 0xffffu);
     const float top = bf ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
-    // 2^e with top * 2^e in [8, 16); rows of 0 and rows beyond 2^123 or below 2^-90 keep a bounded exponent
+    // 2^e with top * 2^e in [8, 16); rows of 0 and rows beyond 2^123 or below 2^-117 keep a bounded exponent
     const int exponent = (int)(__float_as_uint(top) >> 23) - 127;
-    const int e = most ? max(-120, min(93, 3 - exponent)) : 0;
+    const int e = most ? max(-120, min(120, 3 - exponent)) : 0;
     const float up = __uint_as_float((uint32_t)(127 + e) << 23), up16 = 16.f * up;
-    const float down = scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23) * 1048576.f;  // codes counted 2^-20
+    const float plain = scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), lifted = plain * 1048576.f;  // codes counted 2^-20
+    const float down = lifted <= 3.402823466e38f ? fmaxf(lifted, 1.2e-38f) : -plain;
     float sums[D / kKvqGroup];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)

@@ -253,15 +253,15 @@ __device__ __forceinline__ bool out_of_range(uint32_t largest) {
     constexpr uint32_t kLeast = (uint32_t)(127 + least_of(UP)) << 7, kMost = (uint32_t)(127 + most_of(UP)) << 7;  // as bits of bfloat16
     return largest != 0 && largest - kLeast >= kMost - kLeast;
 }
-// A token's power of two, over that of all tokens. Groups of NaN and infinity do not count. Of V 2^-78 to 2^103: sums of P
-// without the powers stay inside 32 bits' range.
+// A token's power of two, over that of all tokens. Groups of NaN and infinity do not count. Of V 2^-78 to 2^103, so that sums
+// of P without the powers stay inside 32 bits' range; of K 2^-114 to 2^110.
 template <int UP, int G>
 __device__ __forceinline__ float power_of(const uint32_t (&par)[G]) {
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < G; ++i)
         if ((par[i] & 0x7f800000u) != 0x7f800000u) most = max(most, max((par[i] & 0x7fffffffu) >> 16, par[i] & 0x7fffu));
-    return most ? __uint_as_float((uint32_t)(127 + UP + max(-81, min(100, (int)(most >> 7) - 127 - 10))) << 23) : 1.f;
+    return most ? __uint_as_float((uint32_t)(127 + UP + max(UP == kUpV ? -81 : -112, min(UP == kUpV ? 100 : 112, (int)(most >> 7) - 127 - 10))) << 23) : 1.f;
 }
 __host__ __device__ constexpr float two_to(int e) { return e < 0 ? 1.f / (float)(1 << -e) : (float)(1 << e); }
 // What steps and minima are multiplied with: 2^UP / power.
@@ -430,9 +430,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             }
             most = max(most >> 16, most & 0xffffu);
             const float top = BF ? __uint_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
-            const int e = most ? max(-120, min(93, 3 - ((int)(__float_as_uint(top) >> 23) - 127))) : 0;
+            const int e = most ? max(-120, min(110, 3 - ((int)(__float_as_uint(top) >> 23) - 127))) : 0;
             const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-            back = a.scale_log2 * two_to(-kUpK) * __uint_as_float((uint32_t)(127 - e) << 23);
+            back = fmaxf(a.scale_log2 * two_to(-kUpK) * __uint_as_float((uint32_t)(127 - e) << 23), 1.2e-38f);
 #pragma unroll 4
             for (int i = 0; i < D / 8; ++i) {
                 const uint4 x = reinterpret_cast<const uint4*>(src)[i];
