@@ -30,7 +30,7 @@ namespace remp {
 
 namespace {
 
-constexpr float kNoRef = -1e30f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
+constexpr float kNoRef = -3e38f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
 // Rows up to which this kernel takes a sequence; above, the prompt kernel. Prompt / this one, us: rows x sequences x keys, 8 KV

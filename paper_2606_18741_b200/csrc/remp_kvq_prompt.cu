@@ -38,7 +38,7 @@ namespace remp {
 namespace {
 
 constexpr int kRowsM = 128;
-constexpr float kUnset = -1e30f;     // reference of a row that has seen nothing
+constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
 // What K and V are multiplied with to become halves, as powers of two, where all tokens of a tile allow it: the larger of

@@ -1,7 +1,11 @@
 """Attention over the 4-bit cache at the ends of the numbers' range, for one query token (up to 32 rows of a sequence and KV head) and
 for prompts. Tolerances are test_kvq_prompt_gpu's, none of them absolute."""
+import numpy as np
 import pytest
+import torch
 
+import paper_2606_18741_b200 as remp
+from tests import test_kvq_gpu as base
 from tests import test_kvq_prompt_gpu as prompt
 
 pytestmark = pytest.mark.gpu
@@ -14,3 +18,25 @@ SHAPES = [(64, 2, 1, [70, 33], [1, 1]), (128, 8, 2, [200, 40], [1, 1]), (128, 10
 @pytest.mark.parametrize("d,hq,hk,lens,new", SHAPES)
 def test_queries_and_keys_of_opposite_sizes(d, hq, hk, lens, new, size):
     prompt._range_case(d, hq, hk, lens, new, 1 / size, 1.0, size, seed=d + hq)
+
+
+@pytest.mark.parametrize("size", [1e31, 1e35])
+@pytest.mark.parametrize("d,n", [(64, 1), (128, 1), (128, 40), (256, 33)])
+def test_scores_that_are_all_very_low(d, n, size):
+    # far apart too: the highest takes it all
+    rng = np.random.default_rng(d)
+    lens, new, tables, start, batch = base._batch([100], [n], 16, 7, rng)
+    pool = base._filled(7, 1, d, 16, rng)
+    key = size / d / 1024 * 2.0 ** rng.permutation(np.arange(100) % 7)
+    for p in range(100):
+        pool.write(0, 0, tables[0, p // 16], p, np.full((1, d), -2.0 ** np.round(np.log2(key[p])), dtype=np.float32))
+    buf, dev = base._dev_pool(pool)
+    q = torch.full((n, 1, d), 1024.0, device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(n, 1, device="cuda")
+    remp.remp_kvq_attend(dev, batch, q, out, 1.0, remp.make_kvq_workspace(), lse=lse)
+    k, v = (pool.rows(0, kv, tables[0], 100) for kv in (0, 1))
+    want, want_lse, _, size, _ = base.ref.attend(q.double().cpu().numpy(), k, v, 100 - n, 1.0, 0)
+    assert (want_lse < -1e30).all()
+    err = np.abs(out.double().cpu().numpy() - want)
+    assert (err <= 2.0 ** -9 * np.abs(want) + 2.0 ** -10 * size[..., None]).all()
+    assert (np.abs(lse.double().cpu().numpy() - want_lse) <= 2e-5 * np.abs(want_lse)).all()
