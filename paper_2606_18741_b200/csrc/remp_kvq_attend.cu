@@ -32,7 +32,9 @@ namespace {
 
 constexpr float kNoRef = -3e38f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
-constexpr float kTopStep = 1.f / 1024;  // steps below this are not looked at
+// Steps below this are not looked at: p stays at or below 2^45, so that p*m of groups without a step (m up to 2^60 and more) and
+// their sums fit, and p*s of steps down to 2^-50 keeps its bits.
+constexpr float kTopStep = 0x1p-30f, kTopBound = 0x1p45f;
 // Rows up to which this kernel takes a sequence; above, the prompt kernel. Prompt / this one, us: rows x sequences x keys, 8 KV
 // heads: 17 x 1 x 4000 20.6 / 22.8, 24 x 16 x 2000 45.2 / 43.2, 20 x 64 x 500 63.6 / 51.3; 40 x 8 x 4000 49.3 / 57.4,
 // 64 x 64 x 1000 100.7 / 135.4.
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
         float qsum[NT][G][2], back[NT][2];
         int limit[NT][2];  // positions of columns 2t, 2t+1
         float o[NT][D / 16][4], ref[NT][2], sum[NT][2], low[NT][G][2];
-        float top_step = kTopStep, bound = 0x1p25f;  // p * top_step <= 2^15: p <= bound
+        float top_step = kTopStep, bound = kTopBound;  // p * top_step <= 2^15: p <= bound
         uint32_t lift = 0;                       // columns whose scores take the 2^20 that `back` does not hold, bit 2n + e
         bool fresh = true;                       // the next step is the first of its unit here
 
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) o[n][j][0] = o[n][j][1] = o[n][j][2] = o[n][j][3] = 0.f;
                 }
-                top_step = kTopStep, bound = 0x1p25f, fresh = false;
+                top_step = kTopStep, bound = kTopBound, fresh = false;
             }
             const uint8_t* buf = ring + ((i - 1) & 1) * Z::kBuffer;
             const int key0 = (wq.tile0 + w_step * kStepTiles) * kKvqTile;

@@ -40,3 +40,24 @@ def test_scores_that_are_all_very_low(d, n, size):
     err = np.abs(out.double().cpu().numpy() - want)
     assert (err <= 2.0 ** -9 * np.abs(want) + 2.0 ** -10 * size[..., None]).all()
     assert (np.abs(lse.double().cpu().numpy() - want_lse) <= 2e-5 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("size", [1e-5, 1e-10, 1e-12, 1e-14, 1e7, 1e18])
+@pytest.mark.parametrize("d,hq,hk,lens,new", SHAPES)
+def test_values_of_any_size(d, hq, hk, lens, new, size):
+    prompt._range_case(d, hq, hk, lens, new, 1.0, size, 1.0, seed=d + hq)
+
+
+def test_values_without_a_step():
+    # groups of one value: the step is 0, and only the minimum counts
+    rng = np.random.default_rng(1)
+    lens, new, tables, start, batch = base._batch([300], [1], 16, 19, rng)
+    for size in (2.0 ** 60, 1.0, 2.0 ** -60):
+        pool = base._filled(19, 1, 128, 16, rng)
+        for p in range(300):
+            pool.write(0, 1, tables[0, p // 16], p, np.full((1, 128), size * (1 + p % 3), dtype=np.float32))
+        buf, dev = base._dev_pool(pool)
+        q = torch.randn(1, 4, 128, device="cuda").bfloat16()
+        out, lse = torch.empty_like(q), torch.empty(1, 4, device="cuda")
+        remp.remp_kvq_attend(dev, batch, q, out, 128 ** -0.5, remp.make_kvq_workspace(), lse=lse)
+        prompt._check_range(out, lse, q, pool, lens, new, tables, 128 ** -0.5)
