@@ -386,6 +386,7 @@ remp_status kvq_view(const remp_kvq_pool* pool, const remp_kvq_batch* batch, Kvq
     const remp_block_tables& bt = batch->tables;
     if (bt.num_seqs < 0 || bt.max_blocks_per_seq < 0 || batch->num_tokens < 0 || batch->max_queries < 0)
         return fail(REMP_ERR_INVALID_ARG, "negative batch dimensions");
+    if (bt.num_seqs > kKvqMost || batch->num_tokens > kKvqMost) return fail(REMP_ERR_SHAPE, "too many sequences or tokens");
     if (batch->num_tokens > 0 && (!bt.seq_lens || !batch->query_start || (bt.max_blocks_per_seq > 0 && !bt.block_tables)))
         return fail(REMP_ERR_INVALID_ARG, "null seq_lens, block_tables or query_start");
     v->base = reinterpret_cast<uint8_t*>(s.base + (uint64_t)((int64_t)pool->layer * s.s_layer));

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include "remp_internal.h"
+#include "remp_kvq_span.h"
 
 namespace remp {
 

@@ -65,13 +65,10 @@ struct Seq {  // one sequence's share of the list
 template <int RB>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     Seq r;
-    const int qs = max(0, a.v.query_start[s]), qe = min(a.v.num_tokens, a.v.query_start[s + 1]);
-    const int len = a.v.seq_lens[s], n = max(0, qe - qs);
-    r.len = min(max(len, 0), a.room);
-    r.q0 = qs, r.rows = n * a.group, r.blocks = (r.rows + RB - 1) / RB;
-    r.first_pos = len - n;
-    const int from = a.window > 0 ? max(0, r.first_pos - a.window + 1) : 0;
-    r.tile0 = min(from, r.len) / kKvqTile;
+    const KvqSpan x = kvq_span(a.v.query_start[s], a.v.query_start[s + 1], a.v.seq_lens[s], a.v.num_tokens, a.room);
+    r.len = x.len, r.q0 = x.q0, r.first_pos = x.first_pos;
+    r.rows = x.queries * a.group, r.blocks = (r.rows + RB - 1) / RB;
+    r.tile0 = min(kvq_first_key(x.first_pos, a.window), x.len) / kKvqTile;
     r.tiles = (r.len + kKvqTile - 1) / kKvqTile - r.tile0;
     r.steps = max(1, (r.tiles + kStepTiles - 1) / kStepTiles);
     return r;
@@ -389,7 +386,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
-                                if (!there || key > limit[n][e] || (a.window > 0 && key <= limit[n][e] - a.window))
+                                if (!there || key > limit[n][e] || (a.window > 0 && limit[n][e] - key >= a.window))
                                     s[j][n][2 * h + e] = -INFINITY;
                     }
             }
@@ -580,7 +577,7 @@ extern "C" remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq
     a.lse = lse, a.workspace = static_cast<uint8_t*>(workspace);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.group = q_heads / pool->kv_heads, a.q_heads = q_heads, a.window = window;
-    a.room = (int32_t)std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, 0x7fffffffLL);
+    a.room = (int32_t)std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, kKvqMost);
     // rows are divided by the group with one multiplication: exact while row * group stays below 2^32
     if ((int64_t)batch->num_tokens * a.group * a.group > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
     a.by_group = a.group == 1 ? 0 : (uint32_t)((0x100000000ULL + a.group - 1) / a.group);

@@ -371,14 +371,13 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     const int head = unit % v.kv_heads;
     unit /= v.kv_heads;
     const int seq = unit % v.num_seqs, block = a.row_blocks - 1 - unit / v.num_seqs;
-    const int qs = max(0, v.query_start[seq]), qe = min(v.num_tokens, v.query_start[seq + 1]);
-    const int queries = max(0, qe - qs), rows_all = queries * a.group, row0 = block * kRows;
+    const KvqSpan span = kvq_span(v.query_start[seq], v.query_start[seq + 1], v.seq_lens[seq], v.num_tokens, a.room);
+    const int qs = span.q0, rows_all = span.queries * a.group, row0 = block * kRows;
     if (row0 >= rows_all) return;
-    const int rows = min(kRows, rows_all - row0), len_ = v.seq_lens[seq], len = min(max(len_, 0), a.room);
-    if (len != len_ && tid == 0) kvq_error(v, kErrBadLength);
-    const int first_pos = len_ - queries;
+    const int rows = min(kRows, rows_all - row0), len = span.len, first_pos = span.first_pos;
+    if (len != v.seq_lens[seq] && tid == 0) kvq_error(v, kErrBadLength);
     const int low_limit = first_pos + prompt_token(a, row0), high_limit = first_pos + prompt_token(a, row0 + rows - 1);
-    const int end = max(0, min(len, high_limit + 1)), begin = min(end, a.window > 0 ? max(0, low_limit - a.window + 1) : 0) / kKvqTile * kKvqTile;
+    const int end = max(0, min(len, high_limit + 1)), begin = min(end, kvq_first_key(low_limit, a.window)) / kKvqTile * kKvqTile;
     const int blocks_all = (end - begin + Z::kKeys - 1) / Z::kKeys;
     const int b0 = (int)((long long)blocks_all * split / splits), b1 = (int)((long long)blocks_all * (split + 1) / splits);
     const int blocks = b1 - b0, first_key = begin + b0 * Z::kKeys;
@@ -418,7 +417,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), s_at = lanes + mat * Z::kKeys, o_at = lanes + Z::kO + mat * D;
         const int row = row0 + min(tid, rows - 1), token = prompt_token(a, row), q_head = head * a.group + row - token * a.group;
         const bool real = tid < rows;
-        const int limit = min(first_pos + token, len - 1), from = a.window > 0 ? first_pos + token - a.window + 1 : 0;
+        const int limit = min(first_pos + token, len - 1), from = kvq_first_key(first_pos + token, a.window);
         float back;
         {
             const uint16_t* src = a.q.data + (int64_t)(qs + token) * a.q.s_token + (int64_t)q_head * a.q.s_head;
@@ -457,7 +456,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             tmem_after();
             const int key0 = first_key + j * Z::kKeys;
             const unsigned long long marked = *reinterpret_cast<const volatile unsigned long long*>(marks[j & 3]);
-            const bool whole = (marked & kGone * 0x0101010101010101ull) == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || key0 > high_limit - a.window);
+            const bool whole = (marked & kGone * 0x0101010101010101ull) == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || high_limit - key0 < a.window);
             if (marked & (kOwnK | kOwnV) * 0x0101010101010101ull)
                 put_powers<D>(s_at, marked, powers + (j & 3) * 2 * Z::kKeys, limit - key0, from - key0, back, apart + tid);
 #pragma unroll 1

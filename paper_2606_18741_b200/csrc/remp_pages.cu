@@ -498,6 +498,7 @@ extern "C" remp_status remp_pages_compact(const int32_t* seq_lens, const int32_t
     if (num_seqs > 0 && max_blocks_per_seq > 0 && !block_tables_out) return fail(REMP_ERR_INVALID_ARG, "null argument");
     if (max_pairs < num_blocks / 2 || (max_pairs > 0 && !pairs))
         return fail(REMP_ERR_INVALID_ARG, "pairs must have num_blocks / 2 rows");
+    if (max_pairs > 0x7fffffff - kChunk) return fail(REMP_ERR_SHAPE, "too many rows of pairs");
     if (reinterpret_cast<uint64_t>(pairs) & 7) return fail(REMP_ERR_SHAPE, "pairs must be 8-byte aligned");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     Compact c{seq_lens, block_tables, num_seqs, max_blocks_per_seq, block_size, refs, num_blocks, block_tables_out, refs_out,

@@ -137,3 +137,9 @@ def test_quantiser_of_the_reference():
     c, s, m = ref.quantise(x)
     sf, mf = np.repeat(ref.bf16_value(s), 64, -1), np.repeat(ref.bf16_value(m), 64, -1)
     assert (np.abs(c * sf + mf - x) <= 0.5 * sf * (1 + 2 ** -6) + 2 ** -8 * np.abs(mf)).all()
+
+
+def test_numbers_close_to_2_to_the_31():
+    assert _attend(batch=_batch(tokens=2 ** 31 - 1)) == SHAPE and _append(batch=_batch(seqs=2 ** 31 - 1)) == SHAPE
+    L = _lib.load()
+    assert L.remp_pages_compact(PTR, PTR, 3, 4, 16, PTR, 9, PTR, PTR, PTR, 2 ** 31 - 1, PTR, None) == SHAPE
