@@ -360,7 +360,8 @@ typedef struct {
     int32_t max_queries;        /* no sequence has more rows than this (chooses the kernel; more are not read) */
     uint32_t* error;            /* device word or NULL: bits of what the device found are OR-ed into it, with the
                                    meaning of remp_remap_tables_noalloc's status word: bit 1 bad length (negative
-                                   position, position beyond the table row or the rotation table), bit 3 block id outside the pool;
+                                   position, position beyond the table row or the rotation table; for remp_kvq_attend
+                                   a sequence's length, also of one without rows), bit 3 block id outside the pool;
                                    remp_kvq_attend also bit 2 (too many steps) and bit 4 (a wait ran out) */
 } remp_kvq_batch;
 

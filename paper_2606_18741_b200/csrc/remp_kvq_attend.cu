@@ -60,12 +60,15 @@ struct Seq {  // one sequence's share of the list
     int steps;              // of kStepTiles; at least one, so that rows which see nothing are written too
     int first_pos;          // position of its first query
     int blocks;             // row blocks
+    bool bad;               // the length was cut, or a row stands before position 0
 };
 
 template <int RB>
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     Seq r;
-    const KvqSpan x = kvq_span(a.v.query_start[s], a.v.query_start[s + 1], a.v.seq_lens[s], a.v.num_tokens, a.room);
+    const int length = a.v.seq_lens[s];
+    const KvqSpan x = kvq_span(a.v.query_start[s], a.v.query_start[s + 1], length, a.v.num_tokens, a.room);
+    r.bad = kvq_span_bad(x, length);
     r.len = x.len, r.q0 = x.q0, r.first_pos = x.first_pos;
     r.rows = x.queries * a.group, r.blocks = (r.rows + RB - 1) / RB;
     r.tile0 = min(kvq_first_key(x.first_pos, a.window), x.len) / kKvqTile;
@@ -208,7 +211,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
     for (int s = s0; s < s1; ++s) {
         const Seq q = seq_of<RB>(a, s);
         mine += (long long)(q.blocks * v.kv_heads) * q.steps;
-        if (blockIdx.x == 0 && q.len != v.seq_lens[s]) kvq_error(v, kErrBadLength);  // it was cut
+        if (blockIdx.x == 0 && q.bad) kvq_error(v, kErrBadLength);
     }
     long long before = mine;
 #pragma unroll

@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     const int qs = span.q0, rows_all = span.queries * a.group, row0 = block * kRows;
     if (row0 >= rows_all) return;
     const int rows = min(kRows, rows_all - row0), len = span.len, first_pos = span.first_pos;
-    if (len != v.seq_lens[seq] && tid == 0) kvq_error(v, kErrBadLength);
+    if (kvq_span_bad(span, v.seq_lens[seq]) && tid == 0) kvq_error(v, kErrBadLength);
     const int low_limit = first_pos + prompt_token(a, row0), high_limit = first_pos + prompt_token(a, row0 + rows - 1);
     const int end = max(0, min(len, high_limit + 1)), begin = min(end, kvq_first_key(low_limit, a.window)) / kKvqTile * kKvqTile;
     const int blocks_all = (end - begin + Z::kKeys - 1) / Z::kKeys;

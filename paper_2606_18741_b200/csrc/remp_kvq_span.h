@@ -29,6 +29,9 @@ REMP_HD KvqSpan kvq_span(int32_t start, int32_t end, int32_t length, int32_t num
     return KvqSpan{qs, qe - qs, tokens > room ? room : tokens, tokens - (qe - qs)};
 }
 
+// The length does not fit the row, or a row stands before position 0.
+REMP_HD bool kvq_span_bad(const KvqSpan& s, int32_t length) { return s.len != length || (s.queries > 0 && s.first_pos < 0); }
+
 // The first key that a row at position `pos` sees (window 0: the first of all).
 REMP_HD int32_t kvq_first_key(int32_t pos, int32_t window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
 

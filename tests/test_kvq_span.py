@@ -15,8 +15,8 @@ int main() {
     int s, e, l, n, r, w;
     while (std::scanf("%d %d %d %d %d %d", &s, &e, &l, &n, &r, &w) == 6) {
         const remp::KvqSpan x = remp::kvq_span(s, e, l, n, r);
-        std::printf("%d %d %d %d %d %d\n", x.q0, x.queries, x.len, x.first_pos, remp::kvq_first_key(x.first_pos, w),
-                    remp::kvq_first_key(x.first_pos + (x.queries ? x.queries - 1 : 0), w));
+        std::printf("%d %d %d %d %d %d %d\n", x.q0, x.queries, x.len, x.first_pos, remp::kvq_first_key(x.first_pos, w),
+                    remp::kvq_first_key(x.first_pos + (x.queries ? x.queries - 1 : 0), w), (int)remp::kvq_span_bad(x, l));
     }
 }
 """
@@ -39,4 +39,4 @@ def test_spans_at_the_ends_of_32_bits(tmp_path):
         first = max(length, 0) - queries
         last = first + max(0, queries - 1)
         keys = [max(0, p - window + 1) if window else 0 for p in (first, last)]
-        assert got == (q0, queries, min(max(length, 0), room), first, *keys)
+        assert got == (q0, queries, min(max(length, 0), room), first, *keys, int(not 0 <= length <= room or (queries > 0 and first < 0)))
