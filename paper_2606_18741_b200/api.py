@@ -400,9 +400,13 @@ def make_kvq_batch(seq_lens, block_tables, query_start, num_tokens: int, max_que
 
 
 def make_kvq_workspace(device=None):
-    """The zeroed workspace that remp_kvq_attend wants (a CUDA uint8 tensor); one for each stream."""
+    """The zeroed workspace that remp_kvq_attend wants (a CUDA uint8 tensor); one for each stream. Waits for the current
+    stream, so that the zeros are there for every other (not while a graph is captured: there it belongs to the graph's stream)."""
     import torch
-    return torch.zeros(int(_lib.load().remp_kvq_workspace_bytes()), dtype=torch.uint8, device=device or "cuda")
+    workspace = torch.zeros(int(_lib.load().remp_kvq_workspace_bytes()), dtype=torch.uint8, device=device or "cuda")
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(workspace.device).synchronize()
+    return workspace
 
 
 def _rows(t, name: str, num_tokens: int, heads: int, head_dim: int, dtype):

@@ -1,4 +1,5 @@
-"""Calls on the 4-bit cache at the edges of their arguments: windows as large as an int, positions before the sequence."""
+"""Calls on the 4-bit cache at the edges of their arguments: windows as large as an int, positions before the sequence, workspaces and
+streams."""
 import numpy as np
 import pytest
 import torch
@@ -29,3 +30,15 @@ def test_attend_reports_positions_before_the_sequence(hq, lens, new, bits):
     remp.remp_kvq_attend(dev, batch, q, out, 128 ** -0.5, remp.make_kvq_workspace())
     base._check(out, None, q, pool, 0, lens, new, tables, 128 ** -0.5, 0, torch.bfloat16)
     assert int(error) == bits
+
+
+def test_workspace_is_ready_for_any_stream():
+    x = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            x @ x
+        ws = remp.make_kvq_workspace()
+        assert side.query()  # zeroed, whichever stream comes next
+    assert not ws.any()
