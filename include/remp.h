@@ -365,8 +365,9 @@ typedef struct {
                                    remp_kvq_attend also bit 2 (too many steps) and bit 4 (a wait ran out) */
 } remp_kvq_batch;
 
-/* Rows [num_tokens][heads][head_dim] of 16-bit values on the device; strides in elements, multiples of 8, base 16-byte
- * aligned, dims dense: the slices of a fused projection need no copy. */
+/* Rows [num_tokens][heads][head_dim] of 16-bit values on the device; strides in elements, multiples of 8 (of a
+ * single head or token: anything), base 16-byte aligned, dims dense: the slices of a fused projection need no copy. Inputs may
+ * repeat a row (a stride of 0), rows of outputs must not overlap. */
 typedef struct {
     void* data;
     int64_t stride_token, stride_head;

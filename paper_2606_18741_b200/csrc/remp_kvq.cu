@@ -398,14 +398,16 @@ remp_status kvq_view(const remp_kvq_pool* pool, const remp_kvq_batch* batch, Kvq
     return REMP_OK;
 }
 
-remp_status kvq_rows(const remp_kvq_rows* r, int32_t heads, int32_t head_dim, const char* name, KvqRows* out) {
+remp_status kvq_rows(const remp_kvq_rows* r, int32_t tokens, int32_t heads, int32_t head_dim, bool written, const char* name, KvqRows* out) {
     if (!r || !r->data) return fail(REMP_ERR_INVALID_ARG, std::string("null ") + name);
-    if ((reinterpret_cast<uint64_t>(r->data) & 15) || (r->stride_token & 7) || (r->stride_head & 7))
+    const int64_t s_token = tokens > 1 ? r->stride_token : 0, s_head = heads > 1 ? r->stride_head : 0;
+    if ((reinterpret_cast<uint64_t>(r->data) & 15) || (s_token & 7) || (s_head & 7))
         return fail(REMP_ERR_SHAPE, std::string(name) + ": base must be 16-byte aligned and strides multiples of 8 elements");
-    if (heads > 1 && r->stride_head < head_dim && r->stride_head > -head_dim)
-        return fail(REMP_ERR_SHAPE, std::string(name) + ": heads overlap");
+    const auto apart = [&](int64_t stride) { return stride >= head_dim || stride <= -head_dim; };
+    if (heads > 1 && !apart(s_head) && (written || s_head != 0)) return fail(REMP_ERR_SHAPE, std::string(name) + ": heads overlap");
+    if (tokens > 1 && !apart(s_token) && written) return fail(REMP_ERR_SHAPE, std::string(name) + ": tokens overlap");
     out->data = static_cast<uint16_t*>(r->data);
-    out->s_token = r->stride_token, out->s_head = r->stride_head;
+    out->s_token = s_token, out->s_head = s_head;
     return REMP_OK;
 }
 
@@ -447,11 +449,11 @@ extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq
     }
     if (view.num_tokens == 0) return REMP_OK;
     if (q_heads) {
-        if (remp_status st = kvq_rows(q, q_heads, d, "q", &rq)) return st;
-        if (remp_status st = kvq_rows(q_out, q_heads, d, "q_out", &ro)) return st;
+        if (remp_status st = kvq_rows(q, view.num_tokens, q_heads, d, false, "q", &rq)) return st;
+        if (remp_status st = kvq_rows(q_out, view.num_tokens, q_heads, d, true, "q_out", &ro)) return st;
     }
-    if (remp_status st = kvq_rows(k, pool->kv_heads, d, "k", &rk)) return st;
-    if (remp_status st = kvq_rows(v, pool->kv_heads, d, "v", &rv)) return st;
+    if (remp_status st = kvq_rows(k, view.num_tokens, pool->kv_heads, d, false, "k", &rk)) return st;
+    if (remp_status st = kvq_rows(v, view.num_tokens, pool->kv_heads, d, false, "v", &rv)) return st;
     const int64_t rows = (int64_t)q_heads + 2 * (int64_t)pool->kv_heads;
     const int heads = 32 / (d / 8) * kSets;  // of a group
     if (rows > 0x7fffffffLL - 3 * heads) return fail(REMP_ERR_SHAPE, "too many heads");
@@ -481,9 +483,9 @@ extern "C" remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_b
     const int32_t d = pool->head_dim;
     if (view.num_tokens == 0 || (!k_out && !v_out)) return REMP_OK;
     if (k_out)
-        if (remp_status st = kvq_rows(k_out, pool->kv_heads, d, "k_out", &rk)) return st;
+        if (remp_status st = kvq_rows(k_out, view.num_tokens, pool->kv_heads, d, true, "k_out", &rk)) return st;
     if (v_out)
-        if (remp_status st = kvq_rows(v_out, pool->kv_heads, d, "v_out", &rv)) return st;
+        if (remp_status st = kvq_rows(v_out, view.num_tokens, pool->kv_heads, d, true, "v_out", &rv)) return st;
     const int per_item = 32 / (d / 8) * kSets;
     const int64_t sets = (2 * (int64_t)pool->kv_heads + per_item - 1) / per_item;
     const int64_t grid = (view.num_tokens * sets + kWarps - 1) / kWarps;

@@ -572,8 +572,8 @@ extern "C" remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq
         return fail(REMP_ERR_INVALID_ARG, "the workspace must be 256-byte aligned device memory");
     if (a.v.num_tokens == 0) return REMP_OK;
     if (batch->max_queries < 1) return fail(REMP_ERR_INVALID_ARG, "max_queries must be positive");
-    if (remp_status st = kvq_rows(q, q_heads, pool->head_dim, "q", &a.q)) return st;
-    if (remp_status st = kvq_rows(out, q_heads, pool->head_dim, "out", &a.out)) return st;
+    if (remp_status st = kvq_rows(q, a.v.num_tokens, q_heads, pool->head_dim, false, "q", &a.q)) return st;
+    if (remp_status st = kvq_rows(out, a.v.num_tokens, q_heads, pool->head_dim, true, "out", &a.out)) return st;
     int device = -1, sms = 0;
     REMP_CUDA(cudaGetDevice(&device));
     REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));

@@ -1,5 +1,5 @@
 """Calls on the 4-bit cache at the edges of their arguments: windows as large as an int, positions before the sequence, workspaces and
-streams."""
+streams, rows with strides of 0."""
 import numpy as np
 import pytest
 import torch
@@ -42,3 +42,33 @@ def test_workspace_is_ready_for_any_stream():
         ws = remp.make_kvq_workspace()
         assert side.query()  # zeroed, whichever stream comes next
     assert not ws.any()
+
+
+def test_rows_repeated_by_strides_of_zero():
+    # inputs that are broadcast: one key for all heads, one value for all tokens, one query for all heads
+    rng = np.random.default_rng(4)
+    d, hk, n = 128, 4, 6
+    lens, new, tables, start, batch = base._batch([20, 9], [4, 2], 16, 4, rng)
+    k, v, q = (torch.randn(*s, d, device="cuda").bfloat16() for s in ((n, 1), (1, hk), (n, 1)))
+    wide = [k.expand(n, hk, d), v.expand(n, hk, d), q.expand(n, 2 * hk, d)]
+    outs = []
+    for kk, vv, qq in (wide, [x.contiguous() for x in wide]):
+        p = base.ref.Pool(1, 4, hk, d, 16)
+        buf, dev = base._dev_pool(base._filled(4, hk, d, 16, np.random.default_rng(1)))
+        turned, out = torch.empty(n, 2 * hk, d, dtype=k.dtype, device="cuda"), torch.empty(n, 2 * hk, d, dtype=k.dtype, device="cuda")
+        remp.remp_kvq_append(dev, batch, qq, kk, vv, turned)
+        remp.remp_kvq_attend(dev, batch, qq, out, d ** -0.5, remp.make_kvq_workspace())
+        outs.append((buf, turned, out))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_strides_of_single_heads_and_tokens_do_not_matter():
+    rng = np.random.default_rng(5)
+    d = 64
+    lens, new, tables, start, batch = base._batch([20], [1], 16, 2, rng)
+    buf, dev = base._dev_pool(base._filled(2, 1, d, 16, rng))
+    row = torch.randn(d, device="cuda").bfloat16()
+    odd = row.as_strided((1, 1, d), (3, 5, 1))  # what slices of padded tensors can look like
+    out = torch.zeros(d, dtype=row.dtype, device="cuda")
+    remp.remp_kvq_append(dev, batch, odd, odd, odd, out.as_strided((1, 1, d), (3, 5, 1)))
+    assert torch.equal(out, row)

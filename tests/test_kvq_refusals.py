@@ -143,3 +143,11 @@ def test_numbers_close_to_2_to_the_31():
     assert _attend(batch=_batch(tokens=2 ** 31 - 1)) == SHAPE and _append(batch=_batch(seqs=2 ** 31 - 1)) == SHAPE
     L = _lib.load()
     assert L.remp_pages_compact(PTR, PTR, 3, 4, 16, PTR, 9, PTR, PTR, PTR, 2 ** 31 - 1, PTR, None) == SHAPE
+
+
+def test_outputs_whose_rows_overlap():
+    # inputs may repeat a head or a token, outputs may not
+    assert _attend(out=_rows(head=0)) == SHAPE and _attend(out=_rows(token=0)) == SHAPE and _attend(out=_rows(token=64)) == SHAPE
+    assert _append(q=_rows(), q_out=_rows(head=0), q_heads=2) == SHAPE and _append(q=_rows(), q_out=_rows(token=0), q_heads=2) == SHAPE
+    assert _lib.load().remp_kvq_read(_pool(), _batch(), _rows(token=0), None, 1, None) == SHAPE
+    assert _append(v=_rows(token=0), k=_rows(head=0), batch=_batch(tokens=0)) == remp.REMP_OK
