@@ -35,6 +35,12 @@ remp_status device_pool(int device, cudaMemPool_t* out) {
     std::lock_guard<std::mutex> lock(g_pool_mu);
     if (device < 0 || device >= 64) return fail(REMP_ERR_INVALID_ARG, "device index out of range");
     if (!g_pools[device]) {
+        // the first call may be in the capture of a graph: making a pool puts nothing into it
+        struct Relaxed {
+            cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+            Relaxed() { cudaThreadExchangeStreamCaptureMode(&mode); }
+            ~Relaxed() { cudaThreadExchangeStreamCaptureMode(&mode); }
+        } relaxed;
         cudaMemPoolProps props{};
         props.allocType = cudaMemAllocationTypePinned;
         props.handleTypes = cudaMemHandleTypeNone;
