@@ -119,3 +119,58 @@ def test_prompt_tokens_of_different_sizes(d, hq, hk, lens, new):
     _range_case(d, hq, hk, lens, new, 1.0, 1.0, 1.0, seed=d + 3, per_token=((-3, -1), (-5, -2)))  # around where the kernel changes its way
     _range_case(d, hq, hk, lens, new, 1.0, 1.0, 1.0, seed=d + 5, per_token=((0, 0), (1, 4)))
     _range_case(d, hq, hk, lens, new, 1e-2, 1.0, 100.0, seed=d + 4, per_token=((-1.5, 0.5), (3, 6)))
+
+
+# ---- many blocks of keys in a thread block ----
+
+# (head_dim, query heads, KV heads, sequences, tokens, query tokens, window): of 148 units and more, so that the first 148 walk all
+# their keys and the others share theirs; a block of keys is 128 of them (64 with 256 dims); up to 128 rows, and above
+LONG = [(128, 16, 8, 20, 800, 20, 0), (128, 32, 16, 10, 600, 70, 0), (64, 16, 8, 20, 900, 20, 0), (64, 10, 10, 15, 700, 150, 0), (256, 8, 8, 20, 500, 40, 0),
+        (128, 16, 8, 20, 800, 20, 300), (64, 10, 10, 15, 700, 150, 170), (256, 8, 8, 20, 500, 40, 150), (128, 4, 4, 37, 700, 40, 0)]
+
+
+@pytest.mark.parametrize("dtype,half_ulp", [(torch.bfloat16, 2.0 ** -8), (torch.float16, 2.0 ** -11)])
+@pytest.mark.parametrize("rising", [False, True])
+@pytest.mark.parametrize("d,hq,hk,seqs,length,queries,window", LONG)
+def test_prompt_over_many_blocks_of_keys(d, hq, hk, seqs, length, queries, window, rising, dtype, half_ulp):
+    # Keys are whole numbers from -7 to 8 with both ends in each group: step 1 and minimum -7, exact in half, so nothing in the
+    # tolerance grows with the scores (2^-13 is for their sums in 32 bits, 2^-20 of the sizes of some 30 that they add up).
+    # rising: eight dims make the scores of each sixteenth of the sequence 9 (base 2) higher than those of the one before, so that
+    # references move between blocks of keys and within them.
+    rng = np.random.default_rng(d + queries)
+    lens = rng.integers(length * 3 // 4, length + 1, seqs)
+    lens[0] = length
+    blocks = int((-(-lens // 16)).sum())
+    lens, new, tables, start, batch = base._batch(lens, np.full(seqs, queries), 16, blocks, rng)
+    k = rng.integers(-7, 9, (blocks, hk, 16, d))
+    k[..., 0::64], k[..., 1::64] = -7, 8
+    q = rng.standard_normal((int(start[-1]), hq, d))
+    if rising:
+        q[..., 2:10] = 9 / (8 * d ** -0.5 * np.log2(np.e))
+        for s in range(seqs):
+            level = np.arange(-(-lens[s] // 16) * 16) * 16 // lens[s] - 7
+            k[tables[s, :len(level) // 16], :, :, 2:10] = np.minimum(level, 8).reshape(-1, 1, 16, 1)
+    else:
+        q *= 0.5
+    pool = base.ref.Pool(1, blocks, hk, d, 16)
+    for kv, x in enumerate((k, rng.standard_normal(k.shape))):
+        c, step, low = base.ref.quantise(x.astype(np.float32))
+        assert kv or ((step == 0x3f80) & (low == 0xc0e0)).all()
+        c = c[..., base.ref.place_of(d, kv == 1)]
+        codes = (c[..., 0::2] | c[..., 1::2] << 4).reshape(blocks, hk, 1, -1)
+        pool.bytes[0, kv] = np.concatenate([codes, np.stack([step, low], -1).reshape(blocks, hk, 1, -1).view(np.uint8)], -1)
+    buf, dev = base._dev_pool(pool)
+    q = torch.from_numpy(q).to(dtype).cuda()
+    out, again, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = remp.make_kvq_workspace()
+    remp.remp_kvq_attend(dev, batch, q, out, d ** -0.5, ws, window=window, lse=lse)
+    remp.remp_kvq_attend(dev, batch, q, again, d ** -0.5, ws, window=window)
+    assert torch.equal(out, again)
+    for s in (0, 1, seqs // 2, seqs - 1):
+        rows = slice(s * queries, (s + 1) * queries)
+        kk, vv = (pool.rows(0, kv, tables[s], int(lens[s])) for kv in (0, 1))
+        want, want_lse, _, size, _ = base.ref.attend(q[rows].double().cpu().numpy(), kk, vv, int(lens[s]) - queries, d ** -0.5, window)
+        err = np.abs(out[rows].double().cpu().numpy() - want)
+        tol = half_ulp * np.abs(want) + (2.0 ** -10 + 2.0 ** -13) * size[..., None]
+        assert (err <= tol).all(), (s, (err / tol).max())
+        assert (np.abs(lse[rows].double().cpu().numpy() - want_lse) <= 2e-5 * np.maximum(1, np.abs(want_lse))).all()
