@@ -5,11 +5,11 @@
 // running reference for each row that moves only when the probabilities of 32 keys outgrow kBound.
 // Rounding: q is exact in half after a power of two per row; keys and values s*c + m are rounded to half and so is P (twice
 // where a reference moves in the middle of its block of keys); S, O, sums and references are in 32 bits.
-// Range: halves hold K/4 and 8 V where every token of a tile has its largest step or minimum in a range that allows it (2^-7 to
-// 2^13, 2^-12 to 2^8). In other tiles each token has a power of two of its own, which brings that to [2^10, 2^11), so that a
-// value is rounded to 11 bits down to 2^-24 of the token's largest. S is multiplied with K's powers; V's go into P, and the
-// reference bounds P with them in it, so a row that sees only tokens of small values is as exact as any other. The sums of P
-// are without them.
+// Range: halves hold K/4 and 8 V where every token of a thread block's keys has its largest step or minimum in a range that allows
+// it (2^-7 to 2^13, 2^-12 to 2^8). Where one has not, each token gets a power of two of its own, which brings that to [2^10,
+// 2^11), so that a value is rounded to 11 bits down to 2^-24 of the token's largest. S is multiplied with K's powers; V's go
+// into P, and the reference bounds P with them in it, so a row that sees only tokens of small values is as exact as any
+// other. The sums of P are without them. The warps that make no P look at all the parameters first, while the queries come.
 //
 // Bound: tensor cores (4*D flops for each row and key), then issue slots and exponentials: eight warps turn codes into halves
 // once for both matrices, eight compute P (a row to a thread), one thread issues the matrix instructions, which run for
@@ -19,17 +19,19 @@
 // their columns of the tensor memory, O has its own. With 256 dims O takes so much of it that one matrix of 128 rows and
 // blocks of 64 keys are left.
 //
-// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 594 to 607 us in different
-// runs: 792 to 809 TFLOP/s, 48 to 50 % of a library product in bf16. Bound by the chain of one matrix, scores to P to products to
+// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 577 to 594 us in different
+// runs: 810 to 834 TFLOP/s, 50 to 51 % of a library product in bf16. Bound by the chain of one matrix, scores to P to products to
 // the next scores: some 4750 cycles for a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each,
-// which break the chain, took 779 us (both timed with clock reads in the kernel). Where every tile has powers of its own the
-// same call takes 1.21 ms (K's) and 1.75 ms (V's); with them inside the loop that makes P every call took 870 us.
+// which break the chain, took 779 us (both timed with clock reads in the kernel). Looking at
+// the parameters first takes 1 to 3 % (587 us without; 256 dims 562 and 567; 40 rows over 4000 keys 72 and 74); marks for each
+// tile inside the loops took up to 24 % (256 dims 695). With powers of their own the same call takes 0.96 ms.
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up issues no more matrix instructions, goes on
 // without waiting, writes NaN and sets error bit 4. Whatever happens, the issuing warp leaves when everything that it has
 // issued is done and every barrier that it has committed to has been arrived at, so nothing runs on in freed memory.
 
 #include <atomic>
+#include <type_traits>
 
 #include "remp_kvq_device.h"
 
@@ -41,13 +43,12 @@ constexpr int kRowsM = 128;
 constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
-// What K and V are multiplied with to become halves, as powers of two, where all tokens of a tile allow it: the larger of
-// step and minimum is from 2^kLeast to below 2^kMost. Below, steps lose bits as halves, above, 16 times as much is no half.
+// What K and V are multiplied with to become halves, as powers of two, where all tokens allow it: the larger of step and
+// minimum is from 2^least_of to below 2^most_of. Below, steps lose bits as halves, above, 16 times as much is no half.
 // Keys are wide (biases, outliers), values small: K from 2^-7 to 2^13, V from 2^-12 to 2^8.
 constexpr int kUpK = -2, kUpV = 3;
 __host__ __device__ constexpr int least_of(int up) { return -9 - up; }
 __host__ __device__ constexpr int most_of(int up) { return 11 - up; }
-enum : uint8_t { kGone = 1, kOwnK = 2, kOwnV = 4 };  // marks of a tile: not there; K's, V's tokens have powers of their own
 constexpr int kMostSplits = 16;
 constexpr int32_t kWaitTries = 1 << 18;
 std::atomic<int32_t> g_wait_tries{kWaitTries};  // remp_kvq_set_wait_limit
@@ -58,8 +59,7 @@ struct Prompt {
     static constexpr int kKeys = D == 256 ? 64 : 128, kUnpackWarps = kKeys / kKvqTile;  // a tile to a warp
     static constexpr int kQ = kRowsM * D * 2, kK = kKeys * D * 2, kV = kKeys * D * 2;  // bytes of a matrix, of a block
     static constexpr int kPowers = 4 * 2 * kKeys * 4;  // of K and V, four blocks of keys
-    static constexpr int kApart = kRows * 8;          // a reference and a sum for each row
-    static constexpr int kBytes = kMats * kQ + 2 * (kK + kV) + kPowers + kApart + 1024;
+    static constexpr int kBytes = kMats * kQ + 2 * (kK + kV) + kPowers + 1024;
     // columns of the tensor memory: S and P of each matrix, then O of each
     static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
     static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
@@ -248,10 +248,9 @@ __device__ __forceinline__ uint32_t largest_of(const uint32_t (&par)[G]) {
     for (int i = 0; i < G; ++i) most = __vmaxu2(most, par[i] & 0x7fff7fffu);
     return max(most >> 16, most & 0xffffu);
 }
-template <int UP>
-__device__ __forceinline__ bool out_of_range(uint32_t largest) {
-    constexpr uint32_t kLeast = (uint32_t)(127 + least_of(UP)) << 7, kMost = (uint32_t)(127 + most_of(UP)) << 7;  // as bits of bfloat16
-    return largest != 0 && largest - kLeast >= kMost - kLeast;
+__device__ __forceinline__ bool out_of_range(int up, uint32_t largest) {
+    const uint32_t least = (uint32_t)(127 + least_of(up)) << 7, most = (uint32_t)(127 + most_of(up)) << 7;  // as bits of bfloat16
+    return largest != 0 && largest - least >= most - least;
 }
 // A token's power of two, over that of all tokens. Groups of NaN and infinity do not count. Of V 2^-78 to 2^103, so that sums
 // of P without the powers stay inside 32 bits' range; of K 2^-114 to 2^110.
@@ -307,48 +306,6 @@ __device__ __forceinline__ void store_v(uint8_t* const (&place)[2], const RawV<D
         }
 }
 
-// Scores of keys whose tokens have powers of their own, as the loop that makes P wants them: multiplied with K's powers, and with
-// the logarithms of V's added (over `back`, which it multiplies with), so that its P has these in it. What the keys add to the
-// sum, which is without V's powers, is kept in `apart`: a reference and a sum of the row. The loop takes 32 keys at a time, so
-// both of their tiles count here when one has the mark. marked: the block's marks; key_powers: K's, V's kKeys behind; last,
-// first: the row's keys, counted in the block.
-template <int D>
-__device__ __forceinline__ void put_powers(uint32_t s_at, unsigned long long marked, const float* key_powers, int last, int first, float back, float2* apart) {
-    constexpr int kTiles = Prompt<D>::kKeys / kKvqTile;
-    const float per = 1.f / back;
-    float2 state = *apart;
-#pragma unroll 1
-    for (int i = 0; i < kTiles; ++i) {
-        const uint32_t mark = (uint32_t)(marked >> (8 * i)) & 0xffu;
-        const bool own_v = marked >> (16 * (i / 2)) & kOwnV * 0x101u;  // of one of the two tiles
-        if (!(mark & kOwnK) && !own_v) continue;
-        uint32_t s[kKvqTile];
-        tmem_load16(s_at + kKvqTile * i, s);
-        const float* const f = key_powers + kKvqTile * i;
-        float top = -INFINITY, now[kKvqTile];
-#pragma unroll
-        for (int k = 0; k < kKvqTile; ++k) {
-            float x = __uint_as_float(s[k]);
-            if (mark & kOwnK) x *= f[k];
-            const int key = kKvqTile * i + k;
-            now[k] = key > last || key < first || (mark & kGone) ? -INFINITY : x * back;
-            top = fmaxf(top, now[k]);
-            if (mark & kOwnV) x = fmaf((float)((int)(__float_as_uint(f[Prompt<D>::kKeys + k]) >> 23) - 127), per, x);
-            s[k] = __float_as_uint(x);
-        }
-        tmem_store16(s_at + kKvqTile * i, s);
-        if (own_v) {
-            top = fmaxf(top, state.x);
-            float sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < kKvqTile; ++k) sum += exp2_approx(now[k] - top);
-            state = make_float2(top, fmaf(state.y, exp2_approx(state.x - top), sum));
-        }
-    }
-    tmem_stored();
-    *apart = state;
-}
-
 template <int D, bool BF>
 __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(const __grid_constant__ PromptArgs a) {
     using Z = Prompt<D>;
@@ -357,8 +314,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     __shared__ uint32_t tmem_at;
     __shared__ int dead;
     __shared__ int is_last;
+    __shared__ int own_powers;  // tokens have powers of two of their own
     constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kUnpackWarps = Z::kUnpackWarps, kRows = Z::kRows;
-    __shared__ __align__(8) uint8_t marks[4][8];  // of the tiles of a block of keys
+    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const KvqView& v = a.v;
@@ -384,8 +342,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
 
     uint8_t* smem = smem_ + ((1024u - ((uint32_t)__cvta_generic_to_shared(smem_) & 1023u)) & 1023u);
     uint8_t *sq = smem, *sk = smem + Z::kMats * Z::kQ, *sv = sk + 2 * Z::kK;
-    float* const powers = reinterpret_cast<float*>(sv + 2 * Z::kV);  // [block & 3][K, V][key], of tiles with the mark
-    float2* const apart = reinterpret_cast<float2*>(sv + 2 * Z::kV + Z::kPowers);  // see put_powers
+    float* const powers = reinterpret_cast<float*>(sv + 2 * Z::kV);  // [block & 3][K, V][key]
     // blocks of K and V come and go (two places each); scores, probabilities and outputs of each matrix; queries
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t k_full = bar, k_free = bar + 16, v_full = bar + 32, v_free = bar + 48, s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, q_full = bar + 112;
@@ -397,8 +354,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         }
         bar_init(q_full, kSoftmaxWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        dead = 0, is_last = 0;
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(marks[i]) = 0;
+        dead = 0, is_last = 0, own_powers = 0;
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(gone[i]) = 0;
     }
     if (wid == kSoftmaxWarps + kUnpackWarps) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_at)),
@@ -410,6 +367,53 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     __syncthreads();
     tmem_after();
     const uint32_t tmem = tmem_at;
+
+    // Does a token need a power of its own? The warps that make no P look, at tiles nth, nth + kLookers and so on, 16 bytes of
+    // parameters to a lane, while the others bring the queries; all meet behind it.
+    constexpr int kLookers = kUnpackWarps + 1;
+    const auto look = [&](int nth) {
+        constexpr int kLanes = D / 16, kTiles = 16 / kLanes, kAhead = D == 256 ? 16 : 4;  // lanes of a tile's K or V, tiles of a load, loads ahead
+        const int tiles = (max(0, min(end, first_key + blocks * Z::kKeys) - first_key) + kKvqTile - 1) / kKvqTile;
+        const bool of_v = lane / kLanes & 1;
+        const int sub = lane / (2 * kLanes), first_token = lane % kLanes * (256 / D);
+        const uint8_t* params = v.base + (int64_t)head * v.s_head + (of_v ? v.s_kv : 0) + kKvqTile * D / 2 + lane % kLanes * 16;
+        bool odd = false;
+#pragma unroll 1
+        for (int t0 = nth; t0 < tiles; t0 += kLookers * 32) {
+            const int mine = t0 + lane * kLookers, tile = first_key / kKvqTile + mine;  // where this lane's tile is in the pool
+            long long at = -1;
+            if (mine < tiles) {
+                const int in_row = tile / v.block_tiles, id = __ldcg(v.tables + (int64_t)seq * v.max_blocks + in_row);
+                if ((uint32_t)id < (uint32_t)v.nb) at = (int64_t)id * v.s_block + (tile - in_row * v.block_tiles) * (kKvqTile * kvq_token_bytes(D));
+            }
+#pragma unroll 1
+            for (int i = 0; i < 32 && t0 + i * kLookers < tiles; i += kAhead * kTiles) {
+                uint4 par[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const long long from = __shfl_sync(0xffffffffu, at, i + k * kTiles + sub);
+                    par[k] = from >= 0 ? __ldcg(reinterpret_cast<const uint4*>(params + from)) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t w[4] = {par[k].x, par[k].y, par[k].z, par[k].w};
+                    const int token = first_key + (t0 + (i + k * kTiles + sub) * kLookers) * kKvqTile + first_token;
+#pragma unroll
+                    for (int u = 0; u < 256 / D; ++u) {
+                        uint32_t one[D / 64];
+#pragma unroll
+                        for (int x = 0; x < D / 64; ++x) one[x] = w[u * (D / 64) + x];
+                        odd |= token + u < len && out_of_range(of_v ? kUpV : kUpK, largest_of(one));
+                    }
+                }
+            }
+        }
+        if (__any_sync(0xffffffffu, odd) && lane == 0) *static_cast<volatile int*>(&own_powers) = 1;
+    };
+    const auto all_meet = [&] {
+        asm volatile("bar.sync 2, %0;" ::"n"(Z::kThreads) : "memory");
+        return *static_cast<volatile int*>(&own_powers) != 0;
+    };
 
     if (wid < kSoftmaxWarps) {
         // ---- P and the output: one row to a thread ----
@@ -447,90 +451,128 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             __syncwarp();
             if (lane == 0) bar_arrive(q_full);
         }
+        const bool odd = all_meet();
         float ref = kUnset, sum = 0.f;
-        apart[tid] = make_float2(kUnset, 0.f);
+        const auto make_p = [&](auto own) {
+            constexpr bool kOwn = decltype(own)::value;
 #pragma unroll 1
-        for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
-            bar_wait(s_full + 8 * mat, j & 1, &dead, a.tries);
-            __syncwarp();
-            tmem_after();
-            const int key0 = first_key + j * Z::kKeys;
-            const unsigned long long marked = *reinterpret_cast<const volatile unsigned long long*>(marks[j & 3]);
-            const bool whole = (marked & kGone * 0x0101010101010101ull) == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || high_limit - key0 < a.window);
-            if (marked & (kOwnK | kOwnV) * 0x0101010101010101ull)
-                put_powers<D>(s_at, marked, powers + (j & 3) * 2 * Z::kKeys, limit - key0, from - key0, back, apart + tid);
+            for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
+                bar_wait(s_full + 8 * mat, j & 1, &dead, a.tries);
+                __syncwarp();
+                tmem_after();
+                const int key0 = first_key + j * Z::kKeys;
+                const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
+                const bool whole = missing == 0 && key0 + Z::kKeys - 1 <= min(low_limit, len - 1) && (a.window <= 0 || high_limit - key0 < a.window);
+                const float* const block_powers = powers + (j & 3) * 2 * Z::kKeys;
 #pragma unroll 1
-            for (int c = 0; c < Z::kKeys / 32; ++c) {
-                uint32_t s[32];
-                tmem_load32(s_at + 32 * c, s);
-                if (!whole) {
-                    const int last = limit - key0 - 32 * c, first = from - key0 - 32 * c;
-                    uint32_t hidden = 0;  // keys of blocks that are not there
+                for (int c = 0; c < Z::kKeys / 32; ++c) {
+                    const auto load_scores = [&](uint32_t (&s)[32]) {
+                        tmem_load32(s_at + 32 * c, s);
+                        if constexpr (kOwn) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (marked >> (8 * (2 * c + i)) & kGone) hidden |= 0xffffu << (16 * i);
+                            for (int i = 0; i < 32; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * block_powers[32 * c + i]);
+                        }
+                        if (!whole) {
+                            const int last = limit - key0 - 32 * c, first = from - key0 - 32 * c;
+                            uint32_t hidden = 0;  // keys of blocks that are not there
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (i > last || i < first || (hidden >> i & 1)) s[i] = 0xff800000u;  // -infinity
-                }
-                uint32_t p[16];
-                float part;
-#pragma unroll 1
-                for (int round = 0;; ++round) {
-                    float even = 0.f, odd = 0.f;
+                            for (int i = 0; i < 2; ++i)
+                                if (missing >> (8 * (2 * c + i)) & 1) hidden |= 0xffffu << (16 * i);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x = exp2_approx(fmaf(__uint_as_float(s[2 * i]), back, -ref)), y = exp2_approx(fmaf(__uint_as_float(s[2 * i + 1]), back, -ref));
-                        even += x, odd += y;
-                        p[i] = pack2(x, y, false);
-                    }
-                    part = even + odd;
-                    if (round || !__any_sync(0xffffffffu, part > kBound)) break;
+                            for (int i = 0; i < 32; ++i)
+                                if (i > last || i < first || (hidden >> i & 1)) s[i] = 0xff800000u;  // -infinity
+                        }
+                    };
                     // rows that have outgrown their reference get another; what they have so far falls with it
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
-                    const float now = part > kBound ? top * back - kStart : ref, fall = exp2_approx(ref - now);
-                    ref = now, sum *= fall;
-                    if (j > 0) {
-                        bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead, a.tries);
-                        __syncwarp();
-                        tmem_after();
+                    const auto move_reference = [&](float now) {
+                        const float fall = exp2_approx(ref - now);
+                        ref = now, sum *= fall;
+                        if (j > 0) {
+                            bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead, a.tries);
+                            __syncwarp();
+                            tmem_after();
 #pragma unroll 1
-                        for (int i = 0; i < D; i += 16) {
-                            uint32_t o[16];
-                            tmem_load16(o_at + i, o);
+                            for (int i = 0; i < D; i += 16) {
+                                uint32_t o[16];
+                                tmem_load16(o_at + i, o);
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
-                            tmem_store16(o_at + i, o);
+                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+                                tmem_store16(o_at + i, o);
+                            }
+                        }
+                        tmem_stored();
+#pragma unroll 1
+                        for (int i = 0; i < c; ++i) {
+                            uint32_t x[16];
+                            tmem_load16(s_at + 16 * i, x);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) x[k] = as_word(__hmul2(as_half2(x[k]), __float2half2_rn(fall)));
+                            tmem_store16(s_at + 16 * i, x);
+                        }
+                        tmem_stored();
+                    };
+                    uint32_t p[16];
+                    float part;
+                    if constexpr (!kOwn) {
+                        uint32_t s[32];
+                        load_scores(s);
+#pragma unroll 1
+                        for (int round = 0;; ++round) {
+                            float even = 0.f, odds = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float x = exp2_approx(fmaf(__uint_as_float(s[2 * i]), back, -ref)), y = exp2_approx(fmaf(__uint_as_float(s[2 * i + 1]), back, -ref));
+                                even += x, odds += y;
+                                p[i] = pack2(x, y, false);
+                            }
+                            part = even + odds;
+                            if (round || !__any_sync(0xffffffffu, part > kBound)) break;
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
+                            move_reference(part > kBound ? top * back - kStart : ref);
+                        }
+                    } else {
+                        const float* const f = block_powers + Z::kKeys + 32 * c;
+                        float weight = 0.f;  // the sum with V's powers
+#pragma unroll 1
+                        for (int round = 0;; ++round) {
+                            uint32_t s[32];  // read again in the second round: kept, it would cost the registers that P takes
+                            load_scores(s);
+                            if (round) {
+                                float top = -INFINITY;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) top = fmaxf(top, fmaf(__uint_as_float(s[i]), back, (float)((int)(__float_as_uint(f[i]) >> 23) - 127)));
+                                move_reference(weight > kBound ? top - kStart : ref);
+                            }
+                            part = weight = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float x = exp2_approx(fmaf(__uint_as_float(s[2 * i]), back, -ref)), y = exp2_approx(fmaf(__uint_as_float(s[2 * i + 1]), back, -ref));
+                                const float u = x * f[2 * i], v = y * f[2 * i + 1];
+                                part += x + y, weight += u + v;
+                                p[i] = pack2(u, v, false);
+                            }
+                            if (round || !__any_sync(0xffffffffu, weight > kBound)) break;
                         }
                     }
-                    tmem_stored();
-#pragma unroll 1
-                    for (int i = 0; i < c; ++i) {
-                        uint32_t x[16];
-                        tmem_load16(s_at + 16 * i, x);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) x[k] = as_word(__hmul2(as_half2(x[k]), __float2half2_rn(fall)));
-                        tmem_store16(s_at + 16 * i, x);
-                    }
-                    tmem_stored();
+                    sum += part;
+                    tmem_store16(s_at + 16 * c, p);
                 }
-                sum += marked >> (16 * c) & kOwnV * 0x101u ? 0.f : part;
-                tmem_store16(s_at + 16 * c, p);
+                tmem_stored();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full + 8 * mat);
             }
-            tmem_stored();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * mat);
-        }
+        };
+        if (odd) make_p(std::true_type());
+        else make_p(std::false_type());
         const bool some = blocks > 0 && mat < mats;
         if (some) {
             bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead, a.tries);
             __syncwarp();
             tmem_after();
         }
-        if (apart[tid].y != 0.f) sum = fmaf(apart[tid].y, exp2_approx(apart[tid].x - ref), sum);
         // Whoever gave up said so before its next arrival, so no output that went wrong gets here without the mark.
         if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
         uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
@@ -643,60 +685,60 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         const uint8_t* at = find(0);
         load_k<D>(at, g, t, rk);
         load_v<D>(at ? at + v.s_kv : nullptr, valid(0), g, t, rv);
+        look(w);
+        const bool odd = all_meet();
+        const auto unpack = [&](auto own) {
+            constexpr bool kOwn = decltype(own)::value;
 #pragma unroll 1
-        for (int j = 0; j < blocks; ++j) {
-            const int place_of = j & 1, turn = (j >> 1) & 1;
-            const uint8_t* next = find(j + 1);
-            if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead, a.tries);
-            // tokens of sizes that halves do not hold: powers of two, told to the warps that make P before K is
-            float down_k[2] = {two_to(kUpK), two_to(kUpK)};
-            float* const my_powers = powers + (j & 3) * 2 * Z::kKeys + w * kKvqTile;
-            uint8_t mark = at ? 0 : kGone;
-            if (__any_sync(0xffffffffu, at && (out_of_range<kUpK>(largest_of(rk.par[0])) || out_of_range<kUpK>(largest_of(rk.par[1]))))) {
-                mark |= kOwnK;
+            for (int j = 0; j < blocks; ++j) {
+                const int place_of = j & 1, turn = (j >> 1) & 1;
+                const uint8_t* next = find(j + 1);
+                if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+                float down_k[2] = {two_to(kUpK), two_to(kUpK)}, down_v[4] = {two_to(kUpV), two_to(kUpV), two_to(kUpV), two_to(kUpV)};
+                if constexpr (kOwn) {  // told to the warps that make P before K is
+                    float* const my_powers = powers + (j & 3) * 2 * Z::kKeys + w * kKvqTile;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float f = power_of<kUpK>(rk.par[h]);
-                    down_k[h] = down_of<kUpK>(f);
-                    if (t == 0) my_powers[g + 8 * h] = f;
+                    for (int h = 0; h < 2; ++h) {
+                        const float f = at ? power_of<kUpK>(rk.par[h]) : 1.f;
+                        down_k[h] = down_of<kUpK>(f);
+                        if (t == 0) my_powers[g + 8 * h] = f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float f = power_of<kUpV>(rv.par[i]);
+                        down_v[i] = down_of<kUpV>(f);
+                        if (g == 0) my_powers[Z::kKeys + 2 * t + (i & 1) + (i >> 1) * 8] = f;
+                    }
                 }
-            }
-            {
-                uint8_t* place[8];
+                {
+                    uint8_t* place[8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) place[c] = sk + place_of * Z::kK + (k_at0 ^ (c << 4));
-                store_k<D>(place, rk, down_k);
+                    for (int c = 0; c < 8; ++c) place[c] = sk + place_of * Z::kK + (k_at0 ^ (c << 4));
+                    store_k<D>(place, rk, down_k);
+                }
+                for_tensor_cores();
+                if (lane == 0) gone[j & 3][w] = at == nullptr;
+                __syncwarp();
+                if (lane == 0) bar_arrive(k_full + 8 * place_of);
+                load_k<D>(next, g, t, rk);
+                if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+                {
+                    uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
+                    store_v<D>(place, rv, down_v);
+                }
+                for_tensor_cores();
+                __syncwarp();
+                if (lane == 0) bar_arrive(v_full + 8 * place_of);
+                load_v<D>(next ? next + v.s_kv : nullptr, valid(j + 1), g, t, rv);
+                at = next;
             }
-            for_tensor_cores();
-            if (__any_sync(0xffffffffu, out_of_range<kUpV>(largest_of(rv.par[0])) || out_of_range<kUpV>(largest_of(rv.par[1])) || out_of_range<kUpV>(largest_of(rv.par[2])) ||
-                                            out_of_range<kUpV>(largest_of(rv.par[3])))) {
-                mark |= kOwnV;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (g == 0) my_powers[Z::kKeys + 2 * t + (i & 1) + (i >> 1) * 8] = power_of<kUpV>(rv.par[i]);
-            }
-            if (lane == 0) marks[j & 3][w] = mark;
-            __syncwarp();
-            if (lane == 0) bar_arrive(k_full + 8 * place_of);
-            load_k<D>(next, g, t, rk);
-            if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead, a.tries);
-            float down_v[4] = {two_to(kUpV), two_to(kUpV), two_to(kUpV), two_to(kUpV)};
-            if (mark & kOwnV) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) down_v[i] = down_of<kUpV>(power_of<kUpV>(rv.par[i]));
-            }
-            {
-                uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
-                store_v<D>(place, rv, down_v);
-            }
-            for_tensor_cores();
-            __syncwarp();
-            if (lane == 0) bar_arrive(v_full + 8 * place_of);
-            load_v<D>(next ? next + v.s_kv : nullptr, valid(j + 1), g, t, rv);
-            at = next;
-        }
-    } else if (blocks > 0) {
+        };
+        if (odd) unpack(std::true_type());
+        else unpack(std::false_type());
+    } else {
         // ---- matrix instructions: one lane issues them, three wait for what they need at the same time ----
+        look(kUnpackWarps);
+        all_meet();
         const uint32_t leads = lane == 0;
         const int n = __shfl_sync(0xffffffffu, blocks, 0), live = __shfl_sync(0xffffffffu, mats, 0);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -704,9 +746,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                        v_low = operand_low((uint32_t)__cvta_generic_to_shared(sv));
         const auto given_up = [&] { return __any_sync(0xffffffffu, *static_cast<volatile int*>(&dead)) != 0; };
         uint32_t scored[2] = {0, 0}, summed[2] = {0, 0}, left_k = 0, left_v = 0;  // commits so far
-        bar_wait(q_full, 0, &dead, a.tries);
+        if (blocks > 0) bar_wait(q_full, 0, &dead, a.tries);
         __syncwarp();
-        bool go = !given_up();
+        bool go = blocks > 0 && !given_up();
 #pragma unroll 1
         for (int j = -1; go && j < n; ++j) {
             // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
