@@ -484,8 +484,8 @@ def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float
 
 
 def remp_kvq_set_wait_limit(tries: int) -> None:
-    """A test aid, for the whole process: polls of a barrier before remp_kvq_attend's thread blocks give up (0: none, negative: the
-    built-in limit). What gave up is NaN, and bit 4 of the batch's error word."""
+    """A test aid, for the whole process: how often a thread block of remp_kvq_attend for prompts polls for its queries before it
+    gives up (0: never, negative: the built-in limit). What gave up is NaN, and bit 4 of the batch's error word."""
     _lib.load().remp_kvq_set_wait_limit(tries)
 
 

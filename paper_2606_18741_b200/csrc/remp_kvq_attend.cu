@@ -35,9 +35,9 @@ constexpr float kSlack = 4.f;     // log2: a new reference leaves room for score
 // Steps below this are not looked at: p stays at or below 2^45, so that p*m of groups without a step (m up to 2^60 and more) and
 // their sums fit, and p*s of steps down to 2^-50 keeps its bits.
 constexpr float kTopStep = 0x1p-30f, kTopBound = 0x1p45f;
-// Rows up to which this kernel takes a sequence; above, the prompt kernel. Prompt / this one, us: rows x sequences x keys, 8 KV
-// heads: 17 x 1 x 4000 20.6 / 22.8, 24 x 16 x 2000 45.2 / 43.2, 20 x 64 x 500 63.6 / 51.3; 40 x 8 x 4000 49.3 / 57.4,
-// 64 x 64 x 1000 100.7 / 135.4.
+// Rows up to which this kernel takes a sequence; above, the prompt kernel. Prompt / this one, us in a graph: rows x sequences x
+// keys, 8 KV heads of 128 dims, 4 to 8 query heads for each: 24 x 16 x 2000 48.4 / 43.1, 20 x 64 x 500 69.8 / 51.3; 40 x 8 x
+// 4000 51.4 / 55.4, 64 x 64 x 1000 108.7 / 129.3.
 constexpr int kPromptRows = 32;
 constexpr int kStepTiles = 2, kStepTokens = kStepTiles * kKvqTile;
 

@@ -19,16 +19,17 @@
 // their columns of the tensor memory, O has its own. With 256 dims O takes so much of it that one matrix of 128 rows and
 // blocks of 64 keys are left.
 //
-// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 577 to 594 us in different
-// runs: 810 to 834 TFLOP/s, 50 to 51 % of a library product in bf16. Bound by the chain of one matrix, scores to P to products to
+// Measured: 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 481 GFLOP, 568 to 594 us in different
+// runs: 810 to 847 TFLOP/s, 50 to 52 % of a library product in bf16. Bound by the chain of one matrix, scores to P to products to
 // the next scores: some 4750 cycles for a block, 2700 of them from reading S to the last of P. Blocks of 64 keys with two S each,
-// which break the chain, took 779 us (both timed with clock reads in the kernel). Looking at
-// the parameters first takes 1 to 3 % (587 us without; 256 dims 562 and 567; 40 rows over 4000 keys 72 and 74); marks for each
-// tile inside the loops took up to 24 % (256 dims 695). With powers of their own the same call takes 0.96 ms.
+// which break the chain, took 779 us (both timed with clock reads in the kernel). Looking at the parameters first takes 1 to 4 %
+// (8 x 8 units of 40 rows over 4000 keys 51.4 us without, 52.4 with); marks for each tile inside the loops took up to 24 % (2 x
+// 1024 queries of 256 dims 562 to 695 us). With powers of their own the call above takes 0.79 ms.
 //
-// Every wait is on a barrier in shared memory and bounded. A block that gives up issues no more matrix instructions, goes on
-// without waiting, writes NaN and sets error bit 4. Whatever happens, the issuing warp leaves when everything that it has
-// issued is done and every barrier that it has committed to has been arrived at, so nothing runs on in freed memory.
+// Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
+// error bit 4. Whatever happens, the issuing warp leaves when everything that it has issued is done and every barrier that it
+// has committed to has been arrived at, so nothing runs on in freed memory. (Looking before each issue whether the block has
+// given up cost calls of few rows a third: the units above 49 to 66 us.)
 
 #include <atomic>
 #include <type_traits>
@@ -81,7 +82,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok;
 }
 // Bounded: a wait that runs out marks the block, and nothing in it waits any more.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int32_t tries) {
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int32_t tries = kWaitTries) {
     for (int32_t i = 0; i < tries; ++i) {
         if (bar_try(bar, parity)) return;
         if (*dead) return;
@@ -187,7 +188,7 @@ struct PromptArgs {
     uint32_t by_group;
     int32_t row_blocks;        // of a sequence and KV head at most
     int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
-    int32_t tries;             // of a wait
+    int32_t tries;             // of the wait for the queries
 };
 
 __device__ __forceinline__ int prompt_token(const PromptArgs& a, int row) { return a.by_group ? (int)__umulhi((uint32_t)row, a.by_group) : row; }
@@ -310,7 +311,7 @@ template <int D, bool BF>
 __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(const __grid_constant__ PromptArgs a) {
     using Z = Prompt<D>;
     extern __shared__ uint8_t smem_[];
-    __shared__ __align__(8) uint64_t bars[15];
+    __shared__ __align__(8) uint64_t bars[16];
     __shared__ uint32_t tmem_at;
     __shared__ int dead;
     __shared__ int is_last;
@@ -345,14 +346,14 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
     float* const powers = reinterpret_cast<float*>(sv + 2 * Z::kV);  // [block & 3][K, V][key]
     // blocks of K and V come and go (two places each); scores, probabilities and outputs of each matrix; queries
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
-    const uint32_t k_full = bar, k_free = bar + 16, v_full = bar + 32, v_free = bar + 48, s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, q_full = bar + 112;
+    const uint32_t k_full = bar, k_free = bar + 16, v_full = bar + 32, v_free = bar + 48, s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, q_full = bar + 112, all_done = bar + 120;
     const int mats = rows > kRowsM ? 2 : 1;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             bar_init(k_full + 8 * i, kUnpackWarps), bar_init(v_full + 8 * i, kUnpackWarps), bar_init(k_free + 8 * i, 1), bar_init(v_free + 8 * i, 1);
             bar_init(s_full + 8 * i, 1), bar_init(p_full + 8 * i, 4), bar_init(o_done + 8 * i, 1);
         }
-        bar_init(q_full, kSoftmaxWarps);
+        bar_init(q_full, kSoftmaxWarps), bar_init(all_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead = 0, is_last = 0, own_powers = 0;
         for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(gone[i]) = 0;
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             constexpr bool kOwn = decltype(own)::value;
 #pragma unroll 1
             for (int j = 0; j < (mat < mats ? blocks : 0); ++j) {
-                bar_wait(s_full + 8 * mat, j & 1, &dead, a.tries);
+                bar_wait(s_full + 8 * mat, j & 1, &dead);
                 __syncwarp();
                 tmem_after();
                 const int key0 = first_key + j * Z::kKeys;
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                         const float fall = exp2_approx(ref - now);
                         ref = now, sum *= fall;
                         if (j > 0) {
-                            bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead, a.tries);
+                            bar_wait(o_done + 8 * mat, (j - 1) & 1, &dead);
                             __syncwarp();
                             tmem_after();
 #pragma unroll 1
@@ -569,11 +570,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         else make_p(std::false_type());
         const bool some = blocks > 0 && mat < mats;
         if (some) {
-            bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead, a.tries);
+            bar_wait(o_done + 8 * mat, (blocks - 1) & 1, &dead);
             __syncwarp();
             tmem_after();
         }
-        // Whoever gave up said so before its next arrival, so no output that went wrong gets here without the mark.
+        // Whoever gave up said so before its next arrival, and outputs are behind all arrivals: none that went wrong gets here
+        // without the mark.
         if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
         uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
         if (splits == 1) {
@@ -693,7 +695,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
             for (int j = 0; j < blocks; ++j) {
                 const int place_of = j & 1, turn = (j >> 1) & 1;
                 const uint8_t* next = find(j + 1);
-                if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+                if (j > 1) bar_wait(k_free + 8 * place_of, turn ^ 1, &dead);
                 float down_k[2] = {two_to(kUpK), two_to(kUpK)}, down_v[4] = {two_to(kUpV), two_to(kUpV), two_to(kUpV), two_to(kUpV)};
                 if constexpr (kOwn) {  // told to the warps that make P before K is
                     float* const my_powers = powers + (j & 3) * 2 * Z::kKeys + w * kKvqTile;
@@ -721,7 +723,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                 __syncwarp();
                 if (lane == 0) bar_arrive(k_full + 8 * place_of);
                 load_k<D>(next, g, t, rk);
-                if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead, a.tries);
+                if (j > 1) bar_wait(v_free + 8 * place_of, turn ^ 1, &dead);
                 {
                     uint8_t* const place[2] = {sv + place_of * Z::kV + v_at0, sv + place_of * Z::kV + (v_at0 ^ 16)};
                     store_v<D>(place, rv, down_v);
@@ -744,42 +746,32 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const uint32_t q_low = operand_low((uint32_t)__cvta_generic_to_shared(sq)), k_low = operand_low((uint32_t)__cvta_generic_to_shared(sk)),
                        v_low = operand_low((uint32_t)__cvta_generic_to_shared(sv));
-        const auto given_up = [&] { return __any_sync(0xffffffffu, *static_cast<volatile int*>(&dead)) != 0; };
-        uint32_t scored[2] = {0, 0}, summed[2] = {0, 0}, left_k = 0, left_v = 0;  // commits so far
         if (blocks > 0) bar_wait(q_full, 0, &dead, a.tries);
         __syncwarp();
-        bool go = blocks > 0 && !given_up();
 #pragma unroll 1
-        for (int j = -1; go && j < n; ++j) {
+        for (int j = -1; j < n; ++j) {
             // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
             // the order of issue, so the scores may take the place of the probabilities before them.
             const uint32_t place = j & 1, next = place ^ 1;
             const uint32_t v_block = v_low + place * (Z::kV >> 4), k_block = k_low + next * (Z::kK >> 4);
             const bool values = j >= 0, scores = j + 1 < n;
             if (lane == 1 ? scores : values)
-                bar_wait(lane == 1 ? k_full + 8 * next : lane == 2 ? v_full + 8 * place : p_full, (lane == 1 ? j + 1 >> 1 : lane == 2 ? j >> 1 : j) & 1, &dead,
-                         a.tries);
+                bar_wait(lane == 1 ? k_full + 8 * next : lane == 2 ? v_full + 8 * place : p_full, (lane == 1 ? j + 1 >> 1 : lane == 2 ? j >> 1 : j) & 1, &dead);
             __syncwarp();
-            if (given_up()) break;
 #pragma unroll
             for (int mat = 0; mat < Z::kMats; ++mat) {
                 if (mat >= live) break;
                 const uint32_t s = tm + mat * Z::kKeys;
                 if (values) {
                     if (mat > 0) {
-                        bar_wait(p_full + 8 * mat, j & 1, &dead, a.tries);
+                        bar_wait(p_full + 8 * mat, j & 1, &dead);
                         __syncwarp();
-                        if (given_up()) {
-                            go = false;
-                            break;
-                        }
                     }
                     tmem_after();
 #pragma unroll
                     for (int k = 0; k < Z::kKeys / 16; ++k)
                         mma_tmem<D>(tm + Z::kO + mat * D, s + 8 * k, v_block + ((k / 4) * (D * 128) + (k % 4) * 32 >> 4), k ? 1 : j, leads);
                     commit_to(o_done + 8 * mat, leads);
-                    ++summed[mat];
                 }
                 if (scores) {
                     if (!values) tmem_after();
@@ -788,18 +780,20 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kvq_prompt_kernel(cons
                         mma_smem<Z::kKeys>(s, q_low + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
                                            k_block + ((k / 4) * (Z::kKeys * 128) + (k % 4) * 32 >> 4), k > 0, leads);
                     commit_to(s_full + 8 * mat, leads);
-                    ++scored[mat];
                 }
             }
-            if (go && values) commit_to(v_free + 8 * place, leads), ++left_v;
-            if (go && scores) commit_to(k_free + 8 * next, leads), ++left_k;
+            if (values) commit_to(v_free + 8 * place, leads);
+            if (scores) commit_to(k_free + 8 * next, leads);
         }
-        // Nothing stays in flight, whatever happened. A block of keys is issued when its place has been left, so each barrier is
-        // at most one phase behind. Block b is in place b & 1.
+        // Nothing stays in flight, whatever happened: a barrier of its own stands behind everything, since a block that gave up may
+        // have run ahead of the others by several phases. Then the last arrival on each of these; block b is in place b & 1.
+        __syncwarp();
+        commit_to(all_done, leads);
+        bar_drain(all_done, 1, &dead);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            bar_drain(s_full + 8 * i, scored[i], &dead), bar_drain(o_done + 8 * i, summed[i], &dead);
-            bar_drain(k_free + 8 * i, (left_k + 1 - i) >> 1, &dead), bar_drain(v_free + 8 * i, (left_v + 1 - i) >> 1, &dead);
+            if (i < live) bar_drain(s_full + 8 * i, n, &dead), bar_drain(o_done + 8 * i, n, &dead);
+            bar_drain(k_free + 8 * i, (n + 1 - i) >> 1, &dead), bar_drain(v_free + 8 * i, (n + 1 - i) >> 1, &dead);
         }
         __syncwarp();
     }
