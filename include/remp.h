@@ -327,7 +327,7 @@ remp_status remp_weights_reshard(const remp_topo* topo, int32_t num_layers, cons
  * for s*c + m with codes c of 0 to 15:
  *     m = largest bfloat16 <= min x,  s = smallest bfloat16 >= min((max x - m) * (1/15), 65280),  c = clamp(rint((x - m) / s), 0, 15)
  * (all in 32 bits, 1/15 too; rint to nearest even; s = 0: every code is 0), so the codes span every value and none is
- * off by more than s/2. A group that holds a NaN or an infinity is kept as
+ * off by more than s/2 (in groups wider than 15 * 65280 the upper values are: their step stays 65280). A group that holds a NaN or an infinity is kept as
  * m = NaN, s = 0: it stands for NaN in every dim. Rows take remp_kvq_token_bytes(head_dim) = head_dim/2 + head_dim/16
  * bytes for each of K and V, 3.6 times fewer than in 16 bits.
  * A head slice (one block, one head, K or V) is block_size/16 tiles of 16 tokens, each [16][head_dim/2] bytes of codes
@@ -408,10 +408,12 @@ remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_batch* batch
  *   lse        DEVICE float [num_tokens][q_heads] or NULL: natural logarithm of the sum of exp(scale * q.k)
  *   workspace  DEVICE, remp_kvq_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call
  *              leaves it ready for the next. Calls that may overlap need workspaces of their own.
- * With at most 32 rows (max_queries * q_heads / kv_heads) keys and values are used as the codes stand for them; with more,
- * they are rounded to 11 bits on the way, of any size up to 2^110 (dims below 2^-24 of their token's largest to fewer). A NaN in V reaches every row of its sequence that the call computes
- * together with it, also rows whose mask hides it; a NaN in K or in a query only what sees it. 2^30 steps of 32 tokens of
- * a KV head (4 TB of cache) and more are refused on the device (bit 2); where a wait runs out the outputs are NaN (bit 4).
+ * With at most 32 rows (max_queries * q_heads / kv_heads) keys and values are used as the codes stand for them, and products of a
+ * probability and a step are rounded to 11 bits (of steps below 2^-50 to fewer); with more, keys, values and probabilities are, of any size up to 2^110 (dims
+ * below 2^-24 of their token's largest to fewer). Queries count exactly from 2^-107 up, as long as scale * 2^120 is finite.
+ * A NaN in V reaches every row of its sequence that the call computes together with it, also rows whose mask hides it; a NaN in
+ * K or in a query only what sees it. 2^30 steps of 32 tokens of a KV head (4 TB of cache) and more are refused on the device
+ * (bit 2); where a wait runs out the outputs are NaN (bit 4).
  * The result does not depend on the order in which thread blocks run. */
 int64_t remp_kvq_workspace_bytes(void);
 remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
