@@ -9,8 +9,8 @@
 namespace remp {
 
 #ifdef __CUDACC__
-// First thing in such a kernel: the one before it has to be complete. Kernels that write caches, tables or counts stop here:
-// the next kernel is then set up when they are done, with nothing stale in its first-level cache.
+// First thing in such a kernel: the one before it has to be complete, and what it has written is visible then. Kernels that write
+// caches, tables or counts stop here: the next kernel is set up when they are done.
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Kernels that only read those let the next one be set up now.
 __device__ __forceinline__ void grid_begin() {
