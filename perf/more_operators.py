@@ -266,7 +266,7 @@ def _prepare_verify(s, host, dev):
     count = _spread(n, 2 * s["drafts"], host, 0)
     start = torch.cat((torch.zeros(1, dtype=torch.long), count.cumsum(0)))
     total = int(start[-1])
-    s["draft_start"], s["most"], s["total"] = start.int().cuda(), int(count.max()), total
+    s["draft_start"], s["total"] = start.int().cuda(), total
     # the drafting model's logits are near the target's
     logits = torch.randn(total + n, vocab, generator=dev, device="cuda") * 2.5
     s["target"] = torch.softmax(logits, -1).to(kind)
@@ -323,8 +323,7 @@ def _own_evict(s):
 
 def _own_verify(s):
     import paper_2606_18741_b200 as remp
-    remp.remp_draft_verify(s["draft_start"], s["drafted"], s["target"], s["draft"], s["accept"], s["pick"], s["out"], s["accepted"],
-                           max_drafts=s["most"])
+    remp.remp_draft_verify(s["draft_start"], s["drafted"], s["target"], s["draft"], s["accept"], s["pick"], s["out"], s["accepted"])
     return {"tokens": s["out"], "accepted": s["accepted"]}
 
 
