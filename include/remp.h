@@ -340,7 +340,7 @@ remp_status remp_weights_reshard(const remp_topo* topo, int32_t num_layers, cons
  * head_dim is 64, 128 or 256; block_size a multiple of 16. */
 int64_t remp_kvq_token_bytes(int32_t head_dim); /* or REMP_ERR_SHAPE */
 
-typedef enum { REMP_DTYPE_BFLOAT = 1, REMP_DTYPE_HALF = 2 } remp_dtype; /* bfloat16, IEEE half: 16 bits each */
+typedef enum { REMP_DTYPE_BFLOAT = 1, REMP_DTYPE_HALF = 2, REMP_DTYPE_FLOAT = 3 } remp_dtype; /* bfloat16, IEEE half: 16 bits each; 32 bits (remp_draft_verify) */
 
 /* One layer of a rank's 4-bit pool. shard: strides as in remp_shard, 0 = dense (stride_token must be dense). */
 typedef struct {
@@ -424,6 +424,86 @@ remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* bat
  * arrive at before it gives up (0: never; negative: the built-in limit). It then waits for nothing else, writes NaN to its
  * outputs and sets error bit 4. */
 void remp_kvq_set_wait_limit(int32_t tries);
+
+/* ---- serving from a cache of 16-bit values, between two topology switches ----
+ *
+ * A rank's pool as remp_shard describes it, with rows of head_dim values of 16 bits (elem_bytes 2), as remp_migrate_kv moves it:
+ * any strides that keep rows disjoint, so head-major and token-major blocks alike. head_dim is 64, 128 or 256; block_size a
+ * multiple of 16. The batch, the rows and the transform are those of the 4-bit cache. */
+typedef remp_kvq_pool remp_kv_pool;
+
+/* Write new tokens: norm and rotation of q and k, k and v into their pages, one pass and one launch. Arguments and error bits as
+ * for remp_kvq_append; q, q_out, k, v and the cache are of `dtype`, the transform works in 32 bits, what it leaves is rounded
+ * once; v, and without a transform q and k, are copied bit for bit. */
+remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
+                           const remp_kvq_rows* k, const remp_kvq_rows* v, const remp_kvq_rows* q_out, int32_t q_heads,
+                           int32_t dtype, const remp_kvq_transform* transform, void* stream);
+
+/* Attention over the cache: out = softmax(scale * q.K^T).V for every row of the batch. A row at position p sees the positions
+ * j <= p; with window > 0 those with j > p - window or j < first (the first tokens stay visible; window = 0: all, whatever
+ * `first` is). Heads, errors, lse, rows that see nothing and lengths beyond the table row as for remp_kvq_attend. Slots that no
+ * row of a sequence sees are not used and may hold anything; a NaN or an infinity in V that a row of the batch sees may reach the other rows of
+ * its sequence and KV head that the call computes together with it.
+ *   scale      positive
+ *   lse        DEVICE float [num_tokens][q_heads] or NULL
+ *   workspace  DEVICE, remp_kv_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call leaves it
+ *              ready for the next. Calls that may overlap need workspaces of their own.
+ * The result does not depend on the order in which thread blocks run. */
+int64_t remp_kv_workspace_bytes(void);
+remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
+                           const remp_kvq_rows* out, int32_t q_heads, int32_t dtype, float scale, int32_t window,
+                           int32_t first, float* lse, void* workspace, void* stream);
+
+/* The weight that attention gives to each cached position, added up over the rows of the batch and the query heads of each
+ * KV head: weights[s][h][j] += sum of exp(scale * q.k_j - lse) over the rows that see j (as in remp_kv_attend). Positions that the call's own
+ * rows stand at are new: their weight is set, not added to; with fresh != 0 that of every position of a sequence with rows is. Other elements are
+ * left as they are.
+ *   lse      DEVICE float [num_tokens][q_heads], as remp_kv_attend gives it; rows with -infinity count nothing
+ *   weights  DEVICE float [num_seqs][kv_heads][stride]; of sequences longer than `stride` the positions behind it are left out
+ *            (error bit 1)
+ * Each weight is added up by one warp in a fixed order. */
+remp_status remp_kv_weigh(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q, int32_t q_heads,
+                          int32_t dtype, float scale, int32_t window, int32_t first, const float* lse, float* weights,
+                          int64_t stride, int32_t fresh, void* stream);
+
+/* Eviction by accumulated weight: of every sequence longer than keep[s] tokens keep[s] stay, for each KV head its own choice - the
+ * first `first` tokens, the last `recent` (as far as keep[s] goes, first tokens before recent ones), and of the others those
+ * with the largest weights (of equal ones the lowest positions; NaN counts as the least). What stays keeps its order: row i
+ * of the head becomes the i-th position that stays, for K, V and weights_out. Lengths and tables are the caller's to change (min(seq_lens[s],
+ * keep[s]), the same for every head and layer): blocks behind them are free, rows behind the new length keep their bytes.
+ *   tables       blocks of an evicted sequence must not be shared with another (fork copies the last one only)
+ *   keep         DEVICE int32 [num_seqs]
+ *   weights      DEVICE float [num_seqs][kv_heads][stride]
+ *   weights_out  DEVICE, the same shape; may be weights. Elements behind the new length are left as they are
+ *   kept         DEVICE int32 [num_seqs][kv_heads][kept_stride], written: the positions that stay, ascending, -1 behind them
+ *   max_tokens   no sequence is longer (chooses the kernel); at most 2^18 and at most stride
+ *   error        DEVICE word or NULL: bit 1 a length or keep[s] negative, a length beyond max_tokens or the table row, or more
+ *                to keep than kept_stride: the sequence stays as it is and its rows of `kept` are -1; bit 3 block id outside
+ *                the pool: rows that would move from or to it are left out */
+remp_status remp_kv_evict(const remp_kv_pool* pool, const remp_block_tables* tables, const int32_t* keep, int32_t first,
+                          int32_t recent, const float* weights, float* weights_out, int64_t stride, int32_t* kept,
+                          int32_t kept_stride, int32_t max_tokens, uint32_t* error, void* stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers. Draft i of a sequence, token x,
+ * is accepted if all before it are and accept[i] * q(x) < p(x), with q = 1 without draft probabilities. At the first draft that is not,
+ * a token is drawn from max(p - q, 0) (without draft probabilities: from p without x; where all of these are 0: from p); behind the
+ * last draft, from p: the smallest j with sum of w_i over i <= j > pick[s] * sum of all w, in 64 bits. Probabilities need not sum to 1;
+ * NaN and negative ones count as 0; if no j has such a sum, the last with w > 0 is taken.
+ *   draft_start  DEVICE int32 [num_seqs + 1], ascending from 0: sequence s has drafts draft_start[s] to draft_start[s+1] - 1
+ *   drafts       DEVICE int32 [num_drafts]
+ *   target       DEVICE [num_drafts + num_seqs][target_stride] of dtype: sequence s has rows draft_start[s] + s and on, one
+ *                for each draft and one behind the last
+ *   draft_probs  DEVICE [num_drafts][draft_stride] of dtype, or NULL
+ *   accept, pick DEVICE float [num_drafts], [num_seqs], in [0, 1)
+ *   tokens       DEVICE int32 [num_drafts + num_seqs], written: from draft_start[s] + s on the accepted drafts, the token drawn, -1 behind
+ *   accepted     DEVICE int32 [num_seqs], written: drafts accepted
+ *   error        DEVICE word or NULL: bit 1 a draft outside the vocabulary (it is not accepted) or draft_start outside
+ *                [0, num_drafts] or descending (cut to it); bit 2 no probability above 0 to draw from (the token is -1)
+ *   dtype        REMP_DTYPE_FLOAT, _BFLOAT or _HALF; strides in elements */
+remp_status remp_draft_verify(int32_t num_seqs, int32_t num_drafts, int32_t vocab, const int32_t* draft_start,
+                              const int32_t* drafts, const void* target, int64_t target_stride, const void* draft_probs,
+                              int64_t draft_stride, int32_t dtype, const float* accept, const float* pick, int32_t* tokens,
+                              int32_t* accepted, uint32_t* error, void* stream);
 
 /* ---- pages between two switches: fork, free, compact, copy ----
  *

@@ -13,7 +13,8 @@ EXPORTS = (
     "remp_plan_destroy", "remp_last_error", "remp_plan_num_items", "remp_plan_get_items", "remp_plan_traffic",
     "remp_plan_set_option", "remp_kernel_launch_count", "remp_remap_tables_noalloc", "remp_reshard_host", "remp_migrate_kv_layers", "remp_alloc_dst_blocks_preempt", "remp_alloc_dst_blocks_shared", "remp_plan_traffic_tokens", "remp_release_cached_memory", "remp_rank_ownership", "remp_plan_partition", "remp_migrate_kv_exchange", "remp_weight_shard_bytes", "remp_weight_slice",
     "remp_weights_reshard", "remp_kvq_token_bytes", "remp_kvq_append", "remp_kvq_read", "remp_kvq_attend",
-    "remp_kvq_workspace_bytes", "remp_kvq_set_wait_limit", "remp_pages_fork", "remp_pages_free", "remp_pages_compact", "remp_pages_copy",
+    "remp_kvq_workspace_bytes", "remp_kvq_set_wait_limit", "remp_kv_append", "remp_kv_attend", "remp_kv_workspace_bytes",
+    "remp_kv_weigh", "remp_kv_evict", "remp_draft_verify", "remp_pages_fork", "remp_pages_free", "remp_pages_compact", "remp_pages_copy",
 )
 
 
@@ -152,6 +153,21 @@ def load():
     L.remp_kvq_workspace_bytes.restype = C.c_int64
     L.remp_kvq_set_wait_limit.argtypes = [C.c_int32]
     L.remp_kvq_set_wait_limit.restype = None
+    L.remp_kv_append.argtypes = L.remp_kvq_append.argtypes
+    L.remp_kv_append.restype = C.c_int
+    L.remp_kv_attend.argtypes = [P(RempKvqPool), P(RempKvqBatch), P(RempKvqRows), P(RempKvqRows), C.c_int32, C.c_int32,
+                                 C.c_float, C.c_int32, C.c_int32, V, V, V]
+    L.remp_kv_attend.restype = C.c_int
+    L.remp_kv_workspace_bytes.argtypes = []
+    L.remp_kv_workspace_bytes.restype = C.c_int64
+    L.remp_kv_weigh.argtypes = [P(RempKvqPool), P(RempKvqBatch), P(RempKvqRows), C.c_int32, C.c_int32, C.c_float, C.c_int32,
+                                C.c_int32, V, V, C.c_int64, C.c_int32, V]
+    L.remp_kv_weigh.restype = C.c_int
+    L.remp_kv_evict.argtypes = [P(RempKvqPool), P(RempBlockTables), V, C.c_int32, C.c_int32, V, V, C.c_int64, V, C.c_int32,
+                                C.c_int32, V, V]
+    L.remp_kv_evict.restype = C.c_int
+    L.remp_draft_verify.argtypes = [C.c_int32, C.c_int32, C.c_int32, V, V, V, C.c_int64, V, C.c_int64, C.c_int32, V, V, V, V, V, V]
+    L.remp_draft_verify.restype = C.c_int
     L.remp_pages_fork.argtypes = [V, V, C.c_int32, C.c_int32, C.c_int32, V, V, C.c_int32, V, V, C.c_int32, V, V, V]
     L.remp_pages_fork.restype = C.c_int
     L.remp_pages_free.argtypes = [V, V, C.c_int32, C.c_int32, C.c_int32, V, V, C.c_int32, V, V, V, V, V]

@@ -354,7 +354,7 @@ def remp_weights_reshard(topo, num_layers: int, params, dst_shards, stream=None,
 
 # ---- serving from a cache held in 4 bits ----
 
-REMP_DTYPE_BFLOAT, REMP_DTYPE_HALF = 1, 2
+REMP_DTYPE_BFLOAT, REMP_DTYPE_HALF, REMP_DTYPE_FLOAT = 1, 2, 3
 
 
 def remp_kvq_token_bytes(head_dim: int) -> int:
@@ -402,8 +402,12 @@ def make_kvq_batch(seq_lens, block_tables, query_start, num_tokens: int, max_que
 def make_kvq_workspace(device=None):
     """The zeroed workspace that remp_kvq_attend wants (a CUDA uint8 tensor); one for each stream. Waits for the current
     stream, so that the zeros are there for every other (not while a graph is captured: there it belongs to the graph's stream)."""
+    return _zeroed(_workspace_bytes(), device)
+
+
+def _zeroed(nbytes: int, device):
     import torch
-    workspace = torch.zeros(int(_lib.load().remp_kvq_workspace_bytes()), dtype=torch.uint8, device=device or "cuda")
+    workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device or "cuda")
     if not torch.cuda.is_current_stream_capturing():
         torch.cuda.current_stream(workspace.device).synchronize()
     return workspace
@@ -433,8 +437,12 @@ def remp_kvq_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_no
     [head_dim] CUDA tensors of one 16-bit type, any token and head strides (q and q_out may be None, or the same
     tensor); q_norm, k_norm: float32 [head_dim]; rope: float32 [rows][rotary_dim], cosines then sines; positions: int32
     [num_tokens] rows of rope (default: the token's position). Only enqueues."""
-    n, d = batch.num_tokens, pool.head_dim
-    dtype = k.dtype
+    _check(_lib.load().remp_kvq_append(*_append_args(pool, batch, q, k, v, q_out, q_norm, k_norm, eps, rope, interleaved, positions),
+                                       _stream_ptr(stream)))
+
+
+def _append_args(pool, batch, q, k, v, q_out, q_norm, k_norm, eps, rope, interleaved, positions):
+    n, d, dtype = batch.num_tokens, pool.head_dim, k.dtype
     if dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "k must be bfloat16 or float16")
     heads = int(q.shape[1]) if q is not None else 0
@@ -446,11 +454,9 @@ def remp_kvq_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_no
         tr = RempKvqTransform(_f32_cuda(q_norm, "q_norm", d), _f32_cuda(k_norm, "k_norm", d), _f32_cuda(rope, "rope"),
                               _int32_cuda(positions, "positions") if positions is not None else None, eps, rows, dim,
                               int(interleaved))
-    _check(_lib.load().remp_kvq_append(
-        pool, batch, _rows(q, "q", n, heads, d, dtype) if q is not None else None, _rows(k, "k", n, pool.kv_heads, d, dtype),
-        _rows(v, "v", n, pool.kv_heads, d, dtype),
-        _rows(q_out, "q_out", n, heads, d, dtype) if q_out is not None else None, heads, _types()[2][dtype], tr,
-        _stream_ptr(stream)))
+    return (pool, batch, _rows(q, "q", n, heads, d, dtype) if q is not None else None, _rows(k, "k", n, pool.kv_heads, d, dtype),
+            _rows(v, "v", n, pool.kv_heads, d, dtype), _rows(q_out, "q_out", n, heads, d, dtype) if q_out is not None else None,
+            heads, _types()[2][dtype], tr)
 
 
 def remp_kvq_read(pool: RempKvqPool, batch: RempKvqBatch, k_out, v_out, stream=None) -> None:
@@ -492,6 +498,118 @@ def remp_kvq_set_wait_limit(tries: int) -> None:
 @functools.lru_cache(maxsize=None)
 def _workspace_bytes() -> int:
     return int(_lib.load().remp_kvq_workspace_bytes())
+
+
+# ---- serving from a cache of 16-bit values ----
+
+def make_kv_pool(buffer, num_blocks: int, kv_heads: int, head_dim: int, block_size: int, layer: int = 0,
+                 strides: Optional[dict] = None) -> RempKvqPool:
+    """remp_kv_pool of one layer of a rank's pool of 16-bit values (a CUDA tensor; strides in bytes as for make_shards). Its
+    calls take the batches of make_kvq_batch."""
+    return make_kvq_pool(buffer, num_blocks, kv_heads, head_dim, block_size, layer, strides)
+
+
+@functools.lru_cache(maxsize=None)
+def _kv_workspace_bytes() -> int:
+    return int(_lib.load().remp_kv_workspace_bytes())
+
+
+def make_kv_workspace(device=None):
+    """The zeroed workspace that remp_kv_attend wants; one for each stream. As make_kvq_workspace."""
+    return _zeroed(_kv_workspace_bytes(), device)
+
+
+def remp_kv_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6,
+                   rope=None, interleaved: bool = False, positions=None, stream=None) -> None:
+    """Norm and rotation of q and k, k and v into their pages. Arguments as for remp_kvq_append; the cache is of the tensors'
+    type. Only enqueues."""
+    _check(_lib.load().remp_kv_append(*_append_args(pool, batch, q, k, v, q_out, q_norm, k_norm, eps, rope, interleaved, positions),
+                                      _stream_ptr(stream)))
+
+
+def remp_kv_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float, workspace, window: int = 0, first: int = 0,
+                   lse=None, stream=None) -> None:
+    """Causal attention of q [num_tokens][heads][head_dim] over the cached positions of each sequence, into out (same
+    shape); window > 0: over the last `window` positions and the `first` ones. lse: float32 [num_tokens][heads] or None.
+    workspace: make_kv_workspace(). Only enqueues."""
+    n, d, dtype = batch.num_tokens, pool.head_dim, q.dtype
+    if dtype not in _types()[2]:
+        raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
+    heads = q.shape[1]
+    if not workspace.is_cuda or workspace.nbytes < _kv_workspace_bytes():
+        raise RempError(REMP_ERR_INVALID_ARG, "the workspace is too small")
+    _check(_lib.load().remp_kv_attend(pool, batch, _rows(q, "q", n, heads, d, dtype), _rows(out, "out", n, heads, d, dtype), heads,
+                                      _types()[2][dtype], scale, window, first, _f32_cuda(lse, "lse", n, heads),
+                                      workspace.data_ptr(), _stream_ptr(stream)))
+
+
+def _weights(t, name: str, num_seqs: int, heads: int):
+    if t.dim() != 3 or t.shape[0] != num_seqs or t.shape[1] != heads:
+        raise RempError(REMP_ERR_SHAPE, f"{name} must be [{num_seqs}][{heads}][positions]")
+    return _f32_cuda(t, name) or None
+
+
+def remp_kv_weigh(pool: RempKvqPool, batch: RempKvqBatch, q, lse, weights, scale: float, window: int = 0, first: int = 0,
+                  fresh: bool = False, stream=None) -> None:
+    """weights (float32 [num_seqs][kv_heads][positions]) += the attention weight that the rows q [num_tokens][heads][head_dim]
+    give to every cached position they see; lse: float32 [num_tokens][heads] of remp_kv_attend with the same scale, window and first. Positions
+    of the rows themselves, and with `fresh` all of the batch's sequences, are set instead. Only enqueues."""
+    n, d = batch.num_tokens, pool.head_dim
+    if q.dtype not in _types()[2]:
+        raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
+    heads = q.shape[1]
+    _check(_lib.load().remp_kv_weigh(pool, batch, _rows(q, "q", n, heads, d, q.dtype), heads, _types()[2][q.dtype], scale, window, first,
+                                     _f32_cuda(lse, "lse", n, heads), _weights(weights, "weights", batch.tables.num_seqs, pool.kv_heads),
+                                     weights.shape[2], int(fresh), _stream_ptr(stream)))
+
+
+def remp_kv_evict(pool: RempKvqPool, seq_lens, block_tables, keep, weights, weights_out, kept, first: int = 0, recent: int = 0,
+                  max_tokens: Optional[int] = None, error=None, stream=None) -> None:
+    """Of every sequence longer than keep[s] (int32 [n]) the first `first`, the last `recent` and the heaviest tokens stay, keep[s] in
+    all, for each KV head its own; rows of K and V move to the front in their order, weights (float32 [n][kv_heads][positions])
+    to weights_out (may be weights). kept: int32 [n][kv_heads][most], the positions that stay, -1 behind them. max_tokens: no
+    sequence is longer (default: what weights hold, at most 2^18). Lengths and tables stay as they are. Only enqueues."""
+    lens, tabs, n, width = _tables_of(seq_lens, block_tables)
+    w = _weights(weights, "weights", n, pool.kv_heads)
+    if weights_out.shape != weights.shape:
+        raise RempError(REMP_ERR_SHAPE, "weights_out must have the shape of weights")
+    if kept.dim() != 3 or kept.shape[0] != n or kept.shape[1] != pool.kv_heads:
+        raise RempError(REMP_ERR_SHAPE, f"kept must be [{n}][{pool.kv_heads}][most]")
+    positions = weights.shape[2]
+    _check(_lib.load().remp_kv_evict(pool, RempBlockTables(n, width, lens, tabs), _same(keep, seq_lens, "keep"), first, recent, w,
+                                     _f32_cuda(weights_out, "weights_out"), positions, _int32_cuda(kept, "kept") or None, kept.shape[2],
+                                     min(positions, 1 << 18) if max_tokens is None else max_tokens,
+                                     _int32_cuda(error, "error") if error is not None else None, _stream_ptr(stream)))
+
+
+def _probabilities(t, name: str, rows: int, vocab: int, dtype):
+    if not t.is_cuda or t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != vocab or (vocab > 1 and t.stride(1) != 1):
+        raise RempError(REMP_ERR_SHAPE, f"{name} must be a CUDA tensor [{rows}][{vocab}] of {dtype} with dense rows")
+    return t.data_ptr() or None
+
+
+def remp_draft_verify(draft_start, drafts, target, draft_probs, accept, pick, tokens, accepted, error=None,
+                      stream=None) -> None:
+    """Verify drafts (int32 [m]; sequence s has draft_start[s] to draft_start[s + 1]) against target [m + n][vocab] (float32, bfloat16 or
+    float16; a row for each draft and one behind the last of each sequence) and the probabilities that they were drawn with,
+    draft_probs [m][vocab] (None: they were not drawn), by the random numbers accept [m] and pick [n] (float32 in [0, 1)).
+    tokens: int32 [m + n], for each sequence the accepted drafts, the token drawn behind them, -1 for the rest; accepted: int32 [n].
+    Only enqueues."""
+    n, m, vocab = int(accepted.shape[0]), int(drafts.shape[0]), int(target.shape[-1])
+    kind = {**_types()[2], _types()[1]: REMP_DTYPE_FLOAT}.get(target.dtype)
+    if kind is None:
+        raise RempError(REMP_ERR_INVALID_ARG, "probabilities must be float32, bfloat16 or float16")
+    if int(draft_start.shape[0]) != n + 1:
+        raise RempError(REMP_ERR_INVALID_ARG, "draft_start must be [n + 1]")
+    rows = _probabilities(target, "target", m + n, vocab, target.dtype)
+    given = _probabilities(draft_probs, "draft_probs", m, vocab, target.dtype) if draft_probs is not None else None
+    if tokens.numel() != m + n:
+        raise RempError(REMP_ERR_INVALID_ARG, "tokens must be [m + n]")
+    _check(_lib.load().remp_draft_verify(n, m, vocab, _int32_cuda(draft_start, "draft_start"), _int32_cuda(drafts, "drafts") or None, rows,
+                                         target.stride(0), given, draft_probs.stride(0) if draft_probs is not None else 0, kind,
+                                         _f32_cuda(accept, "accept", m) or None, _f32_cuda(pick, "pick", n), _int32_cuda(tokens, "tokens"),
+                                         _int32_cuda(accepted, "accepted"), _int32_cuda(error, "error") if error is not None else None,
+                                         _stream_ptr(stream)))
 
 
 # ---- pages between two switches ----

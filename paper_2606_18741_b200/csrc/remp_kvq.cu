@@ -18,8 +18,8 @@
 
 #include <algorithm>
 
-#include "remp_kvq.h"
 #include "remp_launch.h"
+#include "remp_rows.h"
 
 namespace remp {
 
@@ -28,15 +28,6 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int kSets = 4;
-
-struct Transform {
-    const float* q_norm;
-    const float* k_norm;
-    const float* rope;
-    const int32_t* positions;
-    float eps;
-    int32_t rope_rows, rotary_dim, interleaved;
-};
 
 struct Slot {  // where a token's codes are
     int64_t off;   // bytes from the pool's base to its tile (of head 0, K)
@@ -61,36 +52,6 @@ __device__ __forceinline__ Slot find_slot(const KvqView& v, int token, int tile_
     r.stored = block >= 0 && block < v.nb;
     r.off = (int64_t)block * v.s_block + (int64_t)((int)tile - in_row * v.block_tiles) * tile_bytes;
     return r;
-}
-
-template <bool BF>
-__device__ __forceinline__ void unpack8(const uint4& raw, float (&x)[8]) {
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (BF) {
-            x[2 * i] = bf_low(w[i]), x[2 * i + 1] = bf_high(w[i]);
-        } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            x[2 * i] = f.x, x[2 * i + 1] = f.y;
-        }
-    }
-}
-
-template <bool BF>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (BF) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        } else {
-            const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // One step of a transpose between lanes and nibbles: lane bit `s` changes places with nibble-index bit `s`.
@@ -383,15 +344,20 @@ remp_status kvq_view(const remp_kvq_pool* pool, const remp_kvq_batch* batch, Kvq
     if (remp_status st = resolve_shard(pool->shard, T, 1, m, &s)) return st;
     if (s.s_head < pool->block_size * tb) return fail(REMP_ERR_SHAPE, "stride_head must hold a head slice");
     if (s.nb > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "block ids are 32-bit");
+    if (remp_status st = kvq_batch_view(batch, v)) return st;
+    v->base = reinterpret_cast<uint8_t*>(s.base + (uint64_t)((int64_t)pool->layer * s.s_layer));
+    v->s_kv = s.s_kv, v->s_block = s.s_block, v->s_head = s.s_head;
+    v->nb = (int32_t)s.nb, v->kv_heads = pool->kv_heads, v->block_tiles = pool->block_size / kKvqTile;
+    return REMP_OK;
+}
+
+remp_status kvq_batch_view(const remp_kvq_batch* batch, KvqView* v) {
     const remp_block_tables& bt = batch->tables;
     if (bt.num_seqs < 0 || bt.max_blocks_per_seq < 0 || batch->num_tokens < 0 || batch->max_queries < 0)
         return fail(REMP_ERR_INVALID_ARG, "negative batch dimensions");
     if (bt.num_seqs > kKvqMost || batch->num_tokens > kKvqMost) return fail(REMP_ERR_SHAPE, "too many sequences or tokens");
     if (batch->num_tokens > 0 && (!bt.seq_lens || !batch->query_start || (bt.max_blocks_per_seq > 0 && !bt.block_tables)))
         return fail(REMP_ERR_INVALID_ARG, "null seq_lens, block_tables or query_start");
-    v->base = reinterpret_cast<uint8_t*>(s.base + (uint64_t)((int64_t)pool->layer * s.s_layer));
-    v->s_kv = s.s_kv, v->s_block = s.s_block, v->s_head = s.s_head;
-    v->nb = (int32_t)s.nb, v->kv_heads = pool->kv_heads, v->block_tiles = pool->block_size / kKvqTile;
     v->max_blocks = bt.max_blocks_per_seq, v->num_seqs = bt.num_seqs, v->num_tokens = bt.num_seqs ? batch->num_tokens : 0;
     v->seq_lens = bt.seq_lens, v->tables = bt.block_tables, v->query_start = batch->query_start;
     v->error = batch->error;
@@ -411,7 +377,21 @@ remp_status kvq_rows(const remp_kvq_rows* r, int32_t tokens, int32_t heads, int3
     return REMP_OK;
 }
 
-static remp_status check_dtype(int32_t dtype) {
+remp_status kvq_transform(const remp_kvq_transform* transform, int32_t head_dim, Transform* tr) {
+    *tr = Transform{nullptr, nullptr, nullptr, nullptr, 0.f, 0, 0, 0};
+    if (!transform) return REMP_OK;
+    *tr = Transform{transform->q_norm, transform->k_norm, transform->rope, transform->positions, transform->eps,
+                    transform->rope_rows, transform->rotary_dim, transform->interleaved};
+    if ((reinterpret_cast<uint64_t>(tr->q_norm) | reinterpret_cast<uint64_t>(tr->k_norm) | reinterpret_cast<uint64_t>(tr->rope)) & 15)
+        return fail(REMP_ERR_SHAPE, "norm weights and the rotation table must be 16-byte aligned");
+    if (!(tr->eps >= 0.f)) return fail(REMP_ERR_INVALID_ARG, "eps must not be negative");
+    if (tr->rope && (tr->rotary_dim < 16 || tr->rotary_dim % 16 || tr->rotary_dim > head_dim || tr->rope_rows < 0))
+        return fail(REMP_ERR_SHAPE, "rotary_dim must be a multiple of 16 and at most head_dim");
+    if (!tr->rope) tr->rotary_dim = 0;
+    return REMP_OK;
+}
+
+remp_status kvq_dtype(int32_t dtype) {
     return dtype == REMP_DTYPE_BFLOAT || dtype == REMP_DTYPE_HALF ? REMP_OK : fail(REMP_ERR_INVALID_ARG, "unknown dtype");
 }
 
@@ -432,21 +412,12 @@ extern "C" remp_status remp_kvq_append(const remp_kvq_pool* pool, const remp_kvq
     KvqView view;
     KvqRows rq{nullptr, 0, 0}, rk, rv, ro{nullptr, 0, 0};
     if (remp_status st = kvq_view(pool, batch, &view)) return st;
-    if (remp_status st = check_dtype(dtype)) return st;
+    if (remp_status st = kvq_dtype(dtype)) return st;
     const int32_t d = pool->head_dim;
     if (q_heads < 0 || (q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr))
         return fail(REMP_ERR_INVALID_ARG, "q, q_out and q_heads go together");
-    Transform tr{nullptr, nullptr, nullptr, nullptr, 0.f, 0, 0, 0};
-    if (transform) {
-        tr = Transform{transform->q_norm, transform->k_norm, transform->rope, transform->positions, transform->eps,
-                       transform->rope_rows, transform->rotary_dim, transform->interleaved};
-        if ((reinterpret_cast<uint64_t>(tr.q_norm) | reinterpret_cast<uint64_t>(tr.k_norm) | reinterpret_cast<uint64_t>(tr.rope)) & 15)
-            return fail(REMP_ERR_SHAPE, "norm weights and the rotation table must be 16-byte aligned");
-        if (!(tr.eps >= 0.f)) return fail(REMP_ERR_INVALID_ARG, "eps must not be negative");
-        if (tr.rope && (tr.rotary_dim < 16 || tr.rotary_dim % 16 || tr.rotary_dim > d || tr.rope_rows < 0))
-            return fail(REMP_ERR_SHAPE, "rotary_dim must be a multiple of 16 and at most head_dim");
-        if (!tr.rope) tr.rotary_dim = 0;
-    }
+    Transform tr;
+    if (remp_status st = kvq_transform(transform, d, &tr)) return st;
     if (view.num_tokens == 0) return REMP_OK;
     if (q_heads) {
         if (remp_status st = kvq_rows(q, view.num_tokens, q_heads, d, false, "q", &rq)) return st;
@@ -479,7 +450,7 @@ extern "C" remp_status remp_kvq_read(const remp_kvq_pool* pool, const remp_kvq_b
     KvqView view;
     KvqRows rk{nullptr, 0, 0}, rv{nullptr, 0, 0};
     if (remp_status st = kvq_view(pool, batch, &view)) return st;
-    if (remp_status st = check_dtype(dtype)) return st;
+    if (remp_status st = kvq_dtype(dtype)) return st;
     const int32_t d = pool->head_dim;
     if (view.num_tokens == 0 || (!k_out && !v_out)) return REMP_OK;
     if (k_out)

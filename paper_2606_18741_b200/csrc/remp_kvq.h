@@ -34,6 +34,8 @@ struct KvqRows {  // strides in elements
 
 // Checks of what every call on the cache takes; remp_kvq.cu.
 remp_status kvq_view(const remp_kvq_pool* pool, const remp_kvq_batch* batch, KvqView* v);
+remp_status kvq_batch_view(const remp_kvq_batch* batch, KvqView* v);  // its part about the batch
+remp_status kvq_dtype(int32_t dtype);                                 // a type of 16 bits
 // Strides of a single head or token are whatever the caller's tensor says; inputs may repeat a row (stride 0), outputs may not.
 remp_status kvq_rows(const remp_kvq_rows* r, int32_t tokens, int32_t heads, int32_t head_dim, bool written, const char* name, KvqRows* out);
 

@@ -24,13 +24,13 @@
 // the long case, profiled just before its last step (57 us in the profile), took 404 instructions for a tile's K and V, with
 // the integer pipe at 54 %, issue slots at 56 % and the tensor pipe at 18 %.
 
+#include "remp_attend_parts.h"
 #include "remp_kvq_device.h"
 
 namespace remp {
 
 namespace {
 
-constexpr float kNoRef = -3e38f;  // reference of a row that has seen nothing; finite, so that -inf - kNoRef is -inf
 constexpr float kSlack = 4.f;     // log2: a new reference leaves room for scores up to 4 higher and steps up to 16 times larger
 // Steps below this are not looked at: p stays at or below 2^45, so that p*m of groups without a step (m up to 2^60 and more) and
 // their sums fit, and p*s of steps down to 2^-50 keeps its bits.
@@ -51,8 +51,6 @@ struct AttendArgs {
     uint32_t by_group; // row / group = high half of row * by_group (0: group is 1)
     int32_t room;      // tokens that a row of the table holds
 };
-
-__device__ __forceinline__ int token_of(const AttendArgs& a, int row) { return a.by_group ? (int)__umulhi((uint32_t)row, a.by_group) : row; }
 
 struct Seq {  // one sequence's share of the list
     int len, q0, rows;      // cached tokens, first row of the batch, query rows (queries * group)
@@ -77,27 +75,13 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int s) {
     return r;
 }
 
-struct Unit {  // rows [row0, row0 + rows) of a sequence (first row of the batch q0) and a KV head; its steps in the list
-    int from, to;
-    int q0, row0, rows, head;
-    int live;
-};
-
-struct Chain {  // parts of one unit in the order of the list: the first, and from rest + stride on; merged into slot or the output
-    const float *first, *rest;
-    float* slot;
-    int64_t stride;
-    const Unit* unit;
-    int n;
-};
-
 template <int D, int NT>
 struct Sizes {
     // One block to an SM: twelve warps of 168 registers hold everything where eight rows of up to 128 dims are at work (70B decode
     // step 46 us, 131071 tokens 53 us; two blocks of eight warps, which spill: 52 and 65; three of four: 48 and 75), eight
     // of 255 elsewhere.
     static constexpr int kWarps = D == 256 || NT == 2 ? 8 : 12, kThreads = kWarps * 32;
-    static constexpr int kRows = 8 * NT, kQuads = NT * D / 16;
+    static constexpr int kDim = D, kRows = 8 * NT, kQuads = NT * D / 16;
     static constexpr int kTileBytes = kKvqTile * kvq_token_bytes(D);
     static constexpr int kBuffer = KvqStep<D>::kBytes;
     // a part: accumulators as the lanes hold them (quad by quad), then references and sums of the rows
@@ -106,86 +90,6 @@ struct Sizes {
     static constexpr int kWarpBytes = (kRing + kPart + 127) / 128 * 128;
     static constexpr int kBytes = kWarps * kWarpBytes;
 };
-
-// One quad of results: dims 16i + g, 16i + 8 + g of columns 8n + 2t, +1 -> the output, 4 bytes to a lane.
-template <bool BF>
-__device__ __forceinline__ void put_quad(const float4& o, const float (&inv)[2], uint16_t* dst, bool real) {
-    const uint32_t x = transpose8(pack2(o.x * inv[0], o.y * inv[1], BF)), y = transpose8(pack2(o.z * inv[0], o.w * inv[1], BF));
-    if (real) *reinterpret_cast<uint32_t*>(dst) = x, *reinterpret_cast<uint32_t*>(dst + 8) = y;
-}
-
-// Where row 8n + g of a unit goes (dim 2t of it).
-__device__ __forceinline__ uint16_t* out_row(const AttendArgs& a, const Unit& u, int n, int g, int t) {
-    const int r = u.row0 + 8 * n + g, token = token_of(a, r);
-    return a.out.data + (int64_t)(u.q0 + token) * a.out.s_token + (int64_t)(u.head * a.group + r - token * a.group) * a.out.s_head + 2 * t;
-}
-
-__device__ __forceinline__ void put_lse(const AttendArgs& a, const Unit& u, int col, float ref, float sum) {
-    const int r = u.row0 + col, token = token_of(a, r);
-    if (col < u.rows)
-        a.lse[(int64_t)(u.q0 + token) * a.q_heads + u.head * a.group + r - token * a.group] =
-            sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-}
-
-// Parts are read in shared memory or, written by other blocks, in global memory: past the first-level cache.
-__device__ __forceinline__ float4 part4(const float* p) {
-    float4 x;
-    asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p));
-    return x;
-}
-__device__ __forceinline__ float2 part2(const float* p) {
-    float2 x;
-    asm volatile("ld.volatile.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "l"(p));
-    return x;
-}
-
-// Quad q of a chain.
-template <int D, int NT, bool BF>
-__device__ __forceinline__ void merge_quad(const AttendArgs& a, const Chain& c, int q, int lane) {
-    using Z = Sizes<D, NT>;
-    const int g = lane >> 2, t = lane & 3, tile = q / (D / 16), col = 8 * tile + 2 * t;
-    float2 ref = make_float2(kNoRef, kNoRef), sum = make_float2(0.f, 0.f);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kAhead = 8;
-#pragma unroll 1
-    for (int i0 = 0; i0 < c.n; i0 += kAhead) {
-        float4 o[kAhead];
-        float2 r[kAhead], s[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const float* x = i0 + j ? c.rest + (i0 + j) * c.stride : c.first;
-            r[j] = make_float2(kNoRef, kNoRef), s[j] = make_float2(0.f, 0.f), o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (i0 + j < c.n) o[j] = part4(x + q * 128 + lane * 4), r[j] = part2(x + Z::kQuads * 128 + col), s[j] = part2(x + Z::kQuads * 128 + Z::kRows + col);
-        }
-        float2 top = ref;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) top.x = fmaxf(top.x, r[j].x), top.y = fmaxf(top.y, r[j].y);
-        float fx = exp2_approx(ref.x - top.x), fy = exp2_approx(ref.y - top.y);
-        sum.x *= fx, sum.y *= fy, acc.x *= fx, acc.y *= fy, acc.z *= fx, acc.w *= fy;
-        ref = top;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (i0 + j >= c.n) break;
-            fx = exp2_approx(r[j].x - top.x), fy = exp2_approx(r[j].y - top.y);
-            sum.x = fmaf(fx, s[j].x, sum.x), sum.y = fmaf(fy, s[j].y, sum.y);
-            acc.x = fmaf(fx, o[j].x, acc.x), acc.y = fmaf(fy, o[j].y, acc.y);
-            acc.z = fmaf(fx, o[j].z, acc.z), acc.w = fmaf(fy, o[j].w, acc.w);
-        }
-    }
-    const bool keeper = q % (D / 16) == 0 && g == 0;  // of the rows' references and sums
-    if (c.slot) {
-        *reinterpret_cast<float4*>(c.slot + q * 128 + lane * 4) = acc;
-        if (keeper) {
-            *reinterpret_cast<float2*>(c.slot + Z::kQuads * 128 + col) = ref;
-            *reinterpret_cast<float2*>(c.slot + Z::kQuads * 128 + Z::kRows + col) = sum;
-        }
-    } else {
-        const Unit u = *c.unit;
-        const float inv[2] = {sum.x == 0.f ? 0.f : 1.f / sum.x, sum.y == 0.f ? 0.f : 1.f / sum.y};
-        put_quad<BF>(acc, inv, out_row(a, u, tile, g, t) + q % (D / 16) * 16, 8 * tile + g < u.rows);
-        if (keeper && a.lse) put_lse(a, u, col, ref.x, sum.x), put_lse(a, u, col + 1, ref.y, sum.y);
-    }
-}
 
 template <int D, int NT, bool BF>
 __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(const __grid_constant__ AttendArgs a) {
@@ -494,52 +398,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kvq_attend_kernel(c
         }
     }
 
-    // ---- parts of one unit: first those in this block, then those of several blocks, by the block that arrives last ----
-    uint32_t* counters = reinterpret_cast<uint32_t*>(a.workspace);
-    float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
-    bool shared = false;  // thread's chain is of a unit that other blocks have parts of
-    Chain c{};
-#pragma unroll 1
-    for (int round = 0; round < 2; ++round) {
-        __syncthreads();
-        if (wid == 0) {
-            if (round == 0 && lane <= kWarps) {
-                // chains begin with the part that an earlier block began (lane 0), or with a warp's tail
-                const int at = max(lane - 1, 0);
-                const Unit* u = &parts[at][lane > 0];
-                if (u->live) {
-                    c.n = 1;
-#pragma unroll 1
-                    while (at + c.n < kWarps && parts[at + c.n][0].live && parts[at + c.n][0].from == u->from) ++c.n;
-                    uint8_t* warp = smem + at * Z::kWarpBytes;
-                    c.rest = reinterpret_cast<const float*>(warp + Z::kRing), c.first = lane > 0 ? reinterpret_cast<const float*>(warp) : c.rest;
-                    c.stride = Z::kWarpBytes / 4, c.unit = u;
-                    shared = u->from < cta0 || u->to > cta1;
-                    if (shared) c.slot = slots + (2 * blockIdx.x + (u->from >= cta0)) * Z::kPartFloats;
-                }
-            } else if (round == 1) {
-                c.n = 0;
-                if (shared) {
-                    const int first = (int)((uint32_t)c.unit->from / (uint32_t)per), last = (int)((uint32_t)(c.unit->to - 1) / (uint32_t)per);
-                    uint32_t before;
-                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + first) : "memory");
-                    if (before == (uint32_t)(last - first)) {
-                        counters[first] = 0;  // ready for the next call
-                        c.first = slots + (2 * first + 1) * Z::kPartFloats, c.rest = c.first - Z::kPartFloats, c.stride = 2 * Z::kPartFloats;
-                        c.slot = nullptr, c.n = last - first + 1;
-                    }
-                }
-            }
-            const unsigned live = __ballot_sync(0xffffffffu, c.n > 0);
-            if (c.n > 0) chains[__popc(live & ((1u << lane) - 1))] = c;
-            if (lane == 0) num_chains = __popc(live);
-        }
-        const bool any = __syncthreads_or(shared);
-        const int tasks = num_chains * Z::kQuads;
-#pragma unroll 1
-        for (int task = wid; task < tasks; task += kWarps) merge_quad<D, NT, BF>(a, chains[task / Z::kQuads], task % Z::kQuads, lane);
-        if (!any) return;
-    }
+    merge_parts<Z, BF>(a, smem, parts, chains, &num_chains, cta0, cta1, per);
 }
 
 template <int D, int NT>

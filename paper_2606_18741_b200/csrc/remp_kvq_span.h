@@ -35,4 +35,22 @@ REMP_HD bool kvq_span_bad(const KvqSpan& s, int32_t length) { return s.len != le
 // The first key that a row at position `pos` sees (window 0: the first of all).
 REMP_HD int32_t kvq_first_key(int32_t pos, int32_t window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
 
+// The tiles of 16 tokens that rows from position `pos` on see: [0, sinks) and [tile0, tile0 + rest).
+struct KvTiles {
+    int32_t sinks, tile0, rest;
+};
+
+// first: tokens at the start that stay visible behind a window.
+REMP_HD KvTiles kv_tiles(const KvqSpan& s, int32_t pos, int32_t window, int32_t first) {
+    const int32_t from = kvq_first_key(pos, window);
+    const int32_t end = (s.len + 15) / 16, tile0 = from < s.len ? from / 16 : end;
+    const int32_t few = first < s.len ? first : s.len, sinks = (few + 15) / 16;
+    return KvTiles{sinks < tile0 ? sinks : tile0, tile0, end - tile0};
+}
+
+// A row at position `pos` sees key `key`.
+REMP_HD bool kv_sees(int32_t pos, int32_t key, int32_t window, int32_t first) {
+    return key <= pos && (key >= kvq_first_key(pos, window) || key < first);
+}
+
 }  // namespace remp
