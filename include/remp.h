@@ -420,7 +420,7 @@ remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* bat
                             const remp_kvq_rows* out, int32_t q_heads, int32_t dtype, float scale, int32_t window,
                             float* lse, void* workspace, void* stream);
 
-/* A test aid, for the whole process: how often a thread block of remp_kvq_attend's prompt kernel polls the barrier that its queries
+/* A test aid, for the whole process: how often a thread block of the prompt kernel of remp_kvq_attend or remp_kv_attend polls the barrier that its queries
  * arrive at before it gives up (0: never; negative: the built-in limit). It then waits for nothing else, writes NaN to its
  * outputs and sets error bit 4. */
 void remp_kvq_set_wait_limit(int32_t tries);

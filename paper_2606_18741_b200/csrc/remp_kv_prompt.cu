@@ -1,0 +1,507 @@
+// Attention over a cache of 16-bit values for many queries per sequence (prompts and their chunks, drafts of wide groups), on the tensor
+// cores' own memory.
+//
+// Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
+// matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*scale - ref), O += P.V, with a
+// running reference for each row that moves only when the probabilities of half a block outgrow kBound.
+// Rounding: P is rounded to the cache's type, the only one that the matrix instructions take beside V; S, O, sums and references are
+// in 32 bits.
+//
+// Bound: tensor cores (4*D flops for each row and key) and, as closely, the exponentials (one for each row and key; 16 a cycle of an
+// SM). Eight warps compute P (a row to a thread), one issues the matrix instructions, which run for one matrix while P of the other
+// is made, three bring K and V. Q and a ring of blocks of K and of V lie in shared memory in rows of 128 bytes, 16-byte
+// pieces exchanged within 8 rows (piece ^ (row & 7)), as 16-byte asynchronous copies bring them: the keys of a block are rows
+// of B along the dims for S and across them for O, so nothing is transposed. S and P share their columns of the tensor memory, O
+// has its own; P goes to the matrix instructions in halves of a block, so that the first half's products run while the second is
+// made. With 256 dims O takes so much of it that one matrix of 128 rows and blocks of 64 keys are left.
+// Keys that no row sees are not fetched but zeroed, so what their slots hold is never used.
+//
+// Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
+// error bit 4. Whatever happens, the issuing warp leaves when everything that it has issued is done and every barrier that it
+// has committed to has been arrived at, and the fetching warps when their copies are done.
+
+#include <atomic>
+
+#include "remp_kv_attend.h"
+#include "remp_kvq_device.h"
+#include "remp_tensor.h"
+
+namespace remp {
+
+namespace {
+
+constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
+constexpr float kBound = 16384.f;    // of the sum of half a block's probabilities
+constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
+constexpr int kMostSplits = 64;
+
+template <int D>
+struct Prompt {
+    static constexpr int kMats = D == 256 ? 1 : 2, kRows = kMats * kRowsM;
+    static constexpr int kKeys = D == 256 ? 64 : 128, kHalf = kKeys / 2;
+    static constexpr int kQ = kRowsM * D * 2, kItem = kKeys * D * 2;  // bytes of a matrix, of a block of K or of V
+    static constexpr int kPlaces = 5;                                 // of the ring
+    static constexpr int kBytes = kMats * kQ + kPlaces * kItem + 1024;
+    // columns of the tensor memory: S and P of each matrix, then O of each
+    static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
+    static constexpr int kSoftmaxWarps = 4 * kMats, kFetchWarps = 3, kThreads = (kSoftmaxWarps + 1 + kFetchWarps) * 32;
+    static constexpr int kPartFloats = kRows * (D + 2);
+};
+
+struct PromptArgs {
+    KvAttendArgs t;
+    int32_t row_blocks;        // of a sequence and KV head at most
+    int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
+    int32_t tries;             // of the wait for the queries
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {  // not real: 16 bytes of zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+// Loads of 32 columns: asked for, and there (nothing that uses them can be moved before that).
+__device__ __forceinline__ void tmem_ask32(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_there32(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                   "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                   "+r"(r[28]), "+r"(r[29])
+                 :
+                 : "memory");
+    asm volatile("" : "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+template <int D, bool BF>
+__global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const __grid_constant__ PromptArgs p_) {
+    using Z = Prompt<D>;
+    constexpr uint32_t kType = BF ? kShapeBfloat : 0;
+    constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kRows = Z::kRows, kKeys = Z::kKeys, kHalf = Z::kHalf, kPlaces = Z::kPlaces;
+    const KvAttendArgs& a = p_.t;
+    extern __shared__ uint8_t smem_[];
+    __shared__ __align__(8) uint64_t bars[12 + 2 * kPlaces];
+    __shared__ uint32_t tmem_at;
+    __shared__ int dead;
+    __shared__ int is_last;
+    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const KvView& v = a.v;
+    grid_begin();
+
+    // ---- this block's rows and keys ----
+    // row blocks from the last to the first: the last sees the most keys
+    const int part_of = (int)blockIdx.x - p_.whole, splits = part_of < 0 ? 1 : p_.splits, split = part_of < 0 ? 0 : part_of % splits;
+    int unit = part_of < 0 ? (int)blockIdx.x : p_.whole + part_of / splits;
+    const int head = unit % v.kv_heads;
+    unit /= v.kv_heads;
+    const int seq = unit % v.num_seqs, block = p_.row_blocks - 1 - unit / v.num_seqs;
+    const KvqSpan span = kvq_span(v.query_start[seq], v.query_start[seq + 1], v.seq_lens[seq], v.num_tokens, a.room);
+    if (kvq_span_bad(span, v.seq_lens[seq]) && block == 0 && tid == 0) kvq_error(v, kErrBadLength);
+    const int qs = span.q0, rows_all = span.queries * a.group, row0 = block * kRows;
+    if (row0 >= rows_all) return;
+    const int rows = min(kRows, rows_all - row0), len = span.len, first_pos = span.first_pos;
+    const int low_limit = first_pos + kv_token_of(a.by_group, row0), high_limit = first_pos + kv_token_of(a.by_group, row0 + rows - 1);
+    const int end = max(0, min(len, high_limit + 1)), low_from = kvq_first_key(low_limit, a.window), high_from = kvq_first_key(high_limit, a.window);
+    // blocks of keys: those of the first tokens, then those of the window; one range where they would meet
+    int begin = min(end, low_from) / kKvqTile * kKvqTile, ahead = (min(min(a.first, end), begin) + kKeys - 1) / kKeys;
+    if (ahead * kKeys >= begin) begin = ahead = 0;
+    const int blocks_all = ahead + (end - begin + kKeys - 1) / kKeys;
+    const int b0 = (int)((long long)blocks_all * split / splits), b1 = (int)((long long)blocks_all * (split + 1) / splits);
+    const int blocks = b1 - b0;
+    const auto key_of = [&](int j) { return b0 + j < ahead ? (b0 + j) * kKeys : begin + (b0 + j - ahead) * kKeys; };  // the first key of block j
+
+    uint8_t* smem = smem_ + ((1024u - ((uint32_t)__cvta_generic_to_shared(smem_) & 1023u)) & 1023u);
+    uint8_t *sq = smem, *ring = smem + Z::kMats * Z::kQ;
+    // for each matrix: scores, probabilities and products of the halves of a block; queries; places of the ring (block j of K is item 2j, of V item 2j + 1)
+    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
+    const uint32_t s_full = bar, p_full = bar + 16, o_half = bar + 32, o_done = bar + 48, p_half = bar + 64, q_full = bar + 80, all_done = bar + 88, full = bar + 96, vacant = full + 8 * kPlaces;
+    const int mats = rows > kRowsM ? 2 : 1;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i)  // warps without rows make no P
+            bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))), bar_init(p_full + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))),
+                bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
+        for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, Z::kFetchWarps), bar_init(vacant + 8 * i, 1);
+        bar_init(q_full, kSoftmaxWarps), bar_init(all_done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        dead = 0, is_last = 0;
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned long long*>(gone[i]) = 0;
+    }
+    if (wid == kSoftmaxWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_at)),
+                     "n"(Z::kColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const uint32_t tmem = tmem_at;
+
+    if (wid < kSoftmaxWarps) {
+        // ---- P and the output: one row to a thread ----
+        const int mat = wid >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), s_at = lanes + mat * kKeys, o_at = lanes + Z::kO + mat * D;
+        const int row = row0 + min(tid, rows - 1), token = kv_token_of(a.by_group, row), q_head = head * a.group + row - token * a.group;
+        const bool real = tid < rows, rows_here = (tid & ~31) < rows;  // of this thread, of this warp
+        const int limit = min(first_pos + token, len - 1), from = kvq_first_key(first_pos + token, a.window);
+        // the warp's 32 rows of Q, coalesced
+        if (rows_here) {
+            constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;
+#pragma unroll 8
+            for (int i = 0; i < 32 / kAtOnce; ++i) {
+                const int in = wid * 32 + i * kAtOnce + lane / kPieces, piece = lane % kPieces;
+                const int r = row0 + min(in, rows - 1), tok = kv_token_of(a.by_group, r);
+                const uint4 x = *reinterpret_cast<const uint4*>(a.q.data + (int64_t)(qs + tok) * a.q.s_token + (int64_t)(head * a.group + r - tok * a.group) * a.q.s_head + 8 * piece);
+                *reinterpret_cast<uint4*>(sq + mat * Z::kQ + (piece / 8) * (kRowsM * 128) + (in & 127) * 128 + (((piece % 8) ^ (in & 7)) << 4)) = x;
+            }
+        }
+        for_tensor_cores();
+        __syncwarp();
+        if (lane == 0) bar_arrive(q_full);
+
+        float ref = kUnset, sum = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < (rows_here ? blocks : 0); ++j) {
+            bar_wait(s_full + 8 * mat, j & 1, &dead);
+            __syncwarp();
+            tmem_after();
+            const int key0 = key_of(j);
+            const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
+            const bool whole = missing == 0 && key0 + kKeys - 1 <= min(low_limit, len - 1) && (key0 >= high_from || key0 + kKeys <= a.first);
+            // keys of chunk c (32 of them) that this row sees
+            const auto seen_of = [&](int c) {
+                const int last = limit - key0 - 32 * c, least = from - key0 - 32 * c, few = a.first - key0 - 32 * c;
+                uint32_t seen = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1;
+                seen &= (least <= 0 ? 0xffffffffu : least >= 32 ? 0u : ~0u << least) | (few >= 32 ? 0xffffffffu : few <= 0 ? 0u : (1u << few) - 1);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (missing >> (8 * (2 * c + i)) & 1) seen &= ~(0xffffu << (16 * i));
+                return seen;
+            };
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p[kHalf / 2];
+#pragma unroll 1
+                for (int round = 0;; ++round) {
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t s[kHalf / 32][32];
+#pragma unroll
+                    for (int c = 0; c < kHalf / 32; ++c) tmem_ask32(s_at + h * kHalf + 32 * c, s[c]);
+#pragma unroll
+                    for (int c = 0; c < kHalf / 32; ++c) {
+                        tmem_there32(s[c]);
+                        if (!whole) {
+                            const uint32_t seen = seen_of(h * (kHalf / 32) + c);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!(seen >> i & 1)) s[c][i] = 0xff800000u;  // -infinity
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = exp2_approx(fmaf(__uint_as_float(s[c][2 * i]), a.scale_log2, -ref)), y = exp2_approx(fmaf(__uint_as_float(s[c][2 * i + 1]), a.scale_log2, -ref));
+                            part[2 * (i & 1)] += x, part[2 * (i & 1) + 1] += y;
+                            p[16 * c + i] = pack2(x, y, BF);
+                        }
+                    }
+                    const float total = (part[0] + part[1]) + (part[2] + part[3]);
+                    if (round || !__any_sync(0xffffffffu, total > kBound)) {
+                        sum += total;
+                        break;
+                    }
+                    // rows that have outgrown their reference get another; what they have so far falls with it
+                    float now = ref;
+                    if (total > kBound) {
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int c = 0; c < kHalf / 32; ++c)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[c][i]));
+                        now = top * a.scale_log2 - kStart;
+                    }
+                    const float fall = exp2_approx(ref - now);
+                    ref = now, sum *= fall;
+                    if (j > 0 || h > 0) {
+                        bar_wait(h ? o_half + 8 * mat : o_done + 8 * mat, j - 1 + h & 1, &dead);  // the products of the half before
+                        __syncwarp();
+                        tmem_after();
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 16) {
+                            uint32_t o[16];
+                            tmem_load16(o_at + i, o);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+                            tmem_store16(o_at + i, o);
+                        }
+                        tmem_stored();
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < kHalf / 32; ++c) {
+                    uint32_t x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = p[16 * c + i];
+                    tmem_store16(s_at + h * (kHalf / 2) + 16 * c, x);
+                }
+                tmem_stored();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive((h ? p_full : p_half) + 8 * mat);
+            }
+        }
+        const bool some = blocks > 0 && rows_here;
+        if (some) {
+            bar_wait(o_done + 8 * mat, blocks - 1 & 1, &dead);
+            __syncwarp();
+            tmem_after();
+        }
+        // Whoever gave up said so before its next arrival, and outputs are behind all arrivals: none that went wrong gets here
+        // without the mark.
+        if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
+        uint16_t* dst = a.out.data + (int64_t)(qs + token) * a.out.s_token + (int64_t)q_head * a.out.s_head;
+        if (splits == 1) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
+            for (int i = 0; i < (rows_here ? D : 0); i += 32) {
+                uint32_t o[32];
+                if (some) {
+                    tmem_load32(o_at + i, o);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0;
+                }
+                if (real)
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) w[x] = pack2(__uint_as_float(o[k + 2 * x]) * inv, __uint_as_float(o[k + 2 * x + 1]) * inv, BF);
+                        *reinterpret_cast<uint4*>(dst + i + k) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+            }
+            if (real && a.lse) a.lse[(int64_t)(qs + token) * a.q_heads + q_head] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+        } else {
+            // a part: [dim][row], then references and sums; the block that comes last adds the parts up in their order
+            float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
+            float* mine = slots + (int64_t)part_of * Z::kPartFloats;
+#pragma unroll 1
+            for (int i = 0; i < (rows_here ? D : 0); i += 32) {
+                uint32_t o[32];
+                if (some) {
+                    tmem_load32(o_at + i, o);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0;
+                }
+#pragma unroll
+                for (int k = 0; k < 32; ++k) mine[(i + k) * kRows + tid] = __uint_as_float(o[k]);
+            }
+            mine[D * kRows + tid] = ref, mine[(D + 1) * kRows + tid] = sum;
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+            if (tid == 0) {
+                uint32_t* counter = reinterpret_cast<uint32_t*>(a.workspace) + part_of / splits;
+                uint32_t before;
+                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+                is_last = before == (uint32_t)splits - 1;
+                if (is_last) *counter = 0;  // ready for the next call
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+            if (is_last) {
+                // 32 rows and 16 dims to a warp at a time, in steps of eight parts' references and four parts' values
+                const float* part = slots + (int64_t)(part_of - split) * Z::kPartFloats;
+#pragma unroll 1
+                for (int task = wid; task < (rows + 31) / 32 * (D / 16); task += kSoftmaxWarps) {
+                    const int r = task / (D / 16) * 32 + lane, d = task % (D / 16) * 16;
+                    const int my_row = row0 + min(r, rows - 1), my_token = kv_token_of(a.by_group, my_row), my_head = head * a.group + my_row - my_token * a.group;
+                    const float* refs = part + D * kRows + r;
+                    float top = kUnset, all = 0.f, o[16];
+#pragma unroll 8
+                    for (int i = 0; i < splits; ++i) top = fmaxf(top, __ldcg(refs + (int64_t)i * Z::kPartFloats));
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = 0.f;
+#pragma unroll 4
+                    for (int i = 0; i < splits; ++i) {
+                        const float* x = part + (int64_t)i * Z::kPartFloats + d * kRows + r;
+                        const float f = exp2_approx(__ldcg(refs + (int64_t)i * Z::kPartFloats) - top);
+                        all = fmaf(f, __ldcg(refs + (int64_t)i * Z::kPartFloats + kRows), all);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = fmaf(f, __ldcg(x + k * kRows), o[k]);
+                    }
+                    const float inv = all == 0.f ? 0.f : 1.f / all;
+                    if (r < rows) {
+                        uint16_t* to = a.out.data + (int64_t)(qs + my_token) * a.out.s_token + (int64_t)my_head * a.out.s_head + d;
+                        uint32_t w[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) w[x] = pack2(o[2 * x] * inv, o[2 * x + 1] * inv, BF);
+                        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                        if (a.lse && d == 0)
+                            a.lse[(int64_t)(qs + my_token) * a.q_heads + my_head] = all == 0.f ? -INFINITY : (top + log2f(all)) * 0.69314718055994531f;
+                    }
+                }
+            }
+        }
+    } else if (wid == kSoftmaxWarps) {
+        // ---- matrix instructions: one lane issues them ----
+        const uint32_t leads = lane == 0;
+        const int n = __shfl_sync(0xffffffffu, blocks, 0), live = __shfl_sync(0xffffffffu, mats, 0);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t q_low = operand_low((uint32_t)__cvta_generic_to_shared(sq)), ring_low = operand_low((uint32_t)__cvta_generic_to_shared(ring));
+        const uint32_t across = (uint32_t)(kKeys * 128 >> 4) << 16;  // V: from 64 dims to the next 64
+        const auto wait_for = [&](uint32_t b, uint32_t parity) {
+            bar_wait(b, parity, &dead);
+            __syncwarp();
+        };
+        const auto scores = [&](int mat, uint32_t k_block) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                mma_smem<kKeys, kType>(tm + mat * kKeys, q_low + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
+                                       k_block + ((k / 4) * (kKeys * 128) + (k % 4) * 32 >> 4), k > 0, leads);
+            commit_to(s_full + 8 * mat, leads);
+        };
+        if (n > 0) {
+            bar_wait(q_full, 0, &dead, p_.tries);
+            wait_for(full, 0);
+            tmem_after();
+#pragma unroll
+            for (int mat = 0; mat < Z::kMats; ++mat)
+                if (mat < live) scores(mat, ring_low);
+            commit_to(vacant, leads);
+        }
+        int place_v = 1 % kPlaces, place_k = 2 % kPlaces;
+        uint32_t turn_v = 0, turn_k = 0;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
+            // the order of issue, so the scores may take the place of the probabilities before them.
+            const uint32_t v_block = ring_low + (uint32_t)(place_v * (Z::kItem >> 4)) + across - (1u << 16), k_block = ring_low + (uint32_t)(place_k * (Z::kItem >> 4));
+            const bool more = j + 1 < n;
+#pragma unroll
+            for (int mat = 0; mat < Z::kMats; ++mat) {
+                if (mat >= live) break;
+                if (mat == 0) bar_wait(full + 8 * place_v, turn_v, &dead);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    wait_for((h ? p_full : p_half) + 8 * mat, j & 1);
+                    tmem_after();
+#pragma unroll
+                    for (int k = 0; k < kHalf / 16; ++k)
+                        mma_tmem<D, kType | kShapeBAcross>(tm + Z::kO + mat * D, tm + mat * kKeys + h * (kHalf / 2) + 8 * k, v_block + ((h * kHalf + 16 * k) * 128 >> 4),
+                                                           h + k ? 1 : j, leads);
+                    commit_to(h ? o_done + 8 * mat : o_half + 8 * mat, leads);
+                }
+                if (more) {
+                    if (mat == 0) wait_for(full + 8 * place_k, turn_k);
+                    scores(mat, k_block);
+                }
+            }
+            commit_to(vacant + 8 * place_v, leads);
+            if (more) commit_to(vacant + 8 * place_k, leads);
+            if ((place_v += 2) >= kPlaces) place_v -= kPlaces, turn_v ^= 1;
+            if ((place_k += 2) >= kPlaces) place_k -= kPlaces, turn_k ^= 1;
+        }
+        // Nothing stays in flight, whatever happened: a barrier of its own stands behind everything, since a block that gave up may
+        // have run ahead of the others by several phases. Then the last arrival on each of these.
+        __syncwarp();
+        commit_to(all_done, leads);
+        bar_drain(all_done, 1, &dead);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (i < live) bar_drain(s_full + 8 * i, n, &dead), bar_drain(o_half + 8 * i, n, &dead), bar_drain(o_done + 8 * i, n, &dead);
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) bar_drain(vacant + 8 * i, (2 * n - i + kPlaces - 1) / kPlaces, &dead);
+        __syncwarp();
+    } else {
+        // ---- keys and values: a tile of 16 tokens to a warp at a time ----
+        constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces, kTiles = kKeys / kKvqTile, kLag = 2;
+        const int w = wid - kSoftmaxWarps - 1, piece = lane % kPieces, sub = lane / kPieces;
+        const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
+        const uint8_t* slice = v.base + (int64_t)head * v.s_head + piece * 16;
+        const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + (piece / 8) * (kKeys * 128);
+        const auto bring = [&](int item) {
+            const int j = item >> 1, place = item % kPlaces, turn = item / kPlaces;
+            const bool of_v = item & 1;
+            const int key0 = key_of(j);
+            if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
+#pragma unroll 1
+            for (int t = (w + of_v) % Z::kFetchWarps; t < kTiles; t += Z::kFetchWarps) {
+                const int key = key0 + t * kKvqTile, tile = key / kKvqTile;
+                int id = -1, in_row = 0;
+                if (key < end) {
+                    in_row = tile / v.block_tiles, id = __ldg(row + in_row);
+                    if ((uint32_t)id >= (uint32_t)v.nb && lane == 0) kvq_error(v, kErrBadBlock);
+                }
+                const bool there = (uint32_t)id < (uint32_t)v.nb;
+                if (!of_v && lane == 0) gone[j & 3][t] = !there;
+                const uint8_t* src = slice + (int64_t)id * v.s_block + (of_v ? v.s_kv : 0) + (int64_t)(key - in_row * v.block_tiles * kKvqTile) * v.s_token;
+                const uint32_t dst = ring_at + place * Z::kItem + t * (kKvqTile * 128);
+#pragma unroll
+                for (int i = 0; i < kKvqTile / kAtOnce; ++i) {
+                    const int r = i * kAtOnce + sub;
+                    const bool real = there && key + r < end && (key + r >= low_from || key + r < a.first);
+                    copy16(dst + r * 128 + (((piece % 8) ^ (r & 7)) << 4), real ? src + r * v.s_token : v.base, real);
+                }
+            }
+            cp_async_commit();
+        };
+        const auto tell = [&](int item) {
+            for_tensor_cores();
+            __syncwarp();
+            if (lane == 0) bar_arrive(full + 8 * (item % kPlaces));
+        };
+#pragma unroll 1
+        for (int item = 0; item < 2 * blocks; ++item) {
+            bring(item);
+            if (item >= kLag) cp_async_wait<kLag>(), tell(item - kLag);
+        }
+        cp_async_wait<0>();
+        for (int item = max(0, 2 * blocks - kLag); item < 2 * blocks; ++item) tell(item);
+    }
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    __syncwarp();
+    if (wid == kSoftmaxWarps)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Z::kColumns));
+    if (tid == 0 && dead) kvq_error(v, kErrWaitLimit);
+}
+
+template <int D>
+cudaError_t launch(PromptArgs& p, bool bf, int sms, int max_rows, cudaStream_t stream) {
+    using Z = Prompt<D>;
+    static_assert(Z::kBytes + 512 <= 227 * 1024, "shared memory");
+    const KvView& v = p.t.v;
+    p.row_blocks = (max_rows + Z::kRows - 1) / Z::kRows;
+    const int64_t units = (int64_t)p.row_blocks * v.num_seqs * v.kv_heads;
+    // a unit is a thread block's work; those that are left when the others have filled the GPU whole times share it, each
+    // one's keys split
+    constexpr int kParts = (int)((kAttendWorkspace - kAttendCounterBytes) / (Z::kPartFloats * 4));
+    const int places = std::min(sms, kParts);
+    const int64_t rest = units % sms;
+    p.splits = rest ? (int)std::min<int64_t>(kMostSplits, places / rest) : 1;
+    if (p.splits < 2) p.splits = 1;
+    p.whole = (int)(p.splits > 1 ? units - rest : units);
+    static_assert(kParts >= 148 && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
+    if (units > 0x7fffffff / kMostSplits) return cudaErrorInvalidConfiguration;
+    p.tries = prompt_wait_tries();
+    return launch_after(bf ? kv_prompt_kernel<D, true> : kv_prompt_kernel<D, false>, p.whole + (units - p.whole) * p.splits, Z::kThreads, Z::kBytes, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, int sms, int32_t max_rows, cudaStream_t stream) {
+    PromptArgs p{a, 0, 0, 1, kWaitTries};
+    return head_dim == 64 ? launch<64>(p, bf, sms, max_rows, stream)
+           : head_dim == 128 ? launch<128>(p, bf, sms, max_rows, stream) : launch<256>(p, bf, sms, max_rows, stream);
+}
+
+}  // namespace remp

@@ -17,6 +17,7 @@ constexpr size_t kAttendWorkspace = kAttendCounterBytes + (size_t)300 * 128 * (1
 cudaError_t launch_prompt(const KvqView& v, const KvqRows& q, const KvqRows& out, float* lse, void* workspace, float scale_log2, int32_t head_dim,
                           int32_t q_heads, int32_t group, uint32_t by_group, int32_t window, int32_t room, bool bf, int sms, int32_t max_rows,
                           cudaStream_t stream);
+int32_t prompt_wait_tries();  // remp_kvq_set_wait_limit
 
 #ifdef __CUDACC__
 

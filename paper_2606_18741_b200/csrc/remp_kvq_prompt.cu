@@ -35,12 +35,12 @@
 #include <type_traits>
 
 #include "remp_kvq_device.h"
+#include "remp_tensor.h"
 
 namespace remp {
 
 namespace {
 
-constexpr int kRowsM = 128;
 constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
 constexpr float kBound = 16384.f;    // of the sum of 32 probabilities
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
@@ -51,7 +51,6 @@ constexpr int kUpK = -2, kUpV = 3;
 __host__ __device__ constexpr int least_of(int up) { return -9 - up; }
 __host__ __device__ constexpr int most_of(int up) { return 11 - up; }
 constexpr int kMostSplits = 16;
-constexpr int32_t kWaitTries = 1 << 18;
 std::atomic<int32_t> g_wait_tries{kWaitTries};  // remp_kvq_set_wait_limit
 
 template <int D>
@@ -66,95 +65,6 @@ struct Prompt {
     static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
     static constexpr int kPartFloats = kRows * (D + 2);
 };
-
-// ---- barriers and tensor memory ----
-
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok;
-}
-// Bounded: a wait that runs out marks the block, and nothing in it waits any more.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int32_t tries = kWaitTries) {
-    for (int32_t i = 0; i < tries; ++i) {
-        if (bar_try(bar, parity)) return;
-        if (*dead) return;
-    }
-    *dead = 1;
-}
-// The last of `times` commits to a barrier has arrived. Always with the full limit.
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t times, volatile int* dead) {
-    if (times == 0) return;
-    for (int32_t i = 0; i < kWaitTries; ++i)
-        if (bar_try(bar, (times - 1) & 1)) return;
-    *dead = 1;
-}
-__device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t leads) {
-    asm volatile("{ .reg .pred q; setp.ne.b32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar),
-                 "r"(leads)
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// Descriptors of operands in rows of 128 bytes (64 halves) along K, 16-byte pieces exchanged within 8 rows: the low word goes
-// by the address, in units of 16 bytes, the high word is the same for all. Halves times halves into 32 bits, 128 rows.
-__device__ __forceinline__ uint32_t operand_low(uint32_t at) { return (at >> 4 & 0x3fff) | 1u << 16; }
-constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
-template <int N>
-constexpr uint32_t kShape = 1u << 4 | (uint32_t)(N >> 3) << 17 | (uint32_t)(kRowsM >> 4) << 24;
-
-// The whole warp gets here with the same operands (so they stay in uniform registers); the lane with `leads` issues.
-template <int N>
-__device__ __forceinline__ void mma_smem(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t add, uint32_t leads) {
-    asm volatile(
-        "{ .reg .pred p, q; .reg .b64 a, b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5};"
-        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a_low), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
-        "r"(leads)
-        : "memory");
-}
-template <int N>
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b_low, uint32_t add, uint32_t leads) {
-    asm volatile(
-        "{ .reg .pred p, q; .reg .b64 b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 b, {%2, %5};"
-        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
-        "r"(leads)
-        : "memory");
-}
-__device__ __forceinline__ void for_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---- codes to halves ----
 
@@ -821,11 +731,13 @@ cudaError_t launch(PromptArgs& a, bool bf, int sms, int max_rows, cudaStream_t s
     a.whole = (int)(a.splits > 1 ? units - rest : units);
     static_assert(kParts >= 148 && kParts <= 2 * kAttendMaxCtas, "workspace");  // splits of two at least: a counter for two parts
     if (units > 0x7fffffff / kMostSplits) return cudaErrorInvalidConfiguration;
-    a.tries = g_wait_tries.load(std::memory_order_relaxed);
+    a.tries = prompt_wait_tries();
     return launch_after(bf ? kvq_prompt_kernel<D, true> : kvq_prompt_kernel<D, false>, a.whole + (units - a.whole) * a.splits, Z::kThreads, Z::kBytes, stream, a);
 }
 
 }  // namespace
+
+int32_t prompt_wait_tries() { return g_wait_tries.load(std::memory_order_relaxed); }
 
 cudaError_t launch_prompt(const KvqView& v, const KvqRows& q, const KvqRows& out, float* lse, void* workspace, float scale_log2, int32_t head_dim,
                           int32_t q_heads, int32_t group, uint32_t by_group, int32_t window, int32_t room, bool bf, int sms, int32_t max_rows,
