@@ -9,7 +9,7 @@
 //
 // Bound: tensor cores (4*D flops for each row and key) and, as closely, the exponentials (one for each row and key; 16 a cycle of an
 // SM). Eight warps compute P (a row to a thread), one issues the matrix instructions, which run for one matrix while P of the other
-// is made, three bring K and V. Q and a ring of blocks of K and of V lie in shared memory in rows of 128 bytes, 16-byte
+// is made, one brings K and V. Q and a ring of blocks of K and of V lie in shared memory in rows of 128 bytes, 16-byte
 // pieces exchanged within 8 rows (piece ^ (row & 7)), as 16-byte asynchronous copies bring them: the keys of a block are rows
 // of B along the dims for S and across them for O, so nothing is transposed. S and P share their columns of the tensor memory, O
 // has its own; P goes to the matrix instructions in halves of a block, so that the first half's products run while the second is
@@ -18,9 +18,9 @@
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
 // error bit 4. Whatever happens, the issuing warp leaves when everything that it has issued is done and every barrier that it
-// has committed to has been arrived at, and the fetching warps when their copies are done.
+// has committed to has been arrived at, and the fetching warp when its copies are done.
 
-#include <atomic>
+#include <cuda.h>
 
 #include "remp_kv_attend.h"
 #include "remp_kvq_device.h"
@@ -44,19 +44,26 @@ struct Prompt {
     static constexpr int kBytes = kMats * kQ + kPlaces * kItem + 1024;
     // columns of the tensor memory: S and P of each matrix, then O of each
     static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
-    static constexpr int kSoftmaxWarps = 4 * kMats, kFetchWarps = 3, kThreads = (kSoftmaxWarps + 1 + kFetchWarps) * 32;
+    static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + 2) * 32;
     static constexpr int kPartFloats = kRows * (D + 2);
 };
 
 struct PromptArgs {
+    CUtensorMap k, v;          // [block][head][token][dim] of K and of V, in boxes of 16 tokens and 64 dims
     KvAttendArgs t;
     int32_t row_blocks;        // of a sequence and KV head at most
     int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
     int32_t tries;             // of the wait for the queries
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {  // not real: 16 bytes of zero
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+// 16 tokens of 64 dims of a head, in rows of 128 bytes whose 16-byte pieces change places, to `dst`; their bytes count for `bar`.
+__device__ __forceinline__ void bring_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int dim, int token, int head, int block) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
+                 "r"(dim), "r"(token), "r"(head), "r"(block)
+                 : "memory");
+}
+__device__ __forceinline__ void bar_arrive_expecting(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
 // Loads of 32 columns: asked for, and there (nothing that uses them can be moved before that).
@@ -130,7 +137,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         for (int i = 0; i < 2; ++i)  // warps without rows make no P
             bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))), bar_init(p_full + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))),
                 bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
-        for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, Z::kFetchWarps), bar_init(vacant + 8 * i, 1);
+        for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, 1), bar_init(vacant + 8 * i, 1);
         bar_init(q_full, kSoftmaxWarps), bar_init(all_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead = 0, is_last = 0;
@@ -421,50 +428,58 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         for (int i = 0; i < kPlaces; ++i) bar_drain(vacant + 8 * i, (2 * n - i + kPlaces - 1) / kPlaces, &dead);
         __syncwarp();
     } else {
-        // ---- keys and values: a tile of 16 tokens to a warp at a time ----
-        constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces, kTiles = kKeys / kKvqTile, kLag = 2;
-        const int w = wid - kSoftmaxWarps - 1, piece = lane % kPieces, sub = lane / kPieces;
+        // ---- keys and values: a tile of 16 tokens to a lane, whole ones in boxes, others row by row with zeros between ----
+        constexpr int kTiles = kKeys / kKvqTile, kChunk = kKeys * 128, kTile = kKvqTile * 128;  // 64 dims of a block, of a tile
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
-        const uint8_t* slice = v.base + (int64_t)head * v.s_head + piece * 16;
-        const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + (piece / 8) * (kKeys * 128);
-        const auto bring = [&](int item) {
-            const int j = item >> 1, place = item % kPlaces, turn = item / kPlaces;
-            const bool of_v = item & 1;
-            const int key0 = key_of(j);
-            if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
+        const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+        // This lane's tile of block j: its block (-1: not there) and first token in it. Asked for a block ahead.
+        const auto find = [&](int j) {
+            int2 r = make_int2(-1, 0);
+            const int key = key_of(j) + lane * kKvqTile;
+            if (j < blocks && lane < kTiles && key < end) {
+                const int tile = key / kKvqTile, in_row = tile / v.block_tiles;
+                r = make_int2(__ldg(row + in_row), (tile - in_row * v.block_tiles) * kKvqTile);
+                if ((uint32_t)r.x >= (uint32_t)v.nb) kvq_error(v, kErrBadBlock), r.x = -1;
+            }
+            return r;
+        };
+        int2 at = make_int2(-1, 0), next = find(0);
+        int items = 0;
 #pragma unroll 1
-            for (int t = (w + of_v) % Z::kFetchWarps; t < kTiles; t += Z::kFetchWarps) {
-                const int key = key0 + t * kKvqTile, tile = key / kKvqTile;
-                int id = -1, in_row = 0;
-                if (key < end) {
-                    in_row = tile / v.block_tiles, id = __ldg(row + in_row);
-                    if ((uint32_t)id >= (uint32_t)v.nb && lane == 0) kvq_error(v, kErrBadBlock);
-                }
-                const bool there = (uint32_t)id < (uint32_t)v.nb;
-                if (!of_v && lane == 0) gone[j & 3][t] = !there;
-                const uint8_t* src = slice + (int64_t)id * v.s_block + (of_v ? v.s_kv : 0) + (int64_t)(key - in_row * v.block_tiles * kKvqTile) * v.s_token;
-                const uint32_t dst = ring_at + place * Z::kItem + t * (kKvqTile * 128);
-#pragma unroll
-                for (int i = 0; i < kKvqTile / kAtOnce; ++i) {
-                    const int r = i * kAtOnce + sub;
-                    const bool real = there && key + r < end && (key + r >= low_from || key + r < a.first);
-                    copy16(dst + r * 128 + (((piece % 8) ^ (r & 7)) << 4), real ? src + r * v.s_token : v.base, real);
+        for (; items < 2 * blocks; ++items) {
+            const int j = items >> 1, place = items % kPlaces, turn = items / kPlaces;
+            const bool of_v = items & 1;
+            if (!of_v) at = next, next = find(j + 1);
+            if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
+            __syncwarp();
+            if (*static_cast<volatile int*>(&dead)) break;  // what is asked for is waited for below
+            const int key0 = key_of(j), key = key0 + lane * kKvqTile;
+            if (!of_v && lane < kTiles) gone[j & 3][lane] = at.x < 0;
+            const bool every = at.x >= 0 && key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first);
+            const uint32_t boxes = __ballot_sync(0xffffffffu, every);
+            const uint32_t dst = ring_at + place * Z::kItem;
+            for (uint32_t others = ~boxes & ((1u << kTiles) - 1); others; others &= others - 1) {
+                const int t = __ffs(others) - 1, id = __shfl_sync(0xffffffffu, at.x, t), token = __shfl_sync(0xffffffffu, at.y, t), first_key = key0 + t * kKvqTile;
+                const uint8_t* src = v.base + (int64_t)id * v.s_block + (of_v ? v.s_kv : 0) + (int64_t)head * v.s_head + (int64_t)token * v.s_token;
+                for (int i = lane; i < kKvqTile * (D / 8); i += 32) {
+                    const int r = i / (D / 8), piece = i % (D / 8);
+                    const bool real = id >= 0 && first_key + r < end && (first_key + r >= low_from || first_key + r < a.first);
+                    const uint4 x = real ? *reinterpret_cast<const uint4*>(src + r * v.s_token + piece * 16) : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(ring + place * Z::kItem + (piece / 8) * kChunk + t * kTile + r * 128 + (((piece % 8) ^ (r & 7)) << 4)) = x;
                 }
             }
-            cp_async_commit();
-        };
-        const auto tell = [&](int item) {
             for_tensor_cores();
             __syncwarp();
-            if (lane == 0) bar_arrive(full + 8 * (item % kPlaces));
-        };
-#pragma unroll 1
-        for (int item = 0; item < 2 * blocks; ++item) {
-            bring(item);
-            if (item >= kLag) cp_async_wait<kLag>(), tell(item - kLag);
+            if (lane == 0) bar_arrive_expecting(full + 8 * place, __popc(boxes) * (kKvqTile * D * 2));
+            __syncwarp();
+            if (every)
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) bring_box(dst + c * kChunk + lane * kTile, of_v ? &p_.v : &p_.k, full + 8 * place, 64 * c, at.y, head, at.x);
         }
-        cp_async_wait<0>();
-        for (int item = max(0, 2 * blocks - kLag); item < 2 * blocks; ++item) tell(item);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) bar_drain(full + 8 * i, max(0, items - i + kPlaces - 1) / kPlaces, &dead);
+        __syncwarp();
     }
     tmem_before();
     __syncthreads();
@@ -498,8 +513,29 @@ cudaError_t launch(PromptArgs& p, bool bf, int sms, int max_rows, cudaStream_t s
 
 }  // namespace
 
+bool kv_prompt_takes(const KvView& v) {
+    // strides of a tensor map
+    return v.nb > 0 && std::max(v.s_token, std::max(v.s_head, v.s_block)) < (int64_t)1 << 40;
+}
+
 cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, int sms, int32_t max_rows, cudaStream_t stream) {
-    PromptArgs p{a, 0, 0, 1, kWaitTries};
+    using Encode = decltype(&cuTensorMapEncodeTiled);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) == cudaSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+    }();
+    if (!encode) return cudaErrorNotSupported;
+    PromptArgs p{};
+    p.t = a, p.splits = 1;
+    const KvView& v = a.v;
+    const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)v.block_tiles * kKvqTile, (cuuint64_t)v.kv_heads, (cuuint64_t)v.nb};
+    const cuuint64_t strides[3] = {(cuuint64_t)v.s_token, (cuuint64_t)v.s_head, (cuuint64_t)v.s_block};
+    const cuuint32_t box[4] = {64, kKvqTile, 1, 1}, steps[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i)
+        if (encode(i ? &p.v : &p.k, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, v.base + (i ? v.s_kv : 0), dims, strides, box, steps,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
     return head_dim == 64 ? launch<64>(p, bf, sms, max_rows, stream)
            : head_dim == 128 ? launch<128>(p, bf, sms, max_rows, stream) : launch<256>(p, bf, sms, max_rows, stream);
 }
