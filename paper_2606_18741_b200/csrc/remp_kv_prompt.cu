@@ -38,12 +38,14 @@ constexpr int kMostSplits = 64;
 template <int D>
 struct Prompt {
     static constexpr int kMats = D == 256 ? 1 : 2, kRows = kMats * kRowsM;
-    static constexpr int kKeys = D == 256 ? 64 : 128, kHalf = kKeys / 2;
+    static constexpr int kKeys = D == 256 ? 64 : 128;
+    static constexpr int kChunks = kKeys / 32, kFirst = kChunks - 1;  // of 32 keys; those of a block's first part, one makes the second
+    static constexpr int kBuffers = D == 256 ? 2 : 1;                 // of the scores of a matrix
     static constexpr int kQ = kRowsM * D * 2, kItem = kKeys * D * 2;  // bytes of a matrix, of a block of K or of V
     static constexpr int kPlaces = 5;                                 // of the ring
     static constexpr int kBytes = kMats * kQ + kPlaces * kItem + 1024;
-    // columns of the tensor memory: S and P of each matrix, then O of each
-    static constexpr int kO = kMats * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
+    // columns of the tensor memory: S and P of each matrix and buffer, then O of each matrix
+    static constexpr int kO = kMats * kBuffers * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
     static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + 2) * 32;
     static constexpr int kPartFloats = kRows * (D + 2);
 };
@@ -64,6 +66,19 @@ __device__ __forceinline__ void bring_box(uint32_t dst, const CUtensorMap* map, 
 }
 __device__ __forceinline__ void bar_arrive_expecting(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 
 // Loads of 32 columns: asked for, and there (nothing that uses them can be moved before that).
@@ -92,7 +107,7 @@ template <int D, bool BF>
 __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const __grid_constant__ PromptArgs p_) {
     using Z = Prompt<D>;
     constexpr uint32_t kType = BF ? kShapeBfloat : 0;
-    constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kRows = Z::kRows, kKeys = Z::kKeys, kHalf = Z::kHalf, kPlaces = Z::kPlaces;
+    constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kRows = Z::kRows, kKeys = Z::kKeys, kPlaces = Z::kPlaces;
     const KvAttendArgs& a = p_.t;
     extern __shared__ uint8_t smem_[];
     __shared__ __align__(8) uint64_t bars[12 + 2 * kPlaces];
@@ -133,10 +148,15 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t s_full = bar, p_full = bar + 16, o_half = bar + 32, o_done = bar + 48, p_half = bar + 64, q_full = bar + 80, all_done = bar + 88, full = bar + 96, vacant = full + 8 * kPlaces;
     const int mats = rows > kRowsM ? 2 : 1;
+    // scores of block j: their place, and of the barriers that go with it; the phase of these. What a barrier had before that
+    // phase is done when the scores are there, so no wait for a phase meets the one two before it.
+    const auto at_of = [](int mat, int j) { return mat + j % Z::kBuffers; };
+    const auto turn_of = [](int j) { return j / Z::kBuffers & 1; };
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i)  // warps without rows make no P
-            bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))), bar_init(p_full + 8 * i, max(1, min(4, (rows - i * kRowsM + 31) / 32))),
-                bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) {
+            const int warps = max(1, min(4, (rows - (Z::kBuffers == 2 ? 0 : i) * kRowsM + 31) / 32));  // those without rows make no P
+            bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, warps), bar_init(p_full + 8 * i, warps), bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
+        }
         for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, 1), bar_init(vacant + 8 * i, 1);
         bar_init(q_full, kSoftmaxWarps), bar_init(all_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -157,7 +177,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
     if (wid < kSoftmaxWarps) {
         // ---- P and the output: one row to a thread ----
         const int mat = wid >> 2;
-        const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), s_at = lanes + mat * kKeys, o_at = lanes + Z::kO + mat * D;
+        const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), o_at = lanes + Z::kO + mat * D;
         const int row = row0 + min(tid, rows - 1), token = kv_token_of(a.by_group, row), q_head = head * a.group + row - token * a.group;
         const bool real = tid < rows, rows_here = (tid & ~31) < rows;  // of this thread, of this warp
         const int limit = min(first_pos + token, len - 1), from = kvq_first_key(first_pos + token, a.window);
@@ -179,95 +199,122 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         float ref = kUnset, sum = 0.f;
 #pragma unroll 1
         for (int j = 0; j < (rows_here ? blocks : 0); ++j) {
-            bar_wait(s_full + 8 * mat, j & 1, &dead);
+            const int at = at_of(mat, j);
+            const uint32_t s_at = lanes + at * kKeys;
+            bar_wait(s_full + 8 * at, turn_of(j), &dead);
             __syncwarp();
             tmem_after();
             const int key0 = key_of(j);
             const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
             const bool whole = missing == 0 && key0 + kKeys - 1 <= min(low_limit, len - 1) && (key0 >= high_from || key0 + kKeys <= a.first);
-            // keys of chunk c (32 of them) that this row sees
-            const auto seen_of = [&](int c) {
+            // scores of keys of chunk c that this row does not see: -infinity
+            const auto mask = [&](int c, uint32_t(&s)[32]) {
                 const int last = limit - key0 - 32 * c, least = from - key0 - 32 * c, few = a.first - key0 - 32 * c;
                 uint32_t seen = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1;
                 seen &= (least <= 0 ? 0xffffffffu : least >= 32 ? 0u : ~0u << least) | (few >= 32 ? 0xffffffffu : few <= 0 ? 0u : (1u << few) - 1);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (missing >> (8 * (2 * c + i)) & 1) seen &= ~(0xffffu << (16 * i));
-                return seen;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (!(seen >> i & 1)) s[i] = 0xff800000u;
             };
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                uint32_t p[kHalf / 2];
-#pragma unroll 1
-                for (int round = 0;; ++round) {
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t s[kHalf / 32][32];
+            // probabilities of chunk c, two to a word, and their sums
+            const auto weigh = [&](int c, uint32_t(&s)[32], uint32_t* p, float2(&part)[2]) {
+                if (!whole) mask(c, s);
 #pragma unroll
-                    for (int c = 0; c < kHalf / 32; ++c) tmem_ask32(s_at + h * kHalf + 32 * c, s[c]);
-#pragma unroll
-                    for (int c = 0; c < kHalf / 32; ++c) {
-                        tmem_there32(s[c]);
-                        if (!whole) {
-                            const uint32_t seen = seen_of(h * (kHalf / 32) + c);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!(seen >> i & 1)) s[c][i] = 0xff800000u;  // -infinity
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float x = exp2_approx(fmaf(__uint_as_float(s[c][2 * i]), a.scale_log2, -ref)), y = exp2_approx(fmaf(__uint_as_float(s[c][2 * i + 1]), a.scale_log2, -ref));
-                            part[2 * (i & 1)] += x, part[2 * (i & 1) + 1] += y;
-                            p[16 * c + i] = pack2(x, y, BF);
-                        }
-                    }
-                    const float total = (part[0] + part[1]) + (part[2] + part[3]);
-                    if (round || !__any_sync(0xffffffffu, total > kBound)) {
-                        sum += total;
-                        break;
-                    }
-                    // rows that have outgrown their reference get another; what they have so far falls with it
-                    float now = ref;
-                    if (total > kBound) {
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int c = 0; c < kHalf / 32; ++c)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[c][i]));
-                        now = top * a.scale_log2 - kStart;
-                    }
-                    const float fall = exp2_approx(ref - now);
-                    ref = now, sum *= fall;
-                    if (j > 0 || h > 0) {
-                        bar_wait(h ? o_half + 8 * mat : o_done + 8 * mat, j - 1 + h & 1, &dead);  // the products of the half before
-                        __syncwarp();
-                        tmem_after();
-#pragma unroll 1
-                        for (int i = 0; i < D; i += 16) {
-                            uint32_t o[16];
-                            tmem_load16(o_at + i, o);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
-                            tmem_store16(o_at + i, o);
-                        }
-                        tmem_stored();
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(-ref, -ref));
+                    x.x = exp2_approx(x.x), x.y = exp2_approx(x.y);
+                    part[i & 1] = add2(part[i & 1], x);
+                    p[i] = pack2(x.x, x.y, BF);
                 }
+            };
+            const auto total_of = [](const float2(&part)[2]) {
+                const float2 x = add2(part[0], part[1]);
+                return x.x + x.y;
+            };
+            // Rows whose probabilities of chunks [c0, c1) outgrow the bound get another reference; what they have so far falls with it.
+            const auto outgrown = [&](float total, int c0, int c1) {
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int c = c0; c < c1; ++c) {
+                    uint32_t s[32];
+                    tmem_ask32(s_at + 32 * c, s);
+                    tmem_there32(s);
+                    if (!whole) mask(c, s);
 #pragma unroll
-                for (int c = 0; c < kHalf / 32; ++c) {
-                    uint32_t x[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = p[16 * c + i];
-                    tmem_store16(s_at + h * (kHalf / 2) + 16 * c, x);
+                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
                 }
+                const float now = total > kBound ? top * a.scale_log2 - kStart : ref, fall = exp2_approx(ref - now);
+                ref = now, sum *= fall;
+                if (j + c0 == 0) return;  // no products yet
+                // products so far are done: of the block before, of this one's first part
+                if (c0 > 0) bar_wait(o_half + 8 * at, turn_of(j), &dead);
+                else bar_wait(o_done + 8 * at_of(mat, j - 1), turn_of(j - 1), &dead);
+                __syncwarp();
+                tmem_after();
+#pragma unroll 1
+                for (int i = 0; i < D; i += 16) {
+                    uint32_t o[16];
+                    tmem_load16(o_at + i, o);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+                    tmem_store16(o_at + i, o);
+                }
+                tmem_stored();
+            };
+            const auto put = [&](int c, const uint32_t* p) {
+                uint32_t x[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = p[i];
+                tmem_store16(s_at + 16 * c, x);
+            };
+            const auto tell = [&](uint32_t b) {
                 tmem_stored();
                 tmem_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive((h ? p_full : p_half) + 8 * mat);
+                if (lane == 0) bar_arrive(b + 8 * at);
+            };
+            uint32_t s[2][32], p[16 * Z::kFirst];
+#pragma unroll 1
+            for (int round = 0;; ++round) {
+                float2 part[2] = {};
+                tmem_ask32(s_at, s[0]);
+                tmem_there32(s[0]);
+#pragma unroll
+                for (int c = 0; c < Z::kFirst; ++c) {  // the next chunk comes meanwhile
+                    tmem_ask32(s_at + 32 * (c + 1), s[c + 1 & 1]);
+                    weigh(c, s[c & 1], p + 16 * c, part);
+                    tmem_there32(s[c + 1 & 1]);
+                }
+                const float total = total_of(part);
+                if (round || !__any_sync(0xffffffffu, total > kBound)) {
+                    sum += total;
+                    break;
+                }
+                outgrown(total, 0, Z::kFirst);
             }
+#pragma unroll
+            for (int c = 0; c < Z::kFirst; ++c) put(c, p + 16 * c);
+            tell(p_half);
+#pragma unroll 1
+            for (int round = 0;; ++round) {
+                float2 part[2] = {};
+                weigh(Z::kFirst, s[Z::kFirst & 1], p, part);
+                const float total = total_of(part);
+                if (round || !__any_sync(0xffffffffu, total > kBound)) {
+                    sum += total;
+                    break;
+                }
+                outgrown(total, Z::kFirst, Z::kChunks);
+            }
+            put(Z::kFirst, p);
+            tell(p_full);
         }
         const bool some = blocks > 0 && rows_here;
         if (some) {
-            bar_wait(o_done + 8 * mat, blocks - 1 & 1, &dead);
+            bar_wait(o_done + 8 * at_of(mat, blocks - 1), turn_of(blocks - 1), &dead);
             __syncwarp();
             tmem_after();
         }
@@ -358,74 +405,81 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             }
         }
     } else if (wid == kSoftmaxWarps) {
-        // ---- matrix instructions: one lane issues them ----
-        const uint32_t leads = lane == 0;
-        const int n = __shfl_sync(0xffffffffu, blocks, 0), live = __shfl_sync(0xffffffffu, mats, 0);
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        const uint32_t q_low = operand_low((uint32_t)__cvta_generic_to_shared(sq)), ring_low = operand_low((uint32_t)__cvta_generic_to_shared(ring));
-        const uint32_t across = (uint32_t)(kKeys * 128 >> 4) << 16;  // V: from 64 dims to the next 64
-        const auto wait_for = [&](uint32_t b, uint32_t parity) {
-            bar_wait(b, parity, &dead);
-            __syncwarp();
-        };
-        const auto scores = [&](int mat, uint32_t k_block) {
+        // ---- matrix instructions: one thread waits and issues ----
+        if (elect_one()) {
+            const int n = blocks, live = mats;
+            const uint64_t q_at = operand_at((uint32_t)__cvta_generic_to_shared(sq)), ring_at = operand_at((uint32_t)__cvta_generic_to_shared(ring));
+            constexpr uint64_t kAcross = (uint64_t)((kKeys * 128 >> 4) - 1) << 16;  // V: from 64 dims to the next 64
+            const auto scores = [&](int j, int mat, uint64_t k_block) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                mma_smem<kKeys, kType>(tm + mat * kKeys, q_low + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
-                                       k_block + ((k / 4) * (kKeys * 128) + (k % 4) * 32 >> 4), k > 0, leads);
-            commit_to(s_full + 8 * mat, leads);
-        };
-        if (n > 0) {
-            bar_wait(q_full, 0, &dead, p_.tries);
-            wait_for(full, 0);
-            tmem_after();
-#pragma unroll
-            for (int mat = 0; mat < Z::kMats; ++mat)
-                if (mat < live) scores(mat, ring_low);
-            commit_to(vacant, leads);
-        }
-        int place_v = 1 % kPlaces, place_k = 2 % kPlaces;
-        uint32_t turn_v = 0, turn_k = 0;
+                for (int k = 0; k < D / 16; ++k)
+                    mma_smem_one<kKeys, kType>(tmem + at_of(mat, j) * kKeys, q_at + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
+                                               k_block + ((k / 4) * (kKeys * 128) + (k % 4) * 32 >> 4), k > 0);
+                commit_one(s_full + 8 * at_of(mat, j));
+            };
+            // places of the ring that the next block of K, of V has
+            int place_v = 1 % kPlaces, place_k = 0;
+            uint32_t turn_v = 0, turn_k = 0;
+            const auto next_k = [&] {
+                if ((place_k += 2) >= kPlaces) place_k -= kPlaces, turn_k ^= 1;
+            };
+            if (n > 0) {
+                bar_wait(q_full, 0, &dead, p_.tries);
 #pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-            // P.V of block j and the scores of block j + 1, matrix by matrix: while one's run, P of the other is made. They run in
-            // the order of issue, so the scores may take the place of the probabilities before them.
-            const uint32_t v_block = ring_low + (uint32_t)(place_v * (Z::kItem >> 4)) + across - (1u << 16), k_block = ring_low + (uint32_t)(place_k * (Z::kItem >> 4));
-            const bool more = j + 1 < n;
-#pragma unroll
-            for (int mat = 0; mat < Z::kMats; ++mat) {
-                if (mat >= live) break;
-                if (mat == 0) bar_wait(full + 8 * place_v, turn_v, &dead);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    wait_for((h ? p_full : p_half) + 8 * mat, j & 1);
+                for (int j = 0; j < min(n, Z::kBuffers); ++j) {
+                    bar_wait(full + 8 * place_k, turn_k, &dead);
                     tmem_after();
-#pragma unroll
-                    for (int k = 0; k < kHalf / 16; ++k)
-                        mma_tmem<D, kType | kShapeBAcross>(tm + Z::kO + mat * D, tm + mat * kKeys + h * (kHalf / 2) + 8 * k, v_block + ((h * kHalf + 16 * k) * 128 >> 4),
-                                                           h + k ? 1 : j, leads);
-                    commit_to(h ? o_done + 8 * mat : o_half + 8 * mat, leads);
-                }
-                if (more) {
-                    if (mat == 0) wait_for(full + 8 * place_k, turn_k);
-                    scores(mat, k_block);
+#pragma unroll 1
+                    for (int mat = 0; mat < live; ++mat) scores(j, mat, ring_at + (uint32_t)(place_k * (Z::kItem >> 4)));
+                    commit_one(vacant + 8 * place_k);
+                    next_k();
                 }
             }
-            commit_to(vacant + 8 * place_v, leads);
-            if (more) commit_to(vacant + 8 * place_k, leads);
-            if ((place_v += 2) >= kPlaces) place_v -= kPlaces, turn_v ^= 1;
-            if ((place_k += 2) >= kPlaces) place_k -= kPlaces, turn_k ^= 1;
+#pragma unroll 1
+            for (int j = 0; j < n; ++j) {
+                // P.V of block j and the scores of block j + kBuffers, matrix by matrix: while one's run, P of the other is made. They
+                // run in the order of issue, so the scores may take the place of the probabilities before them.
+                const uint64_t v_block = ring_at + (uint32_t)(place_v * (Z::kItem >> 4)) + kAcross, k_block = ring_at + (uint32_t)(place_k * (Z::kItem >> 4));
+                const bool more = j + Z::kBuffers < n;
+                bar_wait(full + 8 * place_v, turn_v, &dead);
+#pragma unroll 1
+                for (int mat = 0; mat < live; ++mat) {
+                    const int at = at_of(mat, j);
+                    const uint32_t o_at = tmem + Z::kO + mat * D, p_at = tmem + at * kKeys;
+                    bar_wait(p_half + 8 * at, turn_of(j), &dead);
+                    tmem_after();
+#pragma unroll
+                    for (int k = 0; k < 2 * Z::kFirst; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (16 * k * 128 >> 4), k ? 1 : j);
+                    commit_one(o_half + 8 * at);
+                    bar_wait(p_full + 8 * at, turn_of(j), &dead);
+                    tmem_after();
+#pragma unroll
+                    for (int k = 2 * Z::kFirst; k < kKeys / 16; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (16 * k * 128 >> 4), 1);
+                    commit_one(o_done + 8 * at);
+                    if (more) {
+                        if (mat == 0) bar_wait(full + 8 * place_k, turn_k, &dead);
+                        scores(j, mat, k_block);
+                    }
+                }
+                commit_one(vacant + 8 * place_v);
+                if (more) {
+                    commit_one(vacant + 8 * place_k);
+                    next_k();
+                }
+                if ((place_v += 2) >= kPlaces) place_v -= kPlaces, turn_v ^= 1;
+            }
+            // Nothing stays in flight, whatever happened: a barrier of its own stands behind everything, since a block that gave up may
+            // have run ahead of the others by several phases. Then the last arrival on each of these.
+            commit_one(all_done);
+            bar_drain(all_done, 1, &dead);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int times = Z::kBuffers == 2 ? (n + 1 - i) / 2 : i < live ? n : 0;
+                bar_drain(s_full + 8 * i, times, &dead), bar_drain(o_half + 8 * i, times, &dead), bar_drain(o_done + 8 * i, times, &dead);
+            }
+#pragma unroll
+            for (int i = 0; i < kPlaces; ++i) bar_drain(vacant + 8 * i, (2 * n - i + kPlaces - 1) / kPlaces, &dead);
         }
-        // Nothing stays in flight, whatever happened: a barrier of its own stands behind everything, since a block that gave up may
-        // have run ahead of the others by several phases. Then the last arrival on each of these.
-        __syncwarp();
-        commit_to(all_done, leads);
-        bar_drain(all_done, 1, &dead);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i < live) bar_drain(s_full + 8 * i, n, &dead), bar_drain(o_half + 8 * i, n, &dead), bar_drain(o_done + 8 * i, n, &dead);
-#pragma unroll
-        for (int i = 0; i < kPlaces; ++i) bar_drain(vacant + 8 * i, (2 * n - i + kPlaces - 1) / kPlaces, &dead);
         __syncwarp();
     } else {
         // ---- keys and values: a tile of 16 tokens to a lane, whole ones in boxes, others row by row with zeros between ----
@@ -439,7 +493,6 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             if (j < blocks && lane < kTiles && key < end) {
                 const int tile = key / kKvqTile, in_row = tile / v.block_tiles;
                 r = make_int2(__ldg(row + in_row), (tile - in_row * v.block_tiles) * kKvqTile);
-                if ((uint32_t)r.x >= (uint32_t)v.nb) kvq_error(v, kErrBadBlock), r.x = -1;
             }
             return r;
         };
@@ -449,11 +502,16 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         for (; items < 2 * blocks; ++items) {
             const int j = items >> 1, place = items % kPlaces, turn = items / kPlaces;
             const bool of_v = items & 1;
-            if (!of_v) at = next, next = find(j + 1);
-            if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
-            __syncwarp();
-            if (*static_cast<volatile int*>(&dead)) break;  // what is asked for is waited for below
             const int key0 = key_of(j), key = key0 + lane * kKvqTile;
+            if (!of_v) {
+                at = next, next = find(j + 1);
+                if ((uint32_t)at.x >= (uint32_t)v.nb) {
+                    if (lane < kTiles && key < end) kvq_error(v, kErrBadBlock);
+                    at.x = -1;
+                }
+            }
+            if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
+            if (__any_sync(0xffffffffu, *static_cast<volatile int*>(&dead))) break;  // what is asked for is waited for below
             if (!of_v && lane < kTiles) gone[j & 3][lane] = at.x < 0;
             const bool every = at.x >= 0 && key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first);
             const uint32_t boxes = __ballot_sync(0xffffffffu, every);

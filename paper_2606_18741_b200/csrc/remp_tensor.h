@@ -99,6 +99,29 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b_low,
         "r"(leads)
         : "memory");
 }
+
+// The same from one thread (that which elect_one names), with whole descriptors.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t is;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(is));
+    return is;
+}
+__device__ __forceinline__ uint64_t operand_at(uint32_t at) { return (uint64_t)kOperandHigh << 32 | operand_low(at); }
+template <int N, uint32_t kMore = 0>
+__device__ __forceinline__ void mma_smem_one(uint32_t d, uint64_t a, uint64_t b, uint32_t add) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b),
+                 "r"(kShape<N> | kMore), "r"(add)
+                 : "memory");
+}
+template <int N, uint32_t kMore = 0>
+__device__ __forceinline__ void mma_tmem_one(uint32_t d, uint32_t a, uint64_t b, uint32_t add) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b),
+                 "r"(kShape<N> | kMore), "r"(add)
+                 : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void for_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 #endif
