@@ -22,6 +22,8 @@
 
 #include <cuda.h>
 
+#include <numeric>
+
 #include "remp_kv_attend.h"
 #include "remp_kvq_device.h"
 #include "remp_tensor.h"
@@ -42,6 +44,7 @@ struct Prompt {
     static constexpr int kChunks = kKeys / 32, kFirst = kChunks - 1;  // of 32 keys; those of a block's first part, one makes the second
     static constexpr int kBuffers = D == 256 ? 2 : 1;                 // of the scores of a matrix
     static constexpr int kQ = kRowsM * D * 2, kItem = kKeys * D * 2;  // bytes of a matrix, of a block of K or of V
+    static constexpr int kEight = 8 * D * 2;                          // bytes of 8 keys: they lie together, 64 dims behind the other
     static constexpr int kPlaces = 5;                                 // of the ring
     static constexpr int kBytes = kMats * kQ + kPlaces * kItem + 1024;
     // columns of the tensor memory: S and P of each matrix and buffer, then O of each matrix
@@ -51,17 +54,19 @@ struct Prompt {
 };
 
 struct PromptArgs {
-    CUtensorMap k, v;          // [block][head][token][dim] of K and of V, in boxes of 16 tokens and 64 dims
+    CUtensorMap k, v;          // of K and of V, in boxes of a tile: [slice of a block and head][8 tokens][64 dims][token][dim]
+    int32_t i_block, i_head;   // from the slice of a block, of a head to the next
     KvAttendArgs t;
     int32_t row_blocks;        // of a sequence and KV head at most
     int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
     int32_t tries;             // of the wait for the queries
 };
 
-// 16 tokens of 64 dims of a head, in rows of 128 bytes whose 16-byte pieces change places, to `dst`; their bytes count for `bar`.
-__device__ __forceinline__ void bring_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int dim, int token, int head, int block) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
-                 "r"(dim), "r"(token), "r"(head), "r"(block)
+// A tile of a head to `dst`: 8 rows of 128 bytes whose 16-byte pieces change places, of each 64 dims, of each 8 tokens; its bytes
+// count for `bar`.
+__device__ __forceinline__ void bring_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int eighth, int slice) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %3, %3, %4, %5}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
+                 "r"(0), "r"(eighth), "r"(slice)
                  : "memory");
 }
 __device__ __forceinline__ void bar_arrive_expecting(uint32_t bar, uint32_t bytes) {
@@ -409,12 +414,13 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         if (elect_one()) {
             const int n = blocks, live = mats;
             const uint64_t q_at = operand_at((uint32_t)__cvta_generic_to_shared(sq)), ring_at = operand_at((uint32_t)__cvta_generic_to_shared(ring));
-            constexpr uint64_t kAcross = (uint64_t)((kKeys * 128 >> 4) - 1) << 16;  // V: from 64 dims to the next 64
+            // K and V: from 8 keys to the next 8; V, across the keys: from 64 dims to the next 64
+            constexpr uint64_t kOfK = (uint64_t)(Z::kEight - 1024 >> 4) << 32, kOfV = kOfK + ((uint64_t)((1024 >> 4) - 1) << 16);
             const auto scores = [&](int j, int mat, uint64_t k_block) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     mma_smem_one<kKeys, kType>(tmem + at_of(mat, j) * kKeys, q_at + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
-                                               k_block + ((k / 4) * (kKeys * 128) + (k % 4) * 32 >> 4), k > 0);
+                                               k_block + ((k / 4) * 1024 + (k % 4) * 32 >> 4), k > 0);
                 commit_one(s_full + 8 * at_of(mat, j));
             };
             // places of the ring that the next block of K, of V has
@@ -430,7 +436,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     bar_wait(full + 8 * place_k, turn_k, &dead);
                     tmem_after();
 #pragma unroll 1
-                    for (int mat = 0; mat < live; ++mat) scores(j, mat, ring_at + (uint32_t)(place_k * (Z::kItem >> 4)));
+                    for (int mat = 0; mat < live; ++mat) scores(j, mat, ring_at + (uint32_t)(place_k * (Z::kItem >> 4)) + kOfK);
                     commit_one(vacant + 8 * place_k);
                     next_k();
                 }
@@ -439,7 +445,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             for (int j = 0; j < n; ++j) {
                 // P.V of block j and the scores of block j + kBuffers, matrix by matrix: while one's run, P of the other is made. They
                 // run in the order of issue, so the scores may take the place of the probabilities before them.
-                const uint64_t v_block = ring_at + (uint32_t)(place_v * (Z::kItem >> 4)) + kAcross, k_block = ring_at + (uint32_t)(place_k * (Z::kItem >> 4));
+                const uint64_t v_block = ring_at + (uint32_t)(place_v * (Z::kItem >> 4)) + kOfV, k_block = ring_at + (uint32_t)(place_k * (Z::kItem >> 4)) + kOfK;
                 const bool more = j + Z::kBuffers < n;
                 bar_wait(full + 8 * place_v, turn_v, &dead);
 #pragma unroll 1
@@ -449,12 +455,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     bar_wait(p_half + 8 * at, turn_of(j), &dead);
                     tmem_after();
 #pragma unroll
-                    for (int k = 0; k < 2 * Z::kFirst; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (16 * k * 128 >> 4), k ? 1 : j);
+                    for (int k = 0; k < 2 * Z::kFirst; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (2 * k * Z::kEight >> 4), k ? 1 : j);
                     commit_one(o_half + 8 * at);
                     bar_wait(p_full + 8 * at, turn_of(j), &dead);
                     tmem_after();
 #pragma unroll
-                    for (int k = 2 * Z::kFirst; k < kKeys / 16; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (16 * k * 128 >> 4), 1);
+                    for (int k = 2 * Z::kFirst; k < kKeys / 16; ++k) mma_tmem_one<D, kType | kShapeBAcross>(o_at, p_at + 8 * k, v_block + (2 * k * Z::kEight >> 4), 1);
                     commit_one(o_done + 8 * at);
                     if (more) {
                         if (mat == 0) bar_wait(full + 8 * place_k, turn_k, &dead);
@@ -483,7 +489,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         __syncwarp();
     } else {
         // ---- keys and values: a tile of 16 tokens to a lane, whole ones in boxes, others row by row with zeros between ----
-        constexpr int kTiles = kKeys / kKvqTile, kChunk = kKeys * 128, kTile = kKvqTile * 128;  // 64 dims of a block, of a tile
+        constexpr int kTiles = kKeys / kKvqTile, kTile = 2 * Z::kEight;
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
         const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
         // This lane's tile of block j: its block (-1: not there) and first token in it. Asked for a block ahead.
@@ -523,16 +529,14 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     const int r = i / (D / 8), piece = i % (D / 8);
                     const bool real = id >= 0 && first_key + r < end && (first_key + r >= low_from || first_key + r < a.first);
                     const uint4 x = real ? *reinterpret_cast<const uint4*>(src + r * v.s_token + piece * 16) : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4*>(ring + place * Z::kItem + (piece / 8) * kChunk + t * kTile + r * 128 + (((piece % 8) ^ (r & 7)) << 4)) = x;
+                    *reinterpret_cast<uint4*>(ring + place * Z::kItem + t * kTile + (r / 8) * Z::kEight + (piece / 8) * 1024 + (r & 7) * 128 + (((piece % 8) ^ (r & 7)) << 4)) = x;
                 }
             }
             for_tensor_cores();
             __syncwarp();
             if (lane == 0) bar_arrive_expecting(full + 8 * place, __popc(boxes) * (kKvqTile * D * 2));
             __syncwarp();
-            if (every)
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c) bring_box(dst + c * kChunk + lane * kTile, of_v ? &p_.v : &p_.k, full + 8 * place, 64 * c, at.y, head, at.x);
+            if (every) bring_tile(dst + lane * kTile, of_v ? &p_.v : &p_.k, full + 8 * place, at.y / 8, at.x * p_.i_block + head * p_.i_head);
         }
         __syncwarp();
 #pragma unroll
@@ -571,9 +575,27 @@ cudaError_t launch(PromptArgs& p, bool bf, int sms, int max_rows, cudaStream_t s
 
 }  // namespace
 
+namespace {
+
+// Blocks and heads as one dimension of a tensor map: slices at the largest step that meets the heads of all blocks.
+struct Slices {
+    int64_t step, i_block, i_head, count;
+};
+Slices slices_of(const KvView& v) {
+    int64_t step = 0;
+    if (v.nb > 1) step = std::gcd(step, v.s_block);
+    if (v.kv_heads > 1) step = std::gcd(step, v.s_head);
+    if (step == 0) step = 16;  // a single slice
+    Slices s{step, v.nb > 1 ? v.s_block / step : 0, v.kv_heads > 1 ? v.s_head / step : 0, 0};
+    s.count = (v.nb - 1) * s.i_block + (v.kv_heads - 1) * s.i_head + 1;
+    return s;
+}
+
+}  // namespace
+
 bool kv_prompt_takes(const KvView& v) {
-    // strides of a tensor map
-    return v.nb > 0 && std::max(v.s_token, std::max(v.s_head, v.s_block)) < (int64_t)1 << 40;
+    // strides and coordinates of a tensor map
+    return v.nb > 0 && std::max(8 * v.s_token, std::max(v.s_head, v.s_block)) < (int64_t)1 << 40 && slices_of(v).count <= 0x7fffffff;
 }
 
 cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, int sms, int32_t max_rows, cudaStream_t stream) {
@@ -587,11 +609,13 @@ cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, i
     PromptArgs p{};
     p.t = a, p.splits = 1;
     const KvView& v = a.v;
-    const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)v.block_tiles * kKvqTile, (cuuint64_t)v.kv_heads, (cuuint64_t)v.nb};
-    const cuuint64_t strides[3] = {(cuuint64_t)v.s_token, (cuuint64_t)v.s_head, (cuuint64_t)v.s_block};
-    const cuuint32_t box[4] = {64, kKvqTile, 1, 1}, steps[4] = {1, 1, 1, 1};
+    const Slices s = slices_of(v);
+    p.i_block = (int32_t)s.i_block, p.i_head = (int32_t)s.i_head;
+    const cuuint64_t dims[5] = {64, 8, (cuuint64_t)head_dim / 64, (cuuint64_t)v.block_tiles * (kKvqTile / 8), (cuuint64_t)s.count};
+    const cuuint64_t strides[4] = {(cuuint64_t)v.s_token, 128, (cuuint64_t)(8 * v.s_token), (cuuint64_t)s.step};
+    const cuuint32_t box[5] = {64, 8, (cuuint32_t)head_dim / 64, kKvqTile / 8, 1}, steps[5] = {1, 1, 1, 1, 1};
     for (int i = 0; i < 2; ++i)
-        if (encode(i ? &p.v : &p.k, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, v.base + (i ? v.s_kv : 0), dims, strides, box, steps,
+        if (encode(i ? &p.v : &p.k, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, v.base + (i ? v.s_kv : 0), dims, strides, box, steps,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     return head_dim == 64 ? launch<64>(p, bf, sms, max_rows, stream)
