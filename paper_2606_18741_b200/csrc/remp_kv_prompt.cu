@@ -212,21 +212,34 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             const int key0 = key_of(j);
             const unsigned long long missing = *reinterpret_cast<const volatile unsigned long long*>(gone[j & 3]);
             const bool whole = missing == 0 && key0 + kKeys - 1 <= min(low_limit, len - 1) && (key0 >= high_from || key0 + kKeys <= a.first);
-            // scores of keys of chunk c that this row does not see: -infinity
-            const auto mask = [&](int c, uint32_t(&s)[32]) {
-                const int last = limit - key0 - 32 * c, least = from - key0 - 32 * c, few = a.first - key0 - 32 * c;
-                uint32_t seen = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1;
-                seen &= (least <= 0 ? 0xffffffffu : least >= 32 ? 0u : ~0u << least) | (few >= 32 ? 0xffffffffu : few <= 0 ? 0u : (1u << few) - 1);
+            if (!whole) {
+                // scores of keys that the row does not see become -infinity where they lie: few blocks have any
+#pragma unroll 1
+                for (int c = 0; c < Z::kChunks; ++c) {
+                    const int last = limit - key0 - 32 * c, least = from - key0 - 32 * c, few = a.first - key0 - 32 * c;
+                    uint32_t seen = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1;
+                    seen &= (least <= 0 ? 0xffffffffu : least >= 32 ? 0u : ~0u << least) | (few >= 32 ? 0xffffffffu : few <= 0 ? 0u : (1u << few) - 1);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (missing >> (8 * (2 * c + i)) & 1) seen &= ~(0xffffu << (16 * i));
+                    for (int i = 0; i < 2; ++i)
+                        if (missing >> (8 * (2 * c + i)) & 1) seen &= ~(0xffffu << (16 * i));
+                    uint32_t s[32];
+                    tmem_ask32(s_at + 32 * c, s);
+                    tmem_there32(s);
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (!(seen >> i & 1)) s[i] = 0xff800000u;
-            };
-            // probabilities of chunk c, two to a word, and their sums
-            const auto weigh = [&](int c, uint32_t(&s)[32], uint32_t* p, float2(&part)[2]) {
-                if (!whole) mask(c, s);
+                    for (int i = 0; i < 32; ++i)
+                        if (!(seen >> i & 1)) s[i] = 0xff800000u;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t x[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = s[16 * h + i];
+                        tmem_store16(s_at + 32 * c + 16 * h, x);
+                    }
+                }
+                tmem_stored();
+            }
+            // probabilities of a chunk, two to a word, and their sums
+            const auto weigh = [&](const uint32_t(&s)[32], uint32_t* p, float2(&part)[2]) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(-ref, -ref));
@@ -247,7 +260,6 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     uint32_t s[32];
                     tmem_ask32(s_at + 32 * c, s);
                     tmem_there32(s);
-                    if (!whole) mask(c, s);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
                 }
@@ -290,7 +302,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
 #pragma unroll
                 for (int c = 0; c < Z::kFirst; ++c) {  // the next chunk comes meanwhile
                     tmem_ask32(s_at + 32 * (c + 1), s[c + 1 & 1]);
-                    weigh(c, s[c & 1], p + 16 * c, part);
+                    weigh(s[c & 1], p + 16 * c, part);
                     tmem_there32(s[c + 1 & 1]);
                 }
                 const float total = total_of(part);
@@ -306,7 +318,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
 #pragma unroll 1
             for (int round = 0;; ++round) {
                 float2 part[2] = {};
-                weigh(Z::kFirst, s[Z::kFirst & 1], p, part);
+                weigh(s[Z::kFirst & 1], p, part);
                 const float total = total_of(part);
                 if (round || !__any_sync(0xffffffffu, total > kBound)) {
                     sum += total;
