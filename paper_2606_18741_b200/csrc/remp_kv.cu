@@ -12,7 +12,9 @@
 #include "remp_kv.h"
 
 #include <algorithm>
+#include <numeric>
 
+#include "remp_kv_boxes.h"
 #include "remp_rows.h"
 
 namespace remp {
@@ -223,6 +225,49 @@ remp_status kv_group(int32_t q_heads, int32_t kv_heads, int64_t num_tokens, int3
     if (g > 0x8000 || num_tokens * g * g > 0x7fffffffLL) return fail(REMP_ERR_SHAPE, "too many query rows");
     *group = g, *by_group = g == 1 ? 0 : (uint32_t)((0x100000000ULL + g - 1) / g);
     return REMP_OK;
+}
+
+namespace {
+
+// Blocks and heads as one dimension of a tensor map: slices at the largest step that meets the heads of all blocks.
+struct Slices {
+    int64_t step, i_block, i_head, count;
+};
+Slices slices_of(const KvView& v) {
+    int64_t step = 0;
+    if (v.nb > 1) step = std::gcd(step, v.s_block);
+    if (v.kv_heads > 1) step = std::gcd(step, v.s_head);
+    if (step == 0) step = 16;  // a single slice
+    Slices s{step, v.nb > 1 ? v.s_block / step : 0, v.kv_heads > 1 ? v.s_head / step : 0, 0};
+    s.count = (v.nb - 1) * s.i_block + (v.kv_heads - 1) * s.i_head + 1;
+    return s;
+}
+
+}  // namespace
+
+bool kv_boxes_take(const KvView& v) {
+    // strides and coordinates of a tensor map
+    return v.nb > 0 && std::max(8 * v.s_token, std::max(v.s_head, v.s_block)) < (int64_t)1 << 40 && slices_of(v).count <= 0x7fffffff;
+}
+
+cudaError_t kv_boxes(const KvView& v, int32_t head_dim, bool bf, KvBoxes* boxes) {
+    using Encode = decltype(&cuTensorMapEncodeTiled);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) == cudaSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+    }();
+    if (!encode) return cudaErrorNotSupported;
+    const Slices s = slices_of(v);
+    boxes->i_block = (int32_t)s.i_block, boxes->i_head = (int32_t)s.i_head;
+    const cuuint64_t dims[5] = {64, 8, (cuuint64_t)head_dim / 64, (cuuint64_t)v.block_tiles * (kKvqTile / 8), (cuuint64_t)s.count};
+    const cuuint64_t strides[4] = {(cuuint64_t)v.s_token, 128, (cuuint64_t)(8 * v.s_token), (cuuint64_t)s.step};
+    const cuuint32_t box[5] = {64, 8, (cuuint32_t)head_dim / 64, kKvqTile / 8, 1}, steps[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i)
+        if (encode(i ? &boxes->v : &boxes->k, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, v.base + (i ? v.s_kv : 0), dims, strides, box, steps,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    return cudaSuccess;
 }
 
 }  // namespace remp

@@ -19,6 +19,7 @@
 #include "remp_attend_parts.h"
 #include "remp_kv.h"
 #include "remp_kv_attend.h"
+#include "remp_kv_boxes.h"
 
 namespace remp {
 
@@ -419,7 +420,7 @@ extern "C" remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_b
     const int64_t max_rows = (int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group;
     const bool bf = dtype == REMP_DTYPE_BFLOAT, wide = max_rows > 8;
     cudaError_t e;
-    if (max_rows > kPromptRows && kv_prompt_takes(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
+    if (max_rows > kPromptRows && kv_boxes_take(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
     else if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, bf, sms, stream) : launch<64, 1>(a, bf, sms, stream);
     else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, bf, sms, stream) : launch<128, 1>(a, bf, sms, stream);
     else e = launch<256, 1>(a, bf, sms, stream);

@@ -16,8 +16,7 @@ struct KvAttendArgs {
     int32_t room;      // tokens that a row of the table holds
 };
 
-// remp_kv_prompt.cu: many queries of a sequence, for caches that it takes
-bool kv_prompt_takes(const KvView& v);
+// remp_kv_prompt.cu: many queries of a sequence, of a cache that comes in boxes
 cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, int sms, int32_t max_rows, cudaStream_t stream);
 
 }  // namespace remp

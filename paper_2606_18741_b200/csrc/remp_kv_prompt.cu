@@ -20,11 +20,8 @@
 // error bit 4. Whatever happens, the issuing warp leaves when everything that it has issued is done and every barrier that it
 // has committed to has been arrived at, and the fetching warp when its copies are done.
 
-#include <cuda.h>
-
-#include <numeric>
-
 #include "remp_kv_attend.h"
+#include "remp_kv_boxes.h"
 #include "remp_kvq_device.h"
 #include "remp_tensor.h"
 
@@ -54,59 +51,12 @@ struct Prompt {
 };
 
 struct PromptArgs {
-    CUtensorMap k, v;          // of K and of V, in boxes of a tile: [slice of a block and head][8 tokens][64 dims][token][dim]
-    int32_t i_block, i_head;   // from the slice of a block, of a head to the next
+    KvBoxes boxes;
     KvAttendArgs t;
     int32_t row_blocks;        // of a sequence and KV head at most
     int32_t whole, splits;     // units that one thread block does alone; parts of the keys of each unit behind them
     int32_t tries;             // of the wait for the queries
 };
-
-// A tile of a head to `dst`: 8 rows of 128 bytes whose 16-byte pieces change places, of each 64 dims, of each 8 tokens; its bytes
-// count for `bar`.
-__device__ __forceinline__ void bring_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int eighth, int slice) {
-    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %3, %3, %4, %5}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
-                 "r"(0), "r"(eighth), "r"(slice)
-                 : "memory");
-}
-__device__ __forceinline__ void bar_arrive_expecting(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; mov.b64 {%0, %1}, x; }"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-
-// Loads of 32 columns: asked for, and there (nothing that uses them can be moved before that).
-__device__ __forceinline__ void tmem_ask32(uint32_t at, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(at));
-}
-__device__ __forceinline__ void tmem_there32(uint32_t (&r)[32]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
-                   "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
-                   "+r"(r[28]), "+r"(r[29])
-                 :
-                 : "memory");
-    asm volatile("" : "+r"(r[30]), "+r"(r[31])::"memory");
-}
 
 template <int D, bool BF>
 __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const __grid_constant__ PromptArgs p_) {
@@ -427,12 +377,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             const int n = blocks, live = mats;
             const uint64_t q_at = operand_at((uint32_t)__cvta_generic_to_shared(sq)), ring_at = operand_at((uint32_t)__cvta_generic_to_shared(ring));
             // K and V: from 8 keys to the next 8; V, across the keys: from 64 dims to the next 64
-            constexpr uint64_t kOfK = (uint64_t)(Z::kEight - 1024 >> 4) << 32, kOfV = kOfK + ((uint64_t)((1024 >> 4) - 1) << 16);
+            constexpr uint64_t kOfK = keys_apart(Z::kEight), kOfV = kOfK + ((uint64_t)((1024 >> 4) - 1) << 16);
             const auto scores = [&](int j, int mat, uint64_t k_block) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    mma_smem_one<kKeys, kType>(tmem + at_of(mat, j) * kKeys, q_at + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
-                                               k_block + ((k / 4) * 1024 + (k % 4) * 32 >> 4), k > 0);
+                    mma_smem_one(tmem + at_of(mat, j) * kKeys, q_at + (mat * Z::kQ + (k / 4) * (kRowsM * 128) + (k % 4) * 32 >> 4),
+                                               k_block + ((k / 4) * 1024 + (k % 4) * 32 >> 4), kShape<kKeys> | kType, k > 0);
                 commit_one(s_full + 8 * at_of(mat, j));
             };
             // places of the ring that the next block of K, of V has
@@ -548,7 +498,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             __syncwarp();
             if (lane == 0) bar_arrive_expecting(full + 8 * place, __popc(boxes) * (kKvqTile * D * 2));
             __syncwarp();
-            if (every) bring_tile(dst + lane * kTile, of_v ? &p_.v : &p_.k, full + 8 * place, at.y / 8, at.x * p_.i_block + head * p_.i_head);
+            if (every) bring_tile(dst + lane * kTile, of_v ? &p_.boxes.v : &p_.boxes.k, full + 8 * place, at.y / 8, at.x * p_.boxes.i_block + head * p_.boxes.i_head);
         }
         __syncwarp();
 #pragma unroll
@@ -587,49 +537,10 @@ cudaError_t launch(PromptArgs& p, bool bf, int sms, int max_rows, cudaStream_t s
 
 }  // namespace
 
-namespace {
-
-// Blocks and heads as one dimension of a tensor map: slices at the largest step that meets the heads of all blocks.
-struct Slices {
-    int64_t step, i_block, i_head, count;
-};
-Slices slices_of(const KvView& v) {
-    int64_t step = 0;
-    if (v.nb > 1) step = std::gcd(step, v.s_block);
-    if (v.kv_heads > 1) step = std::gcd(step, v.s_head);
-    if (step == 0) step = 16;  // a single slice
-    Slices s{step, v.nb > 1 ? v.s_block / step : 0, v.kv_heads > 1 ? v.s_head / step : 0, 0};
-    s.count = (v.nb - 1) * s.i_block + (v.kv_heads - 1) * s.i_head + 1;
-    return s;
-}
-
-}  // namespace
-
-bool kv_prompt_takes(const KvView& v) {
-    // strides and coordinates of a tensor map
-    return v.nb > 0 && std::max(8 * v.s_token, std::max(v.s_head, v.s_block)) < (int64_t)1 << 40 && slices_of(v).count <= 0x7fffffff;
-}
-
 cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, int sms, int32_t max_rows, cudaStream_t stream) {
-    using Encode = decltype(&cuTensorMapEncodeTiled);
-    static const Encode encode = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) == cudaSuccess ? reinterpret_cast<Encode>(f) : nullptr;
-    }();
-    if (!encode) return cudaErrorNotSupported;
     PromptArgs p{};
     p.t = a, p.splits = 1;
-    const KvView& v = a.v;
-    const Slices s = slices_of(v);
-    p.i_block = (int32_t)s.i_block, p.i_head = (int32_t)s.i_head;
-    const cuuint64_t dims[5] = {64, 8, (cuuint64_t)head_dim / 64, (cuuint64_t)v.block_tiles * (kKvqTile / 8), (cuuint64_t)s.count};
-    const cuuint64_t strides[4] = {(cuuint64_t)v.s_token, 128, (cuuint64_t)(8 * v.s_token), (cuuint64_t)s.step};
-    const cuuint32_t box[5] = {64, 8, (cuuint32_t)head_dim / 64, kKvqTile / 8, 1}, steps[5] = {1, 1, 1, 1, 1};
-    for (int i = 0; i < 2; ++i)
-        if (encode(i ? &p.v : &p.k, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, v.base + (i ? v.s_kv : 0), dims, strides, box, steps,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return cudaErrorInvalidValue;
+    if (cudaError_t e = kv_boxes(a.v, head_dim, bf, &p.boxes)) return e;
     return head_dim == 64 ? launch<64>(p, bf, sms, max_rows, stream)
            : head_dim == 128 ? launch<128>(p, bf, sms, max_rows, stream) : launch<256>(p, bf, sms, max_rows, stream);
 }

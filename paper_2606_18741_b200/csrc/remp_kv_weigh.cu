@@ -9,7 +9,8 @@
 // queries come in the same order of dims, so K needs no shared memory. Work is the list of all (sequence, KV head, tile), cut evenly
 // over the warps of the grid; a warp asks for its next tile before it works on this one.
 
-#include "remp_kv.h"
+#include "remp_kv_boxes.h"
+#include "remp_kv_weigh.h"
 #include "remp_kvq_device.h"
 
 namespace remp {
@@ -17,18 +18,7 @@ namespace remp {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-
-struct WeighArgs {
-    KvView v;
-    KvqRows q;
-    const float* lse;
-    float* weights;
-    int64_t stride;
-    float scale_log2;
-    int32_t group, q_heads, window, first, fresh;
-    uint32_t by_group;
-    int32_t room;  // tokens that a row of the table and a row of the weights hold
-};
+constexpr int kWideRows = 32;  // rows up to which this kernel takes a sequence; above, the wide one
 
 struct Seq {
     KvqSpan x;
@@ -230,6 +220,10 @@ extern "C" remp_status remp_kv_weigh(const remp_kv_pool* pool, const remp_kvq_ba
     a.room = (int32_t)std::min<int64_t>(std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, kKvqMost), stride);
     const bool bf = dtype == REMP_DTYPE_BFLOAT;
     const int d = pool->head_dim;
+    if ((int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group > kWideRows && kv_boxes_take(a.v)) {
+        REMP_CUDA(launch_kv_weigh_wide(a, d, bf, sms, static_cast<cudaStream_t>(stream_)));
+        return REMP_OK;
+    }
     const auto kernel = d == 64    ? (bf ? kv_weigh_kernel<64, true> : kv_weigh_kernel<64, false>)
                         : d == 128 ? (bf ? kv_weigh_kernel<128, true> : kv_weigh_kernel<128, false>)
                                    : (bf ? kv_weigh_kernel<256, true> : kv_weigh_kernel<256, false>);
