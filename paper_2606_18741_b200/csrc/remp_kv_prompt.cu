@@ -39,13 +39,12 @@ struct Prompt {
     static constexpr int kMats = D == 256 ? 1 : 2, kRows = kMats * kRowsM;
     static constexpr int kKeys = D == 256 ? 64 : 128;
     static constexpr int kChunks = kKeys / 32, kFirst = kChunks - 1;  // of 32 keys; those of a block's first part, one makes the second
-    static constexpr int kBuffers = D == 256 ? 2 : 1;                 // of the scores of a matrix
     static constexpr int kQ = kRowsM * D * 2, kItem = kKeys * D * 2;  // bytes of a matrix, of a block of K or of V
     static constexpr int kEight = 8 * D * 2;                          // bytes of 8 keys: they lie together, 64 dims behind the other
     static constexpr int kPlaces = 5;                                 // of the ring
     static constexpr int kBytes = kMats * kQ + kPlaces * kItem + 1024;
-    // columns of the tensor memory: S and P of each matrix and buffer, then O of each matrix
-    static constexpr int kO = kMats * kBuffers * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
+    // columns of the tensor memory: S and P of two matrices, or of two blocks of keys of one matrix, then O of each matrix
+    static constexpr int kO = 2 * kKeys, kUsed = kO + kMats * D, kColumns = kUsed <= 256 ? 256 : 512;
     static constexpr int kSoftmaxWarps = 4 * kMats, kThreads = (kSoftmaxWarps + 2) * 32;
     static constexpr int kPartFloats = kRows * (D + 2);
 };
@@ -102,14 +101,16 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
     // for each matrix: scores, probabilities and products of the halves of a block; queries; places of the ring (block j of K is item 2j, of V item 2j + 1)
     const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars);
     const uint32_t s_full = bar, p_full = bar + 16, o_half = bar + 32, o_done = bar + 48, p_half = bar + 64, q_full = bar + 80, all_done = bar + 88, full = bar + 96, vacant = full + 8 * kPlaces;
-    const int mats = rows > kRowsM ? 2 : 1;
+    // Two matrices take turns: while one's products run, P of the other is made. One alone has two buffers of scores instead, those
+    // of the next block are there when P of this one is done.
+    const int mats = rows > kRowsM ? 2 : 1, buffers = 3 - mats;
     // scores of block j: their place, and of the barriers that go with it; the phase of these. What a barrier had before that
     // phase is done when the scores are there, so no wait for a phase meets the one two before it.
-    const auto at_of = [](int mat, int j) { return mat + j % Z::kBuffers; };
-    const auto turn_of = [](int j) { return j / Z::kBuffers & 1; };
+    const auto at_of = [&](int mat, int j) { return mat + (j & buffers - 1); };
+    const auto turn_of = [&](int j) { return j >> buffers - 1 & 1; };
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            const int warps = max(1, min(4, (rows - (Z::kBuffers == 2 ? 0 : i) * kRowsM + 31) / 32));  // those without rows make no P
+            const int warps = max(1, min(4, (rows - (buffers == 2 ? 0 : i) * kRowsM + 31) / 32));  // those without rows make no P
             bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, warps), bar_init(p_full + 8 * i, warps), bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
         }
         for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, 1), bar_init(vacant + 8 * i, 1);
@@ -391,24 +392,26 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             const auto next_k = [&] {
                 if ((place_k += 2) >= kPlaces) place_k -= kPlaces, turn_k ^= 1;
             };
+            const auto scores_alone = [&](int j) {  // of every matrix, behind what was issued
+                bar_wait(full + 8 * place_k, turn_k, &dead);
+                tmem_after();
+#pragma unroll 1
+                for (int mat = 0; mat < live; ++mat) scores(j, mat, ring_at + (uint32_t)(place_k * (Z::kItem >> 4)) + kOfK);
+                commit_one(vacant + 8 * place_k);
+                next_k();
+            };
             if (n > 0) {
                 bar_wait(q_full, 0, &dead, p_.tries);
-#pragma unroll 1
-                for (int j = 0; j < min(n, Z::kBuffers); ++j) {
-                    bar_wait(full + 8 * place_k, turn_k, &dead);
-                    tmem_after();
-#pragma unroll 1
-                    for (int mat = 0; mat < live; ++mat) scores(j, mat, ring_at + (uint32_t)(place_k * (Z::kItem >> 4)) + kOfK);
-                    commit_one(vacant + 8 * place_k);
-                    next_k();
-                }
+                scores_alone(0);
             }
 #pragma unroll 1
             for (int j = 0; j < n; ++j) {
-                // P.V of block j and the scores of block j + kBuffers, matrix by matrix: while one's run, P of the other is made. They
-                // run in the order of issue, so the scores may take the place of the probabilities before them.
+                // P.V of block j and the scores of the next. Of one matrix these come first and take the other buffer, whose
+                // products were issued a block ago; of two they follow, matrix by matrix, and take the place of the probabilities
+                // before them: instructions run in the order of issue.
+                if (buffers == 2 && j + 1 < n) scores_alone(j + 1);
                 const uint64_t v_block = ring_at + (uint32_t)(place_v * (Z::kItem >> 4)) + kOfV, k_block = ring_at + (uint32_t)(place_k * (Z::kItem >> 4)) + kOfK;
-                const bool more = j + Z::kBuffers < n;
+                const bool more = buffers == 1 && j + 1 < n;
                 bar_wait(full + 8 * place_v, turn_v, &dead);
 #pragma unroll 1
                 for (int mat = 0; mat < live; ++mat) {
@@ -426,7 +429,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     commit_one(o_done + 8 * at);
                     if (more) {
                         if (mat == 0) bar_wait(full + 8 * place_k, turn_k, &dead);
-                        scores(j, mat, k_block);
+                        scores(j + 1, mat, k_block);
                     }
                 }
                 commit_one(vacant + 8 * place_v);
@@ -442,7 +445,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             bar_drain(all_done, 1, &dead);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int times = Z::kBuffers == 2 ? (n + 1 - i) / 2 : i < live ? n : 0;
+                const int times = buffers == 2 ? (n + 1 - i) / 2 : n;
                 bar_drain(s_full + 8 * i, times, &dead), bar_drain(o_half + 8 * i, times, &dead), bar_drain(o_done + 8 * i, times, &dead);
             }
 #pragma unroll

@@ -18,7 +18,9 @@ namespace remp {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kWideRows = 32;  // rows up to which this kernel takes a sequence; above, the wide one
+// Rows up to which this kernel takes a sequence; above, the wide one. Two sequences of 16383 tokens, 8 rows to a query: 18 us here and 20
+// there with 2 queries, 25 and 20 with 4, 59 and 23 with 16; 64 sequences of 500 tokens: 20 and 27, 27 and 27, 63 and 35.
+constexpr int kWideRows = 24;
 
 struct Seq {
     KvqSpan x;
