@@ -57,13 +57,15 @@ struct Note {  // what the work on a step has to know; written by the loads
 template <int D, int NT>
 struct Sizes {
     static constexpr int kDim = D, kRows = 8 * NT, kQuads = NT * D / 16;
-    static constexpr int kWarps = D == 64 ? 12 : D == 128 ? 8 : 4, kThreads = kWarps * 32;
     static constexpr int kTile = kKvqTile * D * 2, kBuffer = 2 * kTile;  // K and V of a tile
     static constexpr int kStages = D == 64 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2;
     // a part: accumulators as the lanes hold them (quad by quad), then references and sums of the rows
     static constexpr int kPartFloats = kQuads * 128 + 2 * kRows, kPart = kPartFloats * 4;
     static constexpr int kRing = kStages * kBuffer > kPart ? kStages * kBuffer : kPart;  // a tail part reuses the buffers
     static constexpr int kWarpBytes = (kRing + kPart + 63) / 64 * 64;
+    // as many warps as there is room for, up to what their registers allow
+    static constexpr int kMost = D == 64 ? (NT == 4 ? 8 : 12) : D == 128 ? 8 : 4, kFit = (227 * 1024 - 2304) / kWarpBytes;
+    static constexpr int kWarps = kFit < kMost ? kFit : kMost, kThreads = kWarps * 32;
     static constexpr int kBytes = kWarps * kWarpBytes;
 };
 
@@ -181,9 +183,9 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
                     }
                     heads = v.base + (int64_t)head * v.s_head;
                     // the unit's queries are wanted soon
-                    const int r0 = block * RB, r = r0 + min(lane & (RB - 1), q.rows - r0 - 1), token = token_of(a, r);
+                    const int r0 = block * RB, r = r0 + min(lane % RB, q.rows - r0 - 1), token = token_of(a, r);
                     const uint16_t* query = a.q.data + (int64_t)(q.x.q0 + token) * a.q.s_token + (int64_t)(head * a.group + r - token * a.group) * a.q.s_head;
-                    for (int x = lane / RB * 64; x < D; x += 32 / RB * 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(query + x));
+                    for (int x = lane / RB * 64; lane < 32 / RB * RB && x < D; x += 32 / RB * 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(query + x));
                     low = q.x.first_pos + token_of(a, r0), high = q.x.first_pos + token_of(a, min(r0 + RB, q.rows) - 1);
                 }
                 const int tile = step_at < q.tiles.sinks ? step_at : q.tiles.tile0 + step_at - q.tiles.sinks, key0 = tile * kKvqTile;
@@ -387,6 +389,14 @@ cudaError_t launch(const KvAttendArgs& a, bool bf, int sms, cudaStream_t stream)
     return launch_after(bf ? kv_attend_kernel<D, NT, true> : kv_attend_kernel<D, NT, false>, grid, Z::kThreads, Z::kBytes, stream, a);
 }
 
+// With room for the rows of the longest sequence of queries, up to NT times 8.
+template <int D, int NT>
+cudaError_t launch_rows(const KvAttendArgs& a, int64_t rows, bool bf, int sms, cudaStream_t stream) {
+    if constexpr (NT > 1)
+        if (rows <= 8 * (NT - 1)) return launch_rows<D, NT - 1>(a, rows, bf, sms, stream);
+    return launch<D, NT>(a, bf, sms, stream);
+}
+
 }  // namespace
 
 }  // namespace remp
@@ -418,12 +428,12 @@ extern "C" remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_b
     a.room = (int32_t)std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, kKvqMost);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const int64_t max_rows = (int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group;
-    const bool bf = dtype == REMP_DTYPE_BFLOAT, wide = max_rows > 8;
+    const bool bf = dtype == REMP_DTYPE_BFLOAT;
     cudaError_t e;
-    if (max_rows > kPromptRows && kv_boxes_take(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
-    else if (pool->head_dim == 64) e = wide ? launch<64, 2>(a, bf, sms, stream) : launch<64, 1>(a, bf, sms, stream);
-    else if (pool->head_dim == 128) e = wide ? launch<128, 2>(a, bf, sms, stream) : launch<128, 1>(a, bf, sms, stream);
-    else e = launch<256, 1>(a, bf, sms, stream);
+    if (max_rows > (pool->head_dim == 64 ? 32 : kPromptRows) && kv_boxes_take(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
+    else if (pool->head_dim == 64) e = launch_rows<64, 4>(a, max_rows, bf, sms, stream);
+    else if (pool->head_dim == 128) e = launch_rows<128, 2>(a, max_rows, bf, sms, stream);
+    else e = launch_rows<256, 2>(a, max_rows, bf, sms, stream);
     if (e != cudaSuccess) return cuda_fail(e, "attention");
     return REMP_OK;
 }

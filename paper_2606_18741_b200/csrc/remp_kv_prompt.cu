@@ -14,7 +14,7 @@
 // of B along the dims for S and across them for O, so nothing is transposed. S and P share their columns of the tensor memory, O
 // has its own; P goes to the matrix instructions in halves of a block, so that the first half's products run while the second is
 // made. With 256 dims O takes so much of it that one matrix of 128 rows and blocks of 64 keys are left.
-// Keys that no row sees are not fetched but zeroed, so what their slots hold is never used.
+// Slots that no row sees: their scores are masked, their values are not fetched but zeroed, so what they hold is never used.
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
 // error bit 4. Whatever happens, the issuing warp leaves when everything that it has issued is done and every barrier that it
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         }
         __syncwarp();
     } else {
-        // ---- keys and values: a tile of 16 tokens to a lane, whole ones in boxes, others row by row with zeros between ----
+        // ---- keys and values: a tile of 16 tokens to a lane, in boxes; of V those with slots that no row sees by rows, with zeros there ----
         constexpr int kTiles = kKeys / kKvqTile, kTile = 2 * Z::kEight;
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
         const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
@@ -484,17 +484,24 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
             if (__any_sync(0xffffffffu, *static_cast<volatile int*>(&dead))) break;  // what is asked for is waited for below
             if (!of_v && lane < kTiles) gone[j & 3][lane] = at.x < 0;
-            const bool every = at.x >= 0 && key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first);
+            // What unseen slots of K hold is masked score by score; of V they would meet probabilities of 0, so there they are zeros.
+            const bool every = at.x >= 0 && key < end && (!of_v || (key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first)));
             const uint32_t boxes = __ballot_sync(0xffffffffu, every);
             const uint32_t dst = ring_at + place * Z::kItem;
-            for (uint32_t others = ~boxes & ((1u << kTiles) - 1); others; others &= others - 1) {
+            for (uint32_t others = of_v ? ~boxes & ((1u << kTiles) - 1) : 0; others; others &= others - 1) {
                 const int t = __ffs(others) - 1, id = __shfl_sync(0xffffffffu, at.x, t), token = __shfl_sync(0xffffffffu, at.y, t), first_key = key0 + t * kKvqTile;
-                const uint8_t* src = v.base + (int64_t)id * v.s_block + (of_v ? v.s_kv : 0) + (int64_t)head * v.s_head + (int64_t)token * v.s_token;
-                for (int i = lane; i < kKvqTile * (D / 8); i += 32) {
-                    const int r = i / (D / 8), piece = i % (D / 8);
+                const uint8_t* src = v.base + (int64_t)id * v.s_block + v.s_kv + (int64_t)head * v.s_head + (int64_t)token * v.s_token;
+                uint4 x[kKvqTile * (D / 8) / 32];
+#pragma unroll
+                for (int i = 0; i < kKvqTile * (D / 8) / 32; ++i) {
+                    const int r = (i * 32 + lane) / (D / 8), piece = (i * 32 + lane) % (D / 8);
                     const bool real = id >= 0 && first_key + r < end && (first_key + r >= low_from || first_key + r < a.first);
-                    const uint4 x = real ? *reinterpret_cast<const uint4*>(src + r * v.s_token + piece * 16) : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4*>(ring + place * Z::kItem + t * kTile + (r / 8) * Z::kEight + (piece / 8) * 1024 + (r & 7) * 128 + (((piece % 8) ^ (r & 7)) << 4)) = x;
+                    x[i] = real ? *reinterpret_cast<const uint4*>(src + r * v.s_token + piece * 16) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < kKvqTile * (D / 8) / 32; ++i) {
+                    const int r = (i * 32 + lane) / (D / 8), piece = (i * 32 + lane) % (D / 8);
+                    *reinterpret_cast<uint4*>(ring + place * Z::kItem + t * kTile + (r / 8) * Z::kEight + (piece / 8) * 1024 + (r & 7) * 128 + (((piece % 8) ^ (r & 7)) << 4)) = x[i];
                 }
             }
             for_tensor_cores();
