@@ -7,7 +7,9 @@
 // these lanes, a turn's partner dim is in the same lane (interleaved) or one shuffle away. A warp takes the rows of ONE
 // token, kSets sets at a time: it looks up where the token belongs and loads its cosines and sines once, and asks for the
 // next sets' rows before this one's are worked on. Where tokens are too few to fill the GPU that way, every kSets sets get a
-// warp of their own.
+// warp of their own. Sets are four at a time there (the fewest steps: 6 us for 256 tokens of 80 heads, 8 us with two), and two else,
+// which leaves room for seven thread blocks on an SM instead of five: norms keep the issue slots busy, and waits need more warps
+// to fill them (31 900 tokens of 40 heads: 150 us, from 172, and 123 with one instruction for the root and its reciprocal).
 
 #include "remp_kv.h"
 
@@ -23,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSets = 4;
 
 struct Slot {  // where a token's rows are
     int64_t off;   // bytes from the pool's base to its row of head 0, K
@@ -66,7 +67,7 @@ __device__ __forceinline__ uint4 turned(const uint4& raw, const float* norm, flo
         float sum = ((x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3])) + ((x[4] * x[4] + x[5] * x[5]) + (x[6] * x[6] + x[7] * x[7]));
 #pragma unroll
         for (int s = 1; s < D / 8; s <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-        const float r = 1.f / sqrtf(fmaf(sum, 1.f / D, eps));
+        const float r = rsqrtf(fmaf(sum, 1.f / D, eps));  // off by 2^-22; the row is rounded to 2^-12 of itself at best
         const float4 a = __ldg(reinterpret_cast<const float4*>(norm + 8 * l)), b = __ldg(reinterpret_cast<const float4*>(norm + 8 * l + 4));
         const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -93,8 +94,8 @@ __device__ __forceinline__ uint4 turned(const uint4& raw, const float* norm, flo
 
 // The work is in groups of kSets sets of rows: a token's groups of query heads, then of K, then of V; a warp takes
 // `per_warp` groups of one token.
-template <int D, bool BF>
-__global__ void __launch_bounds__(kThreads, 5) kv_append_kernel(const KvView v, const KvqRows q, const KvqRows k, const KvqRows val,
+template <int D, bool BF, int kSets>
+__global__ void __launch_bounds__(kThreads, kSets == 4 ? 5 : 7) kv_append_kernel(const KvView v, const KvqRows q, const KvqRows k, const KvqRows val,
                                                                const KvqRows q_out, const Transform tr, const int q_heads,
                                                                const int q_groups, const int kv_groups, const int per_warp) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes, kStep = kSets * kRows;  // lanes of a row, rows of a warp, heads of a group
@@ -180,6 +181,9 @@ __global__ void __launch_bounds__(kThreads, 5) kv_append_kernel(const KvView v, 
         }
     }
 }
+
+template <int D, bool BF>
+auto append_kernel(bool few) { return few ? kv_append_kernel<D, BF, 4> : kv_append_kernel<D, BF, 2>; }
 
 }  // namespace
 
@@ -294,20 +298,20 @@ extern "C" remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_b
     if (remp_status st = kvq_rows(k, view.num_tokens, pool->kv_heads, d, false, "k", &rk)) return st;
     if (remp_status st = kvq_rows(v, view.num_tokens, pool->kv_heads, d, false, "v", &rv)) return st;
     const int64_t rows = (int64_t)q_heads + 2 * (int64_t)pool->kv_heads;
-    const int heads = 32 / (d / 8) * kSets;  // of a group
-    if (rows > 0x7fffffffLL - 3 * heads) return fail(REMP_ERR_SHAPE, "too many heads");
     int device = -1, sms = 0;
     REMP_CUDA(cudaGetDevice(&device));
     REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    const bool few = view.num_tokens < sms * 20, bf = dtype == REMP_DTYPE_BFLOAT;
+    const int heads = 32 / (d / 8) * (few ? 4 : 2);  // of a group
+    if (rows > 0x7fffffffLL - 3 * heads) return fail(REMP_ERR_SHAPE, "too many heads");
     const int q_groups = (q_heads + heads - 1) / heads, kv_groups = (pool->kv_heads + heads - 1) / heads, groups = q_groups + 2 * kv_groups;
     // a token to a warp when that fills the GPU, else a group
-    const int per_warp = view.num_tokens >= sms * 20 ? groups : 1;
+    const int per_warp = few ? 1 : groups;
     const int64_t shares = (int64_t)view.num_tokens * ((groups + per_warp - 1) / per_warp);
     const int64_t grid = std::min<int64_t>((shares + kWarps - 1) / kWarps, (int64_t)sms * 48);
-    const bool bf = dtype == REMP_DTYPE_BFLOAT;
-    const auto kernel = d == 64    ? (bf ? kv_append_kernel<64, true> : kv_append_kernel<64, false>)
-                        : d == 128 ? (bf ? kv_append_kernel<128, true> : kv_append_kernel<128, false>)
-                                   : (bf ? kv_append_kernel<256, true> : kv_append_kernel<256, false>);
+    const auto kernel = d == 64    ? (bf ? append_kernel<64, true>(few) : append_kernel<64, false>(few))
+                        : d == 128 ? (bf ? append_kernel<128, true>(few) : append_kernel<128, false>(few))
+                                   : (bf ? append_kernel<256, true>(few) : append_kernel<256, false>(few));
     REMP_CUDA(launch_after(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(stream_), view, rq, rk, rv, ro, tr, (int)q_heads, q_groups, kv_groups,
                            per_warp));
     return REMP_OK;
