@@ -420,9 +420,9 @@ remp_status remp_kvq_attend(const remp_kvq_pool* pool, const remp_kvq_batch* bat
                             const remp_kvq_rows* out, int32_t q_heads, int32_t dtype, float scale, int32_t window,
                             float* lse, void* workspace, void* stream);
 
-/* A test aid, for the whole process: how often a thread block of the prompt kernel of remp_kvq_attend or remp_kv_attend polls the barrier that its queries
- * arrive at before it gives up (0: never; negative: the built-in limit). It then waits for nothing else, writes NaN to its
- * outputs and sets error bit 4. */
+/* A test aid, for the whole process: how often a thread block of the kernels for many rows of remp_kvq_attend, remp_kv_attend and
+ * remp_kv_weigh polls the barrier that its queries arrive at before it gives up (0: never; negative: the built-in limit). It then waits for
+ * nothing else, writes NaN to its outputs and sets error bit 4. */
 void remp_kvq_set_wait_limit(int32_t tries);
 
 /* ---- serving from a cache of 16-bit values, between two topology switches ----
@@ -448,6 +448,9 @@ remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch
  *   lse        DEVICE float [num_tokens][q_heads] or NULL
  *   workspace  DEVICE, remp_kv_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call leaves it
  *              ready for the next. Calls that may overlap need workspaces of their own.
+ * With at most 16 rows (max_queries * q_heads / kv_heads; 32 with 64 dims) a probability keeps 16 bits and more on its way to the
+ * values; with more it is rounded to the cache's type. Sums are in 32 bits throughout. Where a wait of the kernel for more
+ * rows runs out its outputs are NaN (error bit 4).
  * The result does not depend on the order in which thread blocks run. */
 int64_t remp_kv_workspace_bytes(void);
 remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
@@ -461,7 +464,8 @@ remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch
  *   lse      DEVICE float [num_tokens][q_heads], as remp_kv_attend gives it; rows with -infinity count nothing
  *   weights  DEVICE float [num_seqs][kv_heads][stride]; of sequences longer than `stride` the positions behind it are left out
  *            (error bit 1)
- * Each weight is added up by one warp in a fixed order. */
+ * Each weight is added up in a fixed order, so the result does not depend on the run. With more than 24 rows (max_queries * q_heads /
+ * kv_heads) another kernel works; where a wait of its runs out, the weights that it has not written are NaN (error bit 4). */
 remp_status remp_kv_weigh(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q, int32_t q_heads,
                           int32_t dtype, float scale, int32_t window, int32_t first, const float* lse, float* weights,
                           int64_t stride, int32_t fresh, void* stream);

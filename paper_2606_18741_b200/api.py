@@ -490,8 +490,8 @@ def remp_kvq_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float
 
 
 def remp_kvq_set_wait_limit(tries: int) -> None:
-    """A test aid, for the whole process: how often a thread block of remp_kvq_attend for prompts polls for its queries before it
-    gives up (0: never, negative: the built-in limit). What gave up is NaN, and bit 4 of the batch's error word."""
+    """A test aid, for the whole process: how often a thread block of the kernels for many rows (remp_kvq_attend, remp_kv_attend,
+    remp_kv_weigh) polls for its queries before it gives up (0: never, negative: the built-in limit). What gave up is NaN, and bit 4 of the batch's error word."""
     _lib.load().remp_kvq_set_wait_limit(tries)
 
 

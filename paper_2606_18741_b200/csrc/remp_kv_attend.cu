@@ -7,7 +7,7 @@
 //
 // Roles: a tile is 16 tokens of one head. S^T[16 tokens][8 rows] = K.Q^T and O^T[D][8 rows] += V^T.P^T, so the eight query
 // heads of a KV head fill the 8 columns of m16n8k16; P^T goes from accumulator to operand layout with one matrix transpose
-// for each 8 tokens. NT = 2 takes 16 rows and is used when 8 do not hold a sequence's rows.
+// for each 8 tokens. NT = 2 takes 16 rows and is used when 8 do not hold a sequence's rows; 64 dims leave registers for 24 and 32.
 //
 // Bound: HBM. Work is the list of all (sequence, row block, KV head, tile), cut evenly over the thread blocks and within one evenly
 // over its warps, so ragged batches and single long sequences fill the GPU alike. A warp streams its tiles through a ring in
@@ -27,7 +27,10 @@ namespace {
 
 constexpr float kSlack = 4.f, kRoom = 14.f, kBound = 16384.f;  // log2, log2, 2^kRoom
 
-constexpr int kPromptRows = 16;  // rows up to which this kernel takes a sequence; above, the prompt kernel
+// Rows up to which this kernel takes a sequence; above, the prompt kernel. 24 sequences of 8 KV heads, us in a graph, here and there: 128
+// dims, 24 rows, windows of 2048: 68 (three times 8 rows) and 66, 3000 tokens: 82 and 70, 2 x 30000: 76 and 57; 64 dims, 3000 tokens, 24
+// rows: 48 and 68, 32 rows: 60 and 68.
+constexpr int kPromptRows = 16;
 
 struct Seq {  // one sequence's share of the list
     KvqSpan x;

@@ -3,17 +3,23 @@
 //
 // Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
 // matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*scale - ref), O += P.V, with a
-// running reference for each row that moves only when the probabilities of half a block outgrow kBound.
+// running reference for each row that moves only when the probabilities of a part of a block outgrow kBound.
 // Rounding: P is rounded to the cache's type, the only one that the matrix instructions take beside V; S, O, sums and references are
 // in 32 bits.
 //
 // Bound: tensor cores (4*D flops for each row and key) and, as closely, the exponentials (one for each row and key; 16 a cycle of an
-// SM). Eight warps compute P (a row to a thread), one issues the matrix instructions, which run for one matrix while P of the other
-// is made, one brings K and V. Q and a ring of blocks of K and of V lie in shared memory in rows of 128 bytes, 16-byte
-// pieces exchanged within 8 rows (piece ^ (row & 7)), as 16-byte asynchronous copies bring them: the keys of a block are rows
+// SM). Eight warps compute P (a row to a thread), one thread issues the matrix instructions, which run for one matrix while P of the
+// other is made, one warp brings K and V. Q and a ring of blocks of K and of V lie in shared memory in rows of 128 bytes, 16-byte
+// pieces exchanged within 8 rows (piece ^ (row & 7)), as bulk tensor copies of a tile bring them: the keys of a block are rows
 // of B along the dims for S and across them for O, so nothing is transposed. S and P share their columns of the tensor memory, O
-// has its own; P goes to the matrix instructions in halves of a block, so that the first half's products run while the second is
-// made. With 256 dims O takes so much of it that one matrix of 128 rows and blocks of 64 keys are left.
+// has its own; P goes to the matrix instructions in two parts, so that the products of three quarters of a block run while the last
+// is made. With 256 dims O takes so much of it that one matrix of 128 rows and blocks of 64 keys are left.
+//
+// Measured, 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 128 dims (us in a graph): 752 with 16-byte copies by three
+// warps; 570 with boxes of 64 dims; 553 with one thread that waits and issues (a warp took 200 cycles for each wait and 80 for each
+// instruction); 473 with boxes of all dims (a box costs the copy engine some 100 cycles, 2 KB or 4); 438 with masks out of the loop:
+// 1.1 PFLOP/s. A quarter, third or half of the exponentials as polynomials took 459, 467, 479: with two warps on a scheduler the instructions
+// that this adds cost more than the exponentials that it saves.
 // Slots that no row sees: their scores are masked, their values are not fetched but zeroed, so what they hold is never used.
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
@@ -30,7 +36,7 @@ namespace remp {
 namespace {
 
 constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
-constexpr float kBound = 16384.f;    // of the sum of half a block's probabilities
+constexpr float kBound = 16384.f;    // of the sum of the probabilities of a part of a block
 constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
 constexpr int kMostSplits = 64;
 

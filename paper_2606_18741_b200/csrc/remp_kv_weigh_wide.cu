@@ -8,7 +8,8 @@
 // Bound: the exponentials (one for each row and key, 16 a cycle of an SM; the products of 128 dims take half as long). A thread
 // block takes a range of the keys of one sequence and KV head. Eight warps weigh, four for the even chunks of 32 rows and four for
 // the odd ones; one thread issues the matrix instructions, a block of keys ahead (two buffers of S^T); one warp brings K through a
-// ring. The rows that see a key are a range of them, so a mask is two numbers for each key and round.
+// ring. The rows that see a key are a range of them, so a mask is two numbers for each key and round. 2 x 32 queries of 32 heads over
+// 16383 tokens of 4 KV heads, 128 dims: 23 us, 93 in the kernel for few rows.
 //
 // Every wait is on a barrier in shared memory and bounded. A block that gives up goes on without waiting, writes NaN and sets
 // error bit 4; it leaves when all that it has asked for is done.
