@@ -443,7 +443,8 @@ remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch
  * j <= p; with window > 0 those with j > p - window or j < first (the first tokens stay visible; window = 0: all, whatever
  * `first` is). Heads, errors, lse, rows that see nothing and lengths beyond the table row as for remp_kvq_attend. Slots that no
  * row of a sequence sees are not used and may hold anything; a NaN or an infinity in V that a row of the batch sees may reach the other rows of
- * its sequence and KV head that the call computes together with it.
+ * its sequence and KV head that the call computes together with it. Finite values in V may be of any size (in bfloat16 those below 2^-70
+ * lose bits where the sums fall below the normal numbers of 32 bits).
  *   scale      positive
  *   lse        DEVICE float [num_tokens][q_heads] or NULL
  *   workspace  DEVICE, remp_kv_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call leaves it

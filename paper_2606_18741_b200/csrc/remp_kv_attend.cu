@@ -1,7 +1,8 @@
 // Attention over a cache of 16-bit values for few queries per sequence (decode, drafts, short continuations).
 //
-// Mathematics: softmax with a running reference, p = 2^(x - ref). A reference moves only when the sum of a lane's probabilities of a
-// tile passes 2^kRoom, by kSlack further than needed, which one vote for each tile finds out; accumulators are seldom rescaled.
+// Mathematics: softmax with a running reference, p = 2^(x - ref). A reference moves only when a lane's sum of probabilities passes
+// 2^room, by `slack` further than needed, which one vote for each tile finds out; accumulators are seldom rescaled. Sums of all
+// lanes, warps and thread blocks stay below 1 in bfloat16, so that sums of p V stay below V's largest number, whatever that is.
 // Rounding: a probability goes to the matrix instructions as two numbers of the cache's type, what rounds it and what is left, so it
 // keeps 16 bits and more (bfloat16 alone would give every probability an error of 2^-9); scores, references, sums and outputs are in 32 bits.
 //
@@ -25,7 +26,15 @@ namespace remp {
 
 namespace {
 
-constexpr float kSlack = 4.f, kRoom = 14.f, kBound = 16384.f;  // log2, log2, 2^kRoom
+// References. bfloat16: a lane's sum of all its probabilities stays at 2^-17; eight lanes, twelve warps and 512 thread blocks have at
+// most 2^-1.4 of a row. A new reference puts the largest probability 14 powers of two below, far enough for most sequences
+// (131072 tokens that weigh the same move it twice), and as p and V have the same exponents, nothing is lost on the way for V of
+// 2^-70 and more. Half: its 2^-14 to 2^16 have to hold probabilities, and its largest V times 2^31 of them fits 32 bits, so only
+// the sum of a tile is held below 2^14.
+template <bool BF>
+struct Refs {
+    static constexpr float room = BF ? -17.f : 14.f, slack = BF ? 14.f : 4.f, bound = BF ? 0x1p-17f : 0x1p14f;
+};
 
 // Rows up to which this kernel takes a sequence; above, the prompt kernel. 24 sequences of 8 KV heads, us in a graph, here and there: 128
 // dims, 24 rows, windows of 2048: 68 (three times 8 rows) and 66, 3000 tokens: 82 and 70, 2 x 30000: 76 and 57; 64 dims, 3000 tokens, 24
@@ -86,6 +95,7 @@ template <int D, int NT, bool BF>
 __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(const __grid_constant__ KvAttendArgs a) {
     using Z = Sizes<D, NT>;
     constexpr int RB = Z::kRows, kWarps = Z::kWarps, kThreads = Z::kThreads, kStages = Z::kStages, kPieces = D / 8;
+    using Ref = Refs<BF>;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long warp_sum[kWarps];
     __shared__ int first_at[kWarps], first_seq[kWarps];  // where a warp's share begins: sequences from here, at this place in the list
@@ -291,7 +301,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
                 }
             }
             // probabilities against the references as they are, or against higher ones where their sums pass the room
-            float p[NT][4], tsum[NT][2];
+            float p[NT][4], held[NT][2];  // held: the sums with this tile; half: of this tile
 #pragma unroll 1
             for (int round = 0;; ++round) {
                 float most = 0.f;
@@ -299,19 +309,21 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
                 for (int c = 0; c < NT; ++c) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) p[c][e] = exp2_approx(s[c][e] - ref[c][e & 1]);
-                    tsum[c][0] = p[c][0] + p[c][2], tsum[c][1] = p[c][1] + p[c][3];
-                    most = max3(most, tsum[c][0], tsum[c][1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) held[c][e] = p[c][e] + p[c][e + 2] + (BF ? sum[c][e] : 0.f);
+                    most = max3(most, held[c][0], held[c][1]);
                 }
-                if (round || !__any_sync(0xffffffffu, most > kBound)) break;
+                if (round || !__any_sync(0xffffffffu, most > Ref::bound)) break;
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(s[c][e], s[c][e + 2]);
+                        float top = fmaxf(s[c][e], s[c][e + 2]), all = held[c][e];
 #pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        for (int d = 4; d < 32; d <<= 1)
+                            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d)), all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, d));
                         float now = ref[c][e];
-                        if (top - now > kRoom - 1.f) now = top + kSlack - kRoom;  // two of them may be this large
+                        if (all > Ref::bound) now = fmaxf(top + Ref::slack - Ref::room, BF ? now + Ref::slack : now);
                         const float fall = exp2_approx(ref[c][e] - now);
                         ref[c][e] = now, sum[c][e] *= fall;
 #pragma unroll
@@ -321,7 +333,7 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
             uint32_t high_p[NT][2], low_p[NT][2];
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
-                sum[c][0] += tsum[c][0], sum[c][1] += tsum[c][1];
+                sum[c][0] = BF ? held[c][0] : sum[c][0] + held[c][0], sum[c][1] = BF ? held[c][1] : sum[c][1] + held[c][1];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t w = pack2(p[c][2 * h], p[c][2 * h + 1], BF);

@@ -3,7 +3,7 @@
 //
 // Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
 // matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*scale - ref), O += P.V, with a
-// running reference for each row that moves only when the probabilities of a part of a block outgrow kBound.
+// running reference for each row that moves only when its probabilities outgrow a bound.
 // Rounding: P is rounded to the cache's type, the only one that the matrix instructions take beside V; S, O, sums and references are
 // in 32 bits.
 //
@@ -36,9 +36,17 @@ namespace remp {
 namespace {
 
 constexpr float kUnset = -3e38f;     // reference of a row that has seen nothing
-constexpr float kBound = 16384.f;    // of the sum of the probabilities of a part of a block
-constexpr float kStart = 8.f;        // log2 of the largest probability when a reference is set
 constexpr int kMostSplits = 64;
+
+// References. bfloat16: a row's sum of all its probabilities stays at `bound`, so the 64 parts that its keys may be split into have
+// at most 1/2, and sums of p V stay below V's largest number; a new reference puts the largest probability at 2^start, 20 powers
+// of two below (about a million tokens that weigh the same move it once), and as p and V have the same exponents, nothing is lost
+// on the way for V of 2^-70 and more. Half: its 2^-14 to 2^16 have to hold probabilities, and its largest V times 2^31 of them
+// fits 32 bits, so only the sum of a part of a block is bounded.
+template <bool BF>
+struct Refs {
+    static constexpr float bound = BF ? 0x1p-7f : 0x1p14f, start = BF ? -27.f : 8.f, lift = 20.f;
+};
 
 template <int D>
 struct Prompt {
@@ -66,6 +74,7 @@ struct PromptArgs {
 template <int D, bool BF>
 __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const __grid_constant__ PromptArgs p_) {
     using Z = Prompt<D>;
+    using Ref = Refs<BF>;
     constexpr uint32_t kType = BF ? kShapeBfloat : 0;
     constexpr int kSoftmaxWarps = Z::kSoftmaxWarps, kRows = Z::kRows, kKeys = Z::kKeys, kPlaces = Z::kPlaces;
     const KvAttendArgs& a = p_.t;
@@ -210,7 +219,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                 return x.x + x.y;
             };
             // Rows whose probabilities of chunks [c0, c1) outgrow the bound get another reference; what they have so far falls with it.
-            const auto outgrown = [&](float total, int c0, int c1) {
+            const auto outgrown = [&](float held, int c0, int c1) {
                 float top = -INFINITY;
 #pragma unroll 1
                 for (int c = c0; c < c1; ++c) {
@@ -220,7 +229,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
 #pragma unroll
                     for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
                 }
-                const float now = total > kBound ? top * a.scale_log2 - kStart : ref, fall = exp2_approx(ref - now);
+                float now = ref;
+                if (held > Ref::bound) now = fmaxf(top * a.scale_log2 - Ref::start, BF ? ref + Ref::lift : ref);
+                const float fall = exp2_approx(ref - now);
                 ref = now, sum *= fall;
                 if (j + c0 == 0) return;  // no products yet
                 // products so far are done: of the block before, of this one's first part
@@ -262,12 +273,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                     weigh(s[c & 1], p + 16 * c, part);
                     tmem_there32(s[c + 1 & 1]);
                 }
-                const float total = total_of(part);
-                if (round || !__any_sync(0xffffffffu, total > kBound)) {
+                const float total = total_of(part), held = BF ? sum + total : total;
+                if (round || !__any_sync(0xffffffffu, held > Ref::bound)) {
                     sum += total;
                     break;
                 }
-                outgrown(total, 0, Z::kFirst);
+                outgrown(held, 0, Z::kFirst);
             }
 #pragma unroll
             for (int c = 0; c < Z::kFirst; ++c) put(c, p + 16 * c);
@@ -276,12 +287,12 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             for (int round = 0;; ++round) {
                 float2 part[2] = {};
                 weigh(s[Z::kFirst & 1], p, part);
-                const float total = total_of(part);
-                if (round || !__any_sync(0xffffffffu, total > kBound)) {
+                const float total = total_of(part), held = BF ? sum + total : total;
+                if (round || !__any_sync(0xffffffffu, held > Ref::bound)) {
                     sum += total;
                     break;
                 }
-                outgrown(total, Z::kFirst, Z::kChunks);
+                outgrown(held, Z::kFirst, Z::kChunks);
             }
             put(Z::kFirst, p);
             tell(p_full);
