@@ -3,8 +3,10 @@
 // Mathematics: softmax with a running reference, p = 2^(x - ref). A reference moves only when a lane's sum of probabilities passes
 // 2^room, by `slack` further than needed, which one vote for each tile finds out; accumulators are seldom rescaled. Sums of all
 // lanes, warps and thread blocks stay below 1 in bfloat16, so that sums of p V stay below V's largest number, whatever that is.
-// Rounding: a probability goes to the matrix instructions as two numbers of the cache's type, what rounds it and what is left, so it
-// keeps 16 bits and more (bfloat16 alone would give every probability an error of 2^-9); scores, references, sums and outputs are in 32 bits.
+// Rounding: a probability goes to the matrix instructions as two numbers of the cache's type, its first bits and what is left, so it
+// keeps 16 bits and more (bfloat16 alone would give every probability an error of 2^-9); scores, references, sums and outputs are in
+// 32 bits. The first is rounded towards 0 and the second is never 0, so that an infinity in V meets two numbers above 0
+// and stays one.
 //
 // Roles: a tile is 16 tokens of one head. S^T[16 tokens][8 rows] = K.Q^T and O^T[D][8 rows] += V^T.P^T, so the eight query
 // heads of a KV head fill the 8 columns of m16n8k16; P^T goes from accumulator to operand layout with one matrix transpose
@@ -336,10 +338,9 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
                 sum[c][0] = BF ? held[c][0] : sum[c][0] + held[c][0], sum[c][1] = BF ? held[c][1] : sum[c][1] + held[c][1];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t w = pack2(p[c][2 * h], p[c][2 * h + 1], BF);
-                    const float2 f = BF ? make_float2(bf_low(w), bf_high(w)) : __half22float2(*reinterpret_cast<const __half2*>(&w));
-                    high_p[c][h] = transpose8(w);
-                    low_p[c][h] = transpose8(pack2(p[c][2 * h] - f.x, p[c][2 * h + 1] - f.y, BF));
+                    uint32_t high, low;
+                    split2<BF>(p[c][2 * h], p[c][2 * h + 1], &high, &low);
+                    high_p[c][h] = transpose8(high), low_p[c][h] = transpose8(low);
                 }
             }
             {
