@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weigh_wide_kernel(const __grid
             if (__any_sync(0xffffffffu, *static_cast<volatile int*>(&dead))) break;  // what is asked for is waited for below
             if (lane < kTiles) gone[item & 7][lane] = !there;
             const uint32_t boxes = __ballot_sync(0xffffffffu, there);
+            __syncwarp();  // all lanes' marks before the arrival that tells of them: a vote orders no memory
             if (lane == 0) bar_arrive_expecting(full + 8 * place, __popc(boxes) * (kKvqTile * D * 2));
             __syncwarp();
             if (there) bring_tile(ring_at + place * Z::kItem + lane * (2 * Z::kEight), &p_.boxes.k, full + 8 * place, at.y / 8, at.x * p_.boxes.i_block + head * p_.boxes.i_head);
