@@ -442,10 +442,12 @@ remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch
 /* Attention over the cache: out = softmax(scale * q.K^T).V for every row of the batch. A row at position p sees the positions
  * j <= p; with window > 0 those with j > p - window or j < first (the first tokens stay visible; window = 0: all, whatever
  * `first` is). Heads, errors, lse, rows that see nothing and lengths beyond the table row as for remp_kvq_attend. Slots that no
- * row of a sequence sees are not used and may hold anything; a NaN or an infinity in V that a row of the batch sees may reach the other rows of
- * its sequence and KV head that the call computes together with it. Finite values in V may be of any size (in bfloat16 those below 2^-70
- * lose bits where the sums fall below the normal numbers of 32 bits). An infinity in V gives the rows that see it that infinity in its dim; where both
- * signs are seen, NaN; where their probability of it is below 2^-90 (half: 2^-32) of their largest, one or the other.
+ * row of a sequence sees are not used and may hold anything; table entries of pages that no row sees (behind the length, between
+ * the first tokens and the windows) may name anything, also for remp_kv_weigh. A NaN or an infinity in V that a row of the batch
+ * sees may reach the other rows of its sequence and KV head that the call computes together with it. Finite values in V may be
+ * of any size (in bfloat16 those below 2^-70 lose bits where the sums fall below the normal numbers of 32 bits). An infinity in V
+ * gives the rows that see it that infinity in its dim; where both signs are seen, NaN; where their probability of it is below 2^-90
+ * (half: 2^-32) of their largest, one or the other.
  *   scale      positive
  *   lse        DEVICE float [num_tokens][q_heads] or NULL
  *   workspace  DEVICE, remp_kv_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call leaves it

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
     __shared__ uint32_t tmem_at;
     __shared__ int dead;
     __shared__ int is_last;
-    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there
+    __shared__ __align__(8) uint8_t gone[4][8];  // of a block of keys: tiles that are not there, or that no row sees
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const KvView& v = a.v;
@@ -474,11 +474,13 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         constexpr int kTiles = kKeys / kKvqTile, kTile = 2 * Z::kEight;
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
         const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+        // Whether a row sees something of the tile from `key` on; others are not looked up: their pages may have been given back.
+        const auto wanted = [&](int key) { return lane < kTiles && key < end && (key + kKvqTile > low_from || key < a.first); };
         // This lane's tile of block j: its block (-1: not there) and first token in it. Asked for a block ahead.
         const auto find = [&](int j) {
             int2 r = make_int2(-1, 0);
             const int key = key_of(j) + lane * kKvqTile;
-            if (j < blocks && lane < kTiles && key < end) {
+            if (j < blocks && wanted(key)) {
                 const int tile = key / kKvqTile, in_row = tile / v.block_tiles;
                 r = make_int2(__ldg(row + in_row), (tile - in_row * v.block_tiles) * kKvqTile);
             }
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             if (!of_v) {
                 at = next, next = find(j + 1);
                 if ((uint32_t)at.x >= (uint32_t)v.nb) {
-                    if (lane < kTiles && key < end) kvq_error(v, kErrBadBlock);
+                    if (wanted(key)) kvq_error(v, kErrBadBlock);
                     at.x = -1;
                 }
             }
@@ -502,7 +504,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             if (__any_sync(0xffffffffu, *static_cast<volatile int*>(&dead))) break;  // what is asked for is waited for below
             if (!of_v && lane < kTiles) gone[j & 3][lane] = at.x < 0;
             // What unseen slots of K hold is masked score by score; of V they would meet probabilities of 0, so there they are zeros.
-            const bool every = at.x >= 0 && key < end && (!of_v || (key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first)));
+            const bool every = at.x >= 0 && (!of_v || (key + kKvqTile <= end && (key >= low_from || key + kKvqTile <= a.first)));
             const uint32_t boxes = __ballot_sync(0xffffffffu, every);
             const uint32_t dst = ring_at + place * Z::kItem;
             for (uint32_t others = of_v ? ~boxes & ((1u << kTiles) - 1) : 0; others; others &= others - 1) {

@@ -115,9 +115,12 @@ __global__ void __launch_bounds__(kThreads, D == 256 ? 1 : 2) kv_weigh_kernel(co
             }
         }
         const int tile = step < q.tiles.sinks ? step : q.tiles.tile0 + step - q.tiles.sinks;
-        const int in_row = tile / v.block_tiles, id = __ldg(v.tables + (int64_t)seq * v.max_blocks + in_row);
-        next_key = tile * kKvqTile, next_there = (uint32_t)id < (uint32_t)v.nb;
-        if (!next_there && lane == 0) kvq_error(v, kErrBadBlock);
+        next_key = tile * kKvqTile;
+        // tiles that no row sees are in the list of a fresh call only, to get 0; their pages may have been given back
+        const bool seen = next_key + kKvqTile > kvq_first_key(q.x.first_pos, a.window) || next_key < a.first;
+        const int in_row = tile / v.block_tiles, id = seen ? __ldg(v.tables + (int64_t)seq * v.max_blocks + in_row) : -1;
+        next_there = (uint32_t)id < (uint32_t)v.nb;
+        if (seen && !next_there && lane == 0) kvq_error(v, kErrBadBlock);
         const uint8_t* src = v.base + (int64_t)id * v.s_block + (int64_t)head * v.s_head + (int64_t)(tile - in_row * v.block_tiles) * kKvqTile * v.s_token + g * v.s_token + 16 * t;
 #pragma unroll
         for (int h = 0; h < 2; ++h)

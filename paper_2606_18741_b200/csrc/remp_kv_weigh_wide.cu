@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weigh_wide_kernel(const __grid
     __shared__ __align__(8) uint64_t bars[6 + 2 * kPlaces];
     __shared__ __align__(16) float norms[Z::kRows];  // of a round's rows: -lse in powers of two, -infinity for rows that count nothing
     __shared__ float halves[2][kKeys];
-    __shared__ __align__(8) uint8_t gone[8][8];      // of a block of keys: tiles that are not there
+    __shared__ __align__(8) uint8_t gone[8][8];      // of a block of keys: tiles that are not there, or that no row sees
     __shared__ uint32_t tmem_at;
     __shared__ int dead, silent;                     // the block has given up; the round in which rows were met that count nothing
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -217,10 +217,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weigh_wide_kernel(const __grid
         constexpr int kTiles = kKeys / kKvqTile;
         const int32_t* row = v.tables + (int64_t)seq * v.max_blocks;
         const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+        // Whether a row sees something of the tile from `key` on; others are not looked up: their pages may have been given back.
+        const int seen_from = kvq_first_key(first_pos, a.window);
+        const auto wanted = [&](int key) { return lane < kTiles && key < len && (key + kKvqTile > seen_from || key < a.first); };
         const auto find = [&](int j) {  // this lane's tile of block j: its block (-1: not asked for) and first token in it
             int2 r = make_int2(-1, 0);
             const int key = key_of(j) + lane * kKvqTile;
-            if (lane < kTiles && key < len) {
+            if (wanted(key)) {
                 const int tile = key / kKvqTile, in_row = tile / v.block_tiles;
                 r = make_int2(__ldg(row + in_row), (tile - in_row * v.block_tiles) * kKvqTile);
             }
@@ -234,8 +237,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weigh_wide_kernel(const __grid
             const int2 at = next;
             if (++j == blocks) j = 0;
             next = find(j);
-            const bool wanted = lane < kTiles && key < len, there = wanted && (uint32_t)at.x < (uint32_t)v.nb;
-            if (wanted && !there) kvq_error(v, kErrBadBlock);
+            const bool there = (uint32_t)at.x < (uint32_t)v.nb;
+            if (!there && wanted(key)) kvq_error(v, kErrBadBlock);
             if (turn > 0) bar_wait(vacant + 8 * place, (turn - 1) & 1, &dead);
             if (__any_sync(0xffffffffu, *static_cast<volatile int*>(&dead))) break;  // what is asked for is waited for below
             if (lane < kTiles) gone[item & 7][lane] = !there;
