@@ -504,9 +504,17 @@ def _workspace_bytes() -> int:
 
 def make_kv_pool(buffer, num_blocks: int, kv_heads: int, head_dim: int, block_size: int, layer: int = 0,
                  strides: Optional[dict] = None) -> RempKvqPool:
-    """remp_kv_pool of one layer of a rank's pool of 16-bit values (a CUDA tensor; strides in bytes as for make_shards). Its
-    calls take the batches of make_kvq_batch."""
+    """remp_kv_pool of one layer of a rank's pool of 16-bit values (a CUDA tensor of bfloat16 or float16, or of whole numbers that stand
+    for their bytes; strides in bytes as for make_shards). Its calls take the batches of make_kvq_batch."""
+    if not buffer.is_cuda or (buffer.dtype.is_floating_point and buffer.dtype not in _types()[2]):
+        raise RempError(REMP_ERR_INVALID_ARG, "the pool must be a CUDA tensor of bfloat16, float16 or whole numbers")
     return make_kvq_pool(buffer, num_blocks, kv_heads, head_dim, block_size, layer, strides)
+
+
+def _of_cache_type(pool, t, name: str) -> None:
+    held = getattr(pool, "keep", None)
+    if held is not None and held.dtype.is_floating_point and held.dtype is not t.dtype:
+        raise RempError(REMP_ERR_INVALID_ARG, f"{name} is of {t.dtype}, the pool of {held.dtype}")
 
 
 @functools.lru_cache(maxsize=None)
@@ -523,6 +531,7 @@ def remp_kv_append(pool: RempKvqPool, batch: RempKvqBatch, q, k, v, q_out, q_nor
                    rope=None, interleaved: bool = False, positions=None, stream=None) -> None:
     """Norm and rotation of q and k, k and v into their pages. Arguments as for remp_kvq_append; the cache is of the tensors'
     type. Only enqueues."""
+    _of_cache_type(pool, k, "k")
     _check(_lib.load().remp_kv_append(*_append_args(pool, batch, q, k, v, q_out, q_norm, k_norm, eps, rope, interleaved, positions),
                                       _stream_ptr(stream)))
 
@@ -531,10 +540,11 @@ def remp_kv_attend(pool: RempKvqPool, batch: RempKvqBatch, q, out, scale: float,
                    lse=None, stream=None) -> None:
     """Causal attention of q [num_tokens][heads][head_dim] over the cached positions of each sequence, into out (same
     shape); window > 0: over the last `window` positions and the `first` ones. lse: float32 [num_tokens][heads] or None.
-    workspace: make_kv_workspace(). Only enqueues."""
+    workspace: make_kv_workspace(). The cache is of q's type. Only enqueues."""
     n, d, dtype = batch.num_tokens, pool.head_dim, q.dtype
     if dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
+    _of_cache_type(pool, q, "q")
     heads = q.shape[1]
     if not workspace.is_cuda or workspace.nbytes < _kv_workspace_bytes():
         raise RempError(REMP_ERR_INVALID_ARG, "the workspace is too small")
@@ -553,10 +563,11 @@ def remp_kv_weigh(pool: RempKvqPool, batch: RempKvqBatch, q, lse, weights, scale
                   fresh: bool = False, stream=None) -> None:
     """weights (float32 [num_seqs][kv_heads][positions]) += the attention weight that the rows q [num_tokens][heads][head_dim]
     give to every cached position they see; lse: float32 [num_tokens][heads] of remp_kv_attend with the same scale, window and first. Positions
-    of the rows themselves, and with `fresh` all of the batch's sequences, are set instead. Only enqueues."""
+    of the rows themselves, and with `fresh` all of the batch's sequences, are set instead. The cache is of q's type. Only enqueues."""
     n, d = batch.num_tokens, pool.head_dim
     if q.dtype not in _types()[2]:
         raise RempError(REMP_ERR_INVALID_ARG, "q must be bfloat16 or float16")
+    _of_cache_type(pool, q, "q")
     heads = q.shape[1]
     _check(_lib.load().remp_kv_weigh(pool, batch, _rows(q, "q", n, heads, d, q.dtype), heads, _types()[2][q.dtype], scale, window, first,
                                      _f32_cuda(lse, "lse", n, heads), _weights(weights, "weights", batch.tables.num_seqs, pool.kv_heads),
