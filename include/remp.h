@@ -446,15 +446,16 @@ remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch
  * the first tokens and the windows) may name anything, also for remp_kv_weigh. A NaN or an infinity in V that a row of the batch
  * sees may reach the other rows of its sequence and KV head that the call computes together with it. Finite values in V may be
  * of any size (in bfloat16 those below 2^-70 lose bits where the sums fall below the normal numbers of 32 bits). An infinity in V
- * gives the rows that see it that infinity in its dim; where both signs are seen, NaN; where their probability of it is below 2^-90
- * (half: 2^-32) of their largest, one or the other.
+ * gives the rows that see it that infinity in its dim; where both signs are seen, NaN; where their probability of it is below 2^-70
+ * (half: 2^-30) of their largest, one or the other.
  *   scale      positive
  *   lse        DEVICE float [num_tokens][q_heads] or NULL
  *   workspace  DEVICE, remp_kv_workspace_bytes() long, 256-byte aligned, ZEROED ONCE before its first use; every call leaves it
  *              ready for the next. Calls that may overlap need workspaces of their own.
- * With at most 16 rows (max_queries * q_heads / kv_heads; 32 with 64 dims) a probability keeps 16 bits and more on its way to the
- * values; with more it is rounded to the cache's type. Sums are in 32 bits throughout. Where a wait of the kernel for more
- * rows runs out its outputs are NaN (error bit 4).
+ * Of a sequence with at most 64 rows (its queries * q_heads / kv_heads) a probability keeps 16 bits and more on its way to the values,
+ * whatever other sequences of the batch have; with more it is rounded to the cache's type. Sums are in 32 bits throughout. Above 16
+ * rows (max_queries * q_heads / kv_heads; 32 with 64 dims) another kernel works; where a wait of its runs out, outputs are NaN (error
+ * bit 4).
  * The result does not depend on the order in which thread blocks run. */
 int64_t remp_kv_workspace_bytes(void);
 remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,

@@ -338,9 +338,8 @@ __global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1) kv_attend_kernel(co
                 sum[c][0] = BF ? held[c][0] : sum[c][0] + held[c][0], sum[c][1] = BF ? held[c][1] : sum[c][1] + held[c][1];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t high, low;
-                    split2<BF>(p[c][2 * h], p[c][2 * h + 1], &high, &low);
-                    high_p[c][h] = transpose8(high), low_p[c][h] = transpose8(low);
+                    const uint32_t first = first2<BF>(p[c][2 * h], p[c][2 * h + 1]);
+                    high_p[c][h] = transpose8(first), low_p[c][h] = transpose8(left2<BF>(p[c][2 * h], p[c][2 * h + 1], first));
                 }
             }
             {

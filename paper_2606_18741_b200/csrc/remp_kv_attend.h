@@ -22,21 +22,22 @@ cudaError_t launch_kv_prompt(const KvAttendArgs& a, int32_t head_dim, bool bf, i
 
 #ifdef __CUDACC__
 
-// Two probabilities as two numbers of the cache's type each: the first bits, rounded towards 0, and what is left, so that neither
-// is below 0; what is left of one above 0 is at least the type's least normal number (bfloat16: 2^-95 of a row's largest and less) or
-// its least number (half: 2^-34). With an infinity in V two numbers above 0 give that infinity, 0 would give NaN.
+// Two probabilities as two numbers of the cache's type each: the first bits, rounded towards 0, and what is left of them, so that
+// neither is below 0. What is left of one above 0 is not 0 either: with an infinity in V, two numbers above 0 give that infinity, 0
+// would give NaN. bfloat16: the last of a probability's 24 bits is set, so 2^-23 of it are left at least (enough from 2^-72 of a row's
+// largest on). Half: it is the type's least number at least, 2^-32 of a row's largest.
 template <bool BF>
-__device__ __forceinline__ void split2(float x, float y, uint32_t* high, uint32_t* low) {
-    constexpr float kLeast = BF ? 0x1p-126f : 0x1p-24f;
-    float2 f;
-    if (BF) {
-        *high = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
-        f = make_float2(bf_low(*high), bf_high(*high));
-    } else {
-        asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(*high) : "f"(y), "f"(x));
-        f = __half22float2(*reinterpret_cast<const __half2*>(high));
-    }
-    *low = pack2(fmaxf(x - f.x, fminf(x, kLeast)), fmaxf(y - f.y, fminf(y, kLeast)), BF);
+__device__ __forceinline__ uint32_t first2(float x, float y) {
+    if (BF) return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+    uint32_t r;
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    return r;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t left2(float x, float y, uint32_t first) {
+    if (BF) return pack2(__uint_as_float(__float_as_uint(x) | 1) - bf_low(first), __uint_as_float(__float_as_uint(y) | 1) - bf_high(first), true);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&first));
+    return pack2(fmaxf(x - f.x, fminf(x, 0x1p-24f)), fmaxf(y - f.y, fminf(y, 0x1p-24f)), false);
 }
 
 #endif

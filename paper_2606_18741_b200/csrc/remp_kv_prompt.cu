@@ -4,8 +4,11 @@
 // Mathematics: softmax(scale * q.K^T + mask).V, one thread block for 256 rows (tokens x query heads of one KV head; two
 // matrices of 128) and a range of the keys, block by block of kKeys keys: S = Q.K^T, P = 2^(S*scale - ref), O += P.V, with a
 // running reference for each row that moves only when its probabilities outgrow a bound.
-// Rounding: P is rounded to the cache's type, the only one that the matrix instructions take beside V; S, O, sums and references are
-// in 32 bits.
+// Rounding: the matrix instructions take P in the cache's type only. Up to 64 rows (drafts, wide groups, single tokens beside a
+// prompt) fill no more than half of a matrix: the other half takes the same rows, and where lane r has the first bits of a
+// probability, lane 64 + r has what is left of it, so it keeps 16 bits and more at no cost in instructions; the two products are added
+// at the end. More rows round it (bfloat16: by 2^-9 at most): a second product of every block would cost half as much again as
+// both products do now. S, O, sums and references are in 32 bits.
 //
 // Bound: tensor cores (4*D flops for each row and key) and, as closely, the exponentials (one for each row and key; 16 a cycle of an
 // SM). Eight warps compute P (a row to a thread), one thread issues the matrix instructions, which run for one matrix while P of the
@@ -119,13 +122,14 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
     // Two matrices take turns: while one's products run, P of the other is made. One alone has two buffers of scores instead, those
     // of the next block are there when P of this one is done.
     const int mats = rows > kRowsM ? 2 : 1, buffers = 3 - mats;
+    const bool twin = rows <= kRowsM / 2;  // lanes 64 and on take the same rows as lanes 0 and on
     // scores of block j: their place, and of the barriers that go with it; the phase of these. What a barrier had before that
     // phase is done when the scores are there, so no wait for a phase meets the one two before it.
     const auto at_of = [&](int mat, int j) { return mat + (j & buffers - 1); };
     const auto turn_of = [&](int j) { return j >> buffers - 1 & 1; };
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            const int warps = max(1, min(4, (rows - (buffers == 2 ? 0 : i) * kRowsM + 31) / 32));  // those without rows make no P
+            const int warps = twin ? 2 * ((rows + 31) / 32) : max(1, min(4, (rows - (buffers == 2 ? 0 : i) * kRowsM + 31) / 32));  // those without rows make no P
             bar_init(s_full + 8 * i, 1), bar_init(p_half + 8 * i, warps), bar_init(p_full + 8 * i, warps), bar_init(o_half + 8 * i, 1), bar_init(o_done + 8 * i, 1);
         }
         for (int i = 0; i < kPlaces; ++i) bar_init(full + 8 * i, 1), bar_init(vacant + 8 * i, 1);
@@ -149,8 +153,10 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         // ---- P and the output: one row to a thread ----
         const int mat = wid >> 2;
         const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), o_at = lanes + Z::kO + mat * D;
-        const int row = row0 + min(tid, rows - 1), token = kv_token_of(a.by_group, row), q_head = head * a.group + row - token * a.group;
-        const bool real = tid < rows, rows_here = (tid & ~31) < rows;  // of this thread, of this warp
+        const bool rest = twin && (tid & kRowsM / 2);  // this thread makes what is left of probabilities
+        const int mine_of = twin && tid < kRowsM ? tid & kRowsM / 2 - 1 : tid;
+        const int row = row0 + min(mine_of, rows - 1), token = kv_token_of(a.by_group, row), q_head = head * a.group + row - token * a.group;
+        const bool rows_here = (mine_of & ~31) < rows, gives = rows_here && !rest, real = mine_of < rows && !rest;  // of this warp, of this thread
         const int limit = min(first_pos + token, len - 1), from = kvq_first_key(first_pos + token, a.window);
         // the warp's 32 rows of Q, coalesced
         if (rows_here) {
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
 #pragma unroll 8
             for (int i = 0; i < 32 / kAtOnce; ++i) {
                 const int in = wid * 32 + i * kAtOnce + lane / kPieces, piece = lane % kPieces;
-                const int r = row0 + min(in, rows - 1), tok = kv_token_of(a.by_group, r);
+                const int r = row0 + min(twin ? in & kRowsM / 2 - 1 : in, rows - 1), tok = kv_token_of(a.by_group, r);
                 const uint4 x = *reinterpret_cast<const uint4*>(a.q.data + (int64_t)(qs + tok) * a.q.s_token + (int64_t)(head * a.group + r - tok * a.group) * a.q.s_head + 8 * piece);
                 *reinterpret_cast<uint4*>(sq + mat * Z::kQ + (piece / 8) * (kRowsM * 128) + (in & 127) * 128 + (((piece % 8) ^ (in & 7)) << 4)) = x;
             }
@@ -205,13 +211,26 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                 tmem_stored();
             }
             // probabilities of a chunk, two to a word, and their sums
+            const auto weigh_pair = [&](const uint32_t(&s)[32], int i, float2(&part)[2]) {
+                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(-ref, -ref));
+                x.x = exp2_approx(x.x), x.y = exp2_approx(x.y);
+                part[i & 1] = add2(part[i & 1], x);
+                return x;
+            };
             const auto weigh = [&](const uint32_t(&s)[32], uint32_t* p, float2(&part)[2]) {
+                if (!twin) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), make_float2(a.scale_log2, a.scale_log2), make_float2(-ref, -ref));
-                    x.x = exp2_approx(x.x), x.y = exp2_approx(x.y);
-                    part[i & 1] = add2(part[i & 1], x);
-                    p[i] = pack2(x.x, x.y, BF);
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 x = weigh_pair(s, i, part);
+                        p[i] = pack2(x.x, x.y, BF);
+                    }
+                } else {  // both, so that all warps go the same way (a branch for each took 76 us where this takes 66)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 x = weigh_pair(s, i, part);
+                        const uint32_t first = first2<BF>(x.x, x.y), left = left2<BF>(x.x, x.y, first);
+                        p[i] = rest ? left : first;
+                    }
                 }
             };
             const auto total_of = [](const float2(&part)[2]) {
@@ -303,6 +322,29 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             __syncwarp();
             tmem_after();
         }
+        // O of this thread's row, dims from i on, in steps of 32; of twins the first bits' and the rest's
+        float* const rests = reinterpret_cast<float*>(sq) + mine_of;  // [dim][64]; the queries have met all keys
+        if (twin && blocks > 0) {
+#pragma unroll 1
+            for (int i = 0; i < (rows_here && rest ? D : 0); i += 32) {
+                uint32_t o[32];
+                tmem_load32(o_at + i, o);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) rests[(i + k) * (kRowsM / 2)] = __uint_as_float(o[k]);
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+        }
+        const auto load_o = [&](int i, uint32_t(&o)[32]) {
+            if (some) {
+                tmem_load32(o_at + i, o);
+                if (twin)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) + rests[(i + k) * (kRowsM / 2)]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = 0;
+            }
+        };
         // Whoever gave up said so before its next arrival, and outputs are behind all arrivals: none that went wrong gets here
         // without the mark.
         if (*static_cast<volatile int*>(&dead)) sum = __uint_as_float(0x7fc00000u);
@@ -310,14 +352,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         if (splits == 1) {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
-            for (int i = 0; i < (rows_here ? D : 0); i += 32) {
+            for (int i = 0; i < (gives ? D : 0); i += 32) {
                 uint32_t o[32];
-                if (some) {
-                    tmem_load32(o_at + i, o);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = 0;
-                }
+                load_o(i, o);
                 if (real)
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
@@ -333,14 +370,9 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
             float* slots = reinterpret_cast<float*>(a.workspace + kAttendCounterBytes);
             float* mine = slots + (int64_t)part_of * Z::kPartFloats;
 #pragma unroll 1
-            for (int i = 0; i < (rows_here ? D : 0); i += 32) {
+            for (int i = 0; i < (gives ? D : 0); i += 32) {
                 uint32_t o[32];
-                if (some) {
-                    tmem_load32(o_at + i, o);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = 0;
-                }
+                load_o(i, o);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) mine[(i + k) * kRows + tid] = __uint_as_float(o[k]);
             }
