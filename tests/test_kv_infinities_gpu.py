@@ -47,3 +47,18 @@ def test_probabilities_that_are_powers_of_two(dtype):
             v[c.tables[0, 2], 5, :, 1::2] = -math.inf
             out, _ = attend(c, c.queries(hq))
             assert (out[..., 0::2] == math.inf).all() and out[..., 1::2].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,score", [(torch.bfloat16, -48.0), (torch.float16, -20.0)])
+def test_probabilities_far_below_the_largest(dtype, score):
+    """2^-69 and 2^-29 of it: still above 0 as two numbers of the cache's type."""
+    for queries, hq in ((1, 8), (2, 8), (5, 8), (20, 8)):
+        for d in (64, 128, 256):
+            c = Case([300], [queries], 1, d, 16, dtype)
+            c.cache.data[:, 0] = 0
+            k, v, block, q = c.cache.slots(0, 0), c.cache.slots(0, 1), c.tables[0, 2], torch.zeros_like(c.queries(hq))
+            q[..., 0] = 4.0
+            k[block, 5, :, 0] = score / 4 * d ** 0.5
+            v[block, 5, :, 0::2] = math.inf
+            out, _ = attend(c, q)
+            assert (out[..., 0::2] == math.inf).all() and torch.isfinite(out[..., 1::2]).all()
