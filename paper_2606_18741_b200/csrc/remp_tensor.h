@@ -109,19 +109,19 @@ constexpr uint32_t kShapeBfloat = 1u << 7 | 1u << 10;  // added to it: bfloat16 
 constexpr uint32_t kShapeBAcross = 1u << 16;           // added to it: B lies in rows along N, not along K
 
 // The whole warp gets here with the same operands (so they stay in uniform registers); the lane with `leads` issues.
-template <int N, uint32_t kMore = 0>
+template <int N>
 __device__ __forceinline__ void mma_smem(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t add, uint32_t leads) {
     asm volatile(
         "{ .reg .pred p, q; .reg .b64 a, b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5};"
-        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a_low), "r"(b_low), "r"(kShape<N> | kMore), "r"(add), "r"(kOperandHigh),
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a_low), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
         "r"(leads)
         : "memory");
 }
-template <int N, uint32_t kMore = 0>
+template <int N>
 __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b_low, uint32_t add, uint32_t leads) {
     asm volatile(
         "{ .reg .pred p, q; .reg .b64 b; setp.ne.b32 p, %4, 0; setp.ne.b32 q, %6, 0; mov.b64 b, {%2, %5};"
-        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b_low), "r"(kShape<N> | kMore), "r"(add), "r"(kOperandHigh),
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b_low), "r"(kShape<N>), "r"(add), "r"(kOperandHigh),
         "r"(leads)
         : "memory");
 }
