@@ -86,6 +86,20 @@ struct Sizes {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {  // not real: 16 bytes of zero
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
+// Two probabilities' first bits, and what is left of them.
+template <bool BF>
+__device__ __forceinline__ uint32_t first2(float x, float y) {
+    if (BF) return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+    uint32_t r;
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    return r;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t left2(float x, float y, uint32_t first) {
+    if (BF) return pack2(fmaf(x, kAndMore, -bf_low(first)), fmaf(y, kAndMore, -bf_high(first)), true);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&first));
+    return pack2(fmaxf(x - f.x, fminf(x, kLeastHalf)), fmaxf(y - f.y, fminf(y, kLeastHalf)), false);
+}
 __device__ __forceinline__ void load_matrices(uint32_t at, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }

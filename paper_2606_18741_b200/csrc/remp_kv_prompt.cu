@@ -173,6 +173,10 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
         __syncwarp();
         if (lane == 0) bar_arrive(q_full);
 
+        // of twins: which part of a probability this thread makes. (Half numbers below 2^-14 have fewer bits than are taken for the first:
+        // 2^-22 of a row's largest probability and less.)
+        const uint32_t sign = rest ? 0x80000000u : 0u;
+        const float keep = rest ? kAndMore : 0.f, least = rest ? kLeastHalf : 0.f;
         float ref = kUnset, sum = 0.f;
 #pragma unroll 1
         for (int j = 0; j < (rows_here ? blocks : 0); ++j) {
@@ -224,12 +228,15 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads, 1) kv_prompt_kernel(const
                         const float2 x = weigh_pair(s, i, part);
                         p[i] = pack2(x.x, x.y, BF);
                     }
-                } else {  // both, so that all warps go the same way (a branch for each took 76 us where this takes 66)
+                } else {  // one way for all warps: x * keep + first bits, with (0, +) or (1 + 2^-22, -)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float2 x = weigh_pair(s, i, part);
-                        const uint32_t first = first2<BF>(x.x, x.y), left = left2<BF>(x.x, x.y, first);
-                        p[i] = rest ? left : first;
+                        constexpr uint32_t kBits = BF ? 0xffff0000u : 0xffffe000u;
+                        float2 y = make_float2(__uint_as_float((__float_as_uint(x.x) & kBits) ^ sign), __uint_as_float((__float_as_uint(x.y) & kBits) ^ sign));
+                        y = fma2(x, make_float2(keep, keep), y);
+                        if (!BF) y = make_float2(fmaxf(y.x, fminf(x.x, least)), fmaxf(y.y, fminf(x.y, least)));
+                        p[i] = pack2(y.x, y.y, BF);
                     }
                 }
             };
