@@ -301,7 +301,10 @@ extern "C" remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_b
     int device = -1, sms = 0;
     REMP_CUDA(cudaGetDevice(&device));
     REMP_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    const bool few = view.num_tokens < sms * 20, bf = dtype == REMP_DTYPE_BFLOAT;
+    // Few tokens: a warp to a group of four sets; many: a token to a warp. Both, us in a graph, for 1000, 2000 and 5000 tokens: 64 + 2 x 8
+    // heads of 128 dims 18 and 23, 29 and 27, 57 and 51; 32 + 2 x 4 with norms 16 and 16, 25 and 18, 45 and 33; 32 + 2 x 8 of 64 dims
+    // 12 and 12, 16 and 14, 29 and 21; 16 + 2 x 2 of 256 14 and 14, 20 and 16, 39 and 31; 300 tokens of these: 8 to 10 and 12 to 20.
+    const bool few = view.num_tokens < sms * 10, bf = dtype == REMP_DTYPE_BFLOAT;
     const int heads = 32 / (d / 8) * (few ? 4 : 2);  // of a group
     if (rows > 0x7fffffffLL - 3 * heads) return fail(REMP_ERR_SHAPE, "too many heads");
     const int q_groups = (q_heads + heads - 1) / heads, kv_groups = (pool->kv_heads + heads - 1) / heads, groups = q_groups + 2 * kv_groups;

@@ -1,5 +1,5 @@
-"""Append to a cache of 16-bit values of so many tokens that a warp takes a whole token (20 and more for each multiprocessor), in all
-its forms. Tolerances: test_kv_gpu."""
+"""Append to a cache of 16-bit values of so many tokens (20 for each multiprocessor) that a warp takes a whole token, in all its forms.
+Tolerances: test_kv_gpu."""
 import pytest
 import torch
 
@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 
 def case(heads, d, bs, dtype, **kw):
-    """A few tokens above the bound, in a prompt, a longer one behind text, and a single token."""
+    """In a prompt, a longer one behind text, and a single token."""
     most = torch.cuda.get_device_properties(0).multi_processor_count * 20
     first = most // 2
     return Case([first, most - first + 40, 7], [first, most - first + 5, 1], heads, d, bs, dtype, **kw)
