@@ -38,10 +38,21 @@ struct Refs {
     static constexpr float room = BF ? -17.f : 14.f, slack = BF ? 14.f : 4.f, bound = BF ? 0x1p-17f : 0x1p14f;
 };
 
-// Rows up to which this kernel takes a sequence; above, the prompt kernel. 24 sequences of 8 KV heads, us in a graph, here and there: 128
-// dims, 24 rows, windows of 2048: 68 (three times 8 rows) and 66, 3000 tokens: 82 and 70, 2 x 30000: 76 and 57; 64 dims, 3000 tokens, 24
-// rows: 48 and 68, 32 rows: 60 and 68.
-constexpr int kPromptRows = 16;
+// Which kernel: this one takes up to 16 rows of a sequence (32 with 64 dims), and more where sequences and KV heads fill the GPU but are so
+// short that a thread block for each costs more than it saves: this one takes a time for each tile and set of its rows, 1.4 ns for
+// the whole GPU with 128 dims, 1.2 with 64, 4.1 with 256; the prompt kernel one for each tile, whatever the rows up to 256 (1.6, 1.6,
+// 2.5), and for each sequence and KV head about 57, 42 and 46 more. Here and there, us in a graph, 8 KV heads: 128 dims, 20 rows, 1000
+// sequences of 50 tokens 135 and 535, 300 of 500 242 and 266, 64 of 500 70 and 72, 24 of 3000 113 and 86, 2 of 16000 61 and 47; 64
+// rows 254 and 553, 438 and 281, 119 and 78, 207 and 94, 98 and 51. 64 dims, 64 rows: 154 and 490, 213 and 258, 68 and 68, 109 and 84, 59
+// and 43; 256 dims, 20 rows: 399 and 586, 674 and 342, 182 and 94, 322 and 131, 164 and 74. Where the GPU is not filled: 128 dims, 8
+// of 400, 20 rows 25 and 18.
+bool prompt_takes(int head_dim, int64_t rows, int64_t units, int sms, int64_t tokens) {
+    const int set = head_dim == 64 ? 32 : 16;
+    if (rows <= set) return false;
+    if (units <= sms) return true;
+    const int64_t sets = (rows + set - 1) / set, tiles = (tokens + kKvqTile - 1) / kKvqTile;
+    return head_dim == 64 ? tiles * (5 * sets - 7) > 180 : head_dim == 128 ? tiles * (7 * sets - 8) > 290 : tiles * (5 * sets - 3) > 55;
+}
 
 struct Seq {  // one sequence's share of the list
     KvqSpan x;
@@ -459,7 +470,9 @@ extern "C" remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_b
     const int64_t max_rows = (int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group;
     const bool bf = dtype == REMP_DTYPE_BFLOAT;
     cudaError_t e;
-    if (max_rows > (pool->head_dim == 64 ? 32 : kPromptRows) && kv_boxes_take(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
+    // cached tokens that a sequence's rows see at most, as far as the host knows
+    const int64_t seen = window > 0 ? std::min<int64_t>(a.room, (int64_t)window + a.first + batch->max_queries) : a.room;
+    if (prompt_takes(pool->head_dim, max_rows, (int64_t)a.v.num_seqs * pool->kv_heads, sms, seen) && kv_boxes_take(a.v)) e = launch_kv_prompt(a, pool->head_dim, bf, sms, (int32_t)max_rows, stream);
     else if (pool->head_dim == 64) e = launch_rows<64, 4>(a, max_rows, bf, sms, stream);
     else if (pool->head_dim == 128) e = launch_rows<128, 2>(a, max_rows, bf, sms, stream);
     else e = launch_rows<256, 2>(a, max_rows, bf, sms, stream);
