@@ -454,8 +454,8 @@ remp_status remp_kv_append(const remp_kv_pool* pool, const remp_kvq_batch* batch
  *              ready for the next. Calls that may overlap need workspaces of their own.
  * Of a sequence with at most 64 rows (its queries * q_heads / kv_heads) a probability keeps 16 bits and more on its way to the values,
  * whatever other sequences of the batch have; with more it is rounded to the cache's type. Sums are in 32 bits throughout. Above 16
- * rows (max_queries * q_heads / kv_heads; 32 with 64 dims) another kernel works; where a wait of its runs out, outputs are NaN (error
- * bit 4).
+ * rows (max_queries * q_heads / kv_heads; 32 with 64 dims), but for many short sequences, another kernel works; where a wait of its
+ * runs out, outputs are NaN (error bit 4).
  * The result does not depend on the order in which thread blocks run. */
 int64_t remp_kv_workspace_bytes(void);
 remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q,
@@ -470,7 +470,7 @@ remp_status remp_kv_attend(const remp_kv_pool* pool, const remp_kvq_batch* batch
  *   weights  DEVICE float [num_seqs][kv_heads][stride]; of sequences longer than `stride` the positions behind it are left out
  *            (error bit 1)
  * Each weight is added up in a fixed order, so the result does not depend on the run. With more than 24 rows (max_queries * q_heads /
- * kv_heads) another kernel works; where a wait of its runs out, the weights that it has not written are NaN (error bit 4). */
+ * kv_heads), but for many short sequences, another kernel works; where a wait of its runs out, the weights that it has not written are NaN (error bit 4). */
 remp_status remp_kv_weigh(const remp_kv_pool* pool, const remp_kvq_batch* batch, const remp_kvq_rows* q, int32_t q_heads,
                           int32_t dtype, float scale, int32_t window, int32_t first, const float* lse, float* weights,
                           int64_t stride, int32_t fresh, void* stream);

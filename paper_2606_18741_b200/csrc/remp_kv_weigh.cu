@@ -18,9 +18,16 @@ namespace remp {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-// Rows up to which this kernel takes a sequence; above, the wide one. Two sequences of 16383 tokens, 8 rows to a query: 18 us here and 20
-// there with 2 queries, 25 and 20 with 4, 59 and 23 with 16; 64 sequences of 500 tokens: 20 and 27, 27 and 27, 63 and 35.
-constexpr int kWideRows = 24;
+// Which kernel: this one takes up to 24 rows of a sequence, and more where sequences and KV heads fill the GPU but are so short that a
+// thread block for each costs more than it saves: this one takes a time for each tile and set of 8 rows (0.3 ns for the whole GPU,
+// 0.6 with 256 dims), the wide one for each tile, whatever the rows up to 256 (1.0 to 1.3), and for each sequence and KV head about 30
+// ns. Here and there, us in a graph, 8 KV heads of 128 dims: 24 rows, 300 sequences of 500 tokens 117 and 150, 64 of 500 33 and 41, 24
+// of 3000 59 and 70, 2 of 16000 31 and 29; 32 rows 143 and 150, 37 and 41, 70 and 68, 35 and 29; 48 rows 188 and 156, 45 and 43, 90 and
+// 70, 45 and 29; 1000 of 50 57, 68 and 86, and 266 to 291; 8 of 100, 64 rows 16 and 12. 256 dims, 32 rows: 244 and 170, 57 and 51.
+bool wide_takes(int head_dim, int64_t rows, int64_t units, int sms, int64_t tokens) {
+    const int64_t sets = (rows + 7) / 8, tiles = (tokens + kKvqTile - 1) / kKvqTile;
+    return rows > 24 && (units <= sms || tiles * (2 * sets - 3) > (head_dim == 256 ? 100 : 200));
+}
 
 struct Seq {
     KvqSpan x;
@@ -225,7 +232,8 @@ extern "C" remp_status remp_kv_weigh(const remp_kv_pool* pool, const remp_kvq_ba
     a.room = (int32_t)std::min<int64_t>(std::min<int64_t>((int64_t)a.v.max_blocks * a.v.block_tiles * kKvqTile, kKvqMost), stride);
     const bool bf = dtype == REMP_DTYPE_BFLOAT;
     const int d = pool->head_dim;
-    if ((int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group > kWideRows && kv_boxes_take(a.v)) {
+    const int64_t seen = window > 0 && !fresh ? std::min<int64_t>(a.room, (int64_t)window + a.first + batch->max_queries) : a.room;
+    if (wide_takes(d, (int64_t)std::min(batch->max_queries, batch->num_tokens) * a.group, (int64_t)a.v.num_seqs * pool->kv_heads, sms, seen) && kv_boxes_take(a.v)) {
         REMP_CUDA(launch_kv_weigh_wide(a, d, bf, sms, static_cast<cudaStream_t>(stream_)));
         return REMP_OK;
     }
