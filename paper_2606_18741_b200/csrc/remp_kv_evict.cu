@@ -3,8 +3,8 @@
 // The choice, one (sequence, KV head) to a thread block, or to a cluster of them for long sequences: weights become whole numbers of the
 // same order and stay in registers, kKeys to a thread. The smallest weight that stays is found by counting: the range from the
 // least to the most is cut into kThreads equal stretches of a power of two, the weights in each are counted in shared memory (a cluster adds its
-// blocks' counts over distributed shared memory), and the stretch that holds it is the next range: two rounds for most weights, four
-// at most, where two bits at a time took seventeen. Places in the list follow from counts of (round of 32 positions, warp), so equal weights stay lowest
+// blocks' counts over distributed shared memory), and the stretch that holds it is the next range: three or four rounds, eight to ten bits of
+// the range each, where two bits at a time took seventeen. Places in the list follow from counts of (round of 32 positions, warp), so equal weights stay lowest
 // position first and the list is ascending, whatever the order in which threads run.
 //
 // The move, in place: row i comes from position kept[i] >= i, ascending, so a chunk of rows may be written once it AND ALL BEFORE IT

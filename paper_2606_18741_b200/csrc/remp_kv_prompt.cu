@@ -20,8 +20,9 @@
 //
 // Measured, 2 x 2048 queries of 32 heads over 8191 tokens of 4 KV heads, 128 dims (us in a graph): 752 with 16-byte copies by three
 // warps; 570 with boxes of 64 dims; 553 with one thread that waits and issues (a warp took 200 cycles for each wait and 80 for each
-// instruction); 473 with boxes of all dims (a box costs the copy engine some 100 cycles, 2 KB or 4); 438 with masks out of the loop:
-// 1.1 PFLOP/s. A quarter, third or half of the exponentials as polynomials took 459, 467, 479: with two warps on a scheduler the instructions
+// instruction); 473 with boxes of all dims (a box costs the copy engine some 100 cycles, 2 KB or 4); 438 with masks out of the loop;
+// 425 with references that leave a sum of 2^20 times the largest probability room: 1.13 PFLOP/s. (All at 1965 MHz. A second of such calls
+// in a row draws 950 W, the clock falls to 1.77 GHz, and a call or a replay takes 470.) A quarter, third or half of the exponentials as polynomials took 459, 467, 479: with two warps on a scheduler the instructions
 // that this adds cost more than the exponentials that it saves.
 // Slots that no row sees: their scores are masked, their values are not fetched but zeroed, so what they hold is never used.
 //
